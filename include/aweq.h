@@ -33,7 +33,7 @@
 extern "C" {
 #endif
 
-typedef enum { AWEQ_F32 = 0, AWEQ_F16 = 1, AWEQ_I8 = 2 } aweq_dtype;
+typedef enum { AWEQ_F32 = 0, AWEQ_F16 = 1, AWEQ_I8 = 2, AWEQ_BF16 = 3 } aweq_dtype;   /* AWEQ_BF16: where an entry point names it */
 
 enum {
     AWEQ_OK = 0,
@@ -53,8 +53,9 @@ enum {
     AWEQ_ST_NONFINITE = 2u,  /* NaN / Inf seen in the input (results unspecified) */
     AWEQ_ST_BIGQUOT = 4u,    /* |x / Step| >= 2^24: quotient saturated */
     AWEQ_ST_SCALEGUARD = 8u, /* Eq. 10: a channel range was < 1e-5 (s := 1) or s was clamped to [1e-4, 1e4] */
-    AWEQ_ST_ZEROPOINT = 16u  /* stage 4 de-quantisation met a zero point outside [0, 255] (a slice whose range does not
+    AWEQ_ST_ZEROPOINT = 16u, /* stage 4 de-quantisation met a zero point outside [0, 255] (a slice whose range does not
                                 contain 0): its 32-bit integer part is exact only while it fits in 32 bits */
+    AWEQ_ST_INDEX = 32u      /* a page, slot or length on the device lies outside what the call was given: clamped or left out */
 };
 
 typedef enum {
@@ -339,6 +340,92 @@ typedef struct {
 } aweq_calib_weight;
 
 int aweq_calibrate(const aweq_calib_layer* layer, const aweq_calib_weight* weights, int n_weights, void* stream);   /* both host structures */
+
+/* ======== Around the quantised layers of a deployed decoder: a product whose tokens carry scales of their own, and the
+ * attention block between the projections ========
+ *
+ * ---- Quantizer of Eq. 1-2 with b = 8 and a token as the slice.  x[t,k] = X[t,k] * inv_s[k] (one fp32 multiply; inv_s nullable: X is
+ * equalised already).  The token's range is widened to contain 0, so that its zero point lies in [0, 255] and a 0 stays a 0:
+ *   lo = min(0, min_k x), hi = max(0, max_k x), step_x[t] = (hi - lo) / 255 (1 for a token of zeros), zero_x[t] = -round(lo / step),
+ *   xq[t,k] = clamp(round(x / step) + zero, 0, 255) - 128, rowsum_x[t] = sum_k xq        (true fp32 divisions, ties to even).
+ * X[T x K] F32, F16 or BF16, pitch ldx; K <= 32768; xq in the K-panel layout (aweq_panel_bytes(T, K)).  A NaN or infinity raises
+ * AWEQ_ST_NONFINITE (the results of that token are unspecified). */
+int aweq_quant_tokens(const void* X, aweq_dtype dt, int64_t T, int64_t K, int64_t ldx, const float* inv_s,
+                      int8_t* xq, float* step_x, int32_t* zero_x, int32_t* rowsum_x, uint32_t* status, void* stream);
+
+/* ---- Product in 8-bit integers with a (Step, Z) for each token and each output channel.  X F32 / F16 / BF16 is quantised by
+ * aweq_quant_tokens first (xq, step_x, zero_x, rowsum_x are written); X I8 (ldx = K) already is xq, and step_x, zero_x, rowsum_x
+ * are inputs (zero_x in [0, 255], as aweq_quant_tokens writes them).  wq, step_w, zero_w, w_group, rowsum_w, bias (nullable): the
+ * weight as in aweq_w8a8_gemm.
+ *   out[t,n] = step_x[t] step_w[n] (acc - Z'x[t] rowsum_w[n] - Z'w[n] rowsum_x[t] + K Z'x[t] Z'w[n]) + bias[n],  Z' = Z - 128,
+ * the integer exact in 32 bits (zero_w outside [0, 255]: AWEQ_ST_ZEROPOINT, as there), scaled in fp64 and rounded once to out_dt (F32, F16,
+ * BF16; pitch ldo).  K % 8 == 0, K <= 32768, N % 4 == 0, ldo % 4 == 0, 16-byte aligned pointers. */
+int aweq_w8a8_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, int64_t K, int64_t ldx, const float* inv_s,
+                          int8_t* xq, float* step_x, int32_t* zero_x, int32_t* rowsum_x,
+                          const int8_t* wq, int64_t N, const float* step_w, const int32_t* zero_w, int w_group,
+                          const int32_t* rowsum_w, const float* bias, void* out, aweq_dtype out_dt, int64_t ldo,
+                          uint32_t* status, void* stream);
+
+/* ---- Rotation by position.  The pair i of a head's first `rot` values turns by pos * freq[i], i < rot / 2: (x[i], x[i + rot / 2]), or with
+ * interleaved (x[2i], x[2i + 1]).  aweq_rope_frequencies fills freq[rot / 2] (HOST memory, binary64) with base^(-2i / rot), scaled for contexts
+ * `factor` times the trained length:
+ *   AWEQ_ROPE_PLAIN   as it is
+ *   AWEQ_ROPE_LINEAR  freq / factor (positions pressed together)
+ *   AWEQ_ROPE_BASE    base * factor^(rot / (rot - 2)): the slowest pair turns factor times slower, the fastest as before (rot > 2)
+ *   AWEQ_ROPE_PARTS   by the turns a pair makes over the trained length: above `high` as it is, below `low` freq / factor, between
+ *                     them blended linearly in the turns.
+ * Host function; AWEQ_ERR_SHAPE for rot odd or <= 0, base <= 0 (or not finite), factor <= 0, an unknown kind, or (PARTS) trained <= 0 or high <= low. */
+enum { AWEQ_ROPE_PLAIN = 0, AWEQ_ROPE_LINEAR = 1, AWEQ_ROPE_BASE = 2, AWEQ_ROPE_PARTS = 3 };
+int aweq_rope_frequencies(int64_t rot, double base, int kind, double factor, double trained, double low, double high, double* freq);
+
+/* ---- Norm of every head of the queries and keys and their rotation, in one pass.  q[T][Hq][D], k[T][Hk][D] (F32, F16 or BF16; the heads
+ * of a token side by side, pitch ldq / ldk from token to token: parts of the fused projection's rows will do); q or k nullable.
+ *   y = x * w[d] / sqrt(mean_d x^2 + eps)   (q_norm / k_norm fp32[D]; NULL: y = x)
+ *   rotated by pos[t] (int32, any sign) as above, cosine and sine times gain; values past rot are left as they are.
+ * Norm, angle (reduced in binary64) and rotation are not rounded in between; outputs once, to dt (pitch ldqo, ldko).  q_out may be q, and k_out
+ * k, with the same pitch.  rot = 0: the norms alone (pos and freq may be NULL); else rot <= D, a multiple of 16, or of 8 with interleaved.
+ * D % 8 == 0, D <= 256; 16-byte aligned pointers and pitches (freq and pos: of their type). */
+int aweq_qk_rope(const void* q, const void* k, aweq_dtype dt, int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t ldq, int64_t ldk,
+                 const int32_t* pos, const double* freq, int64_t rot, int interleaved, float gain,
+                 const float* q_norm, const float* k_norm, float eps, void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* stream);
+
+/* ---- A paged cache of keys and values.  k_cache and v_cache hold `pages` pages of Hk heads of page_size tokens of D values each,
+ * [pages][Hk][page_size][D], in the queries' type (F16 or BF16), or as 8-bit codes (cache_dt = AWEQ_I8) with k_step and v_step
+ * [pages][Hk][page_size] fp32: the value is code * step, step = max |x| / 127 of the token's head (1 if that is 0), code = round(x / step).
+ * (Symmetric, unlike the quantizers above: a zero point would cost a correction of every score.)  page_size: a power of two from 16 to 256.
+ *
+ * aweq_kv_append: aweq_qk_rope, with the keys, and the values v[T][Hk][D] (pitch ldv) as they are, going to the cache: token t to row slot[t] %
+ * page_size of page slot[t] / page_size (int64; negative: the token is left out of the cache, a padded batch; past the last page: the
+ * same, and AWEQ_ST_INDEX).  Tokens of one call must not share a slot.  An 8-bit code is made of the rotated value before any other rounding.  q
+ * nullable (with q_out).  D % 8 == 0 and D <= 256; dt F16 or BF16. */
+int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, int64_t T, int64_t Hq, int64_t Hk, int64_t D,
+                   int64_t ldq, int64_t ldk, int64_t ldv, const int32_t* pos, const double* freq, int64_t rot, int interleaved, float gain,
+                   const float* q_norm, const float* k_norm, float eps, void* q_out, int64_t ldqo,
+                   void* k_cache, void* v_cache, float* k_step, float* v_step, aweq_dtype cache_dt, int64_t pages, int64_t page_size,
+                   const int64_t* slot, uint32_t* status, void* stream);
+
+/* ---- Attention of a batch over a prefix that all its sequences share and over each one's own pages.  q[T][Hq][D] (F16 or BF16, pitch
+ * ldq): the new tokens of B sequences one after the other, those of sequence b from q_start[b] to q_start[b + 1] (int32[B + 1]; NULL: one each, T = B).
+ * Query head h reads key head h / (Hq / Hk).  The keys of a token are
+ *   the prefix: the first prefix_len tokens of the pages prefix_table[ceil(prefix_len / page_size)] (int32; prefix_len a HOST number, 0: none), and
+ *   its sequence's own: lens[b] tokens (int32, 0 allowed) of the pages table[b][..] (int32, pitch table_ld), of which the last ones are its
+ *   new tokens, appended before this call: new token i of m sees the first lens[b] - m + 1 + i of them.
+ *   out[t][h] = sum_j p_j v_j,  p = softmax(scale * q k_j);   lse[t][h] (fp32, nullable) = log sum_j exp(scale * q k_j).
+ * A token without any key gets zeros, and lse -inf.  max_len and max_q (HOST): no lens[b] and no sequence's count of new tokens is larger; the launch is
+ * laid out for them.  A page outside [0, pages), a length over max_len or over what table_ld pages hold, or rows of q_start out of order
+ * raise AWEQ_ST_INDEX and are clamped (results unspecified, no access out of range).
+ * The prefix is read once for all the batch's queries, which multiply its keys together; long key ranges are split between
+ * workgroups whose partial results (fp32, in ws) a second launch joins.  Scores and softmax in fp32, with products of the stored
+ * type exact in fp32; the probabilities are rounded to F16 / BF16 for the product with v (BF16 queries over an 8-bit cache: both
+ * products in F16, the queries scaled by a power of two).  D 64, 128 or 256; Hq a multiple of Hk; cache as above.
+ * ws: aweq_prefix_attention_ws(...) bytes, 16-byte aligned (host function). */
+size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len);
+int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int64_t D, int64_t ldq,
+                          const void* k_cache, const void* v_cache, const float* k_step, const float* v_step, aweq_dtype cache_dt,
+                          int64_t pages, int64_t page_size, int64_t Hk, const int32_t* prefix_table, int64_t prefix_len,
+                          const int32_t* table, int64_t table_ld, const int32_t* lens, const int32_t* q_start, int64_t B,
+                          int64_t max_len, int64_t max_q, float scale, void* out, int64_t ldo, float* lse,
+                          void* ws, size_t ws_bytes, uint32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

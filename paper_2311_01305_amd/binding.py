@@ -17,19 +17,21 @@ _lib = None
 _calls = None    # the extension module, bound to the library
 _torch = None
 
-AWEQ_F32, AWEQ_F16, AWEQ_I8 = 0, 1, 2
+AWEQ_F32, AWEQ_F16, AWEQ_I8, AWEQ_BF16 = 0, 1, 2, 3
 OP_CALIB_STATS, OP_EQUALIZE, OP_QUANT_WEIGHT, OP_W8A8_GEMM, OP_BIAS_CORRECT, OP_WONLY_GEMM, OP_QUANT_ACT, OP_CALIBRATE = range(8)
 BIAS_W8A8, BIAS_WEIGHT_ONLY = 0, 1
 SCALE_NONE, SCALE_RANGE, SCALE_ABSMAX = 0, 1, 2
-ST_DEGENERATE, ST_NONFINITE, ST_BIGQUOT, ST_SCALEGUARD, ST_ZEROPOINT = 1, 2, 4, 8, 16
+ST_DEGENERATE, ST_NONFINITE, ST_BIGQUOT, ST_SCALEGUARD, ST_ZEROPOINT, ST_INDEX = 1, 2, 4, 8, 16, 32
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 
 EXPORTS = ("aweq_workspace_size", "aweq_status_string", "aweq_calib_stats", "aweq_equalize",
            "aweq_quant_weight", "aweq_quant_act", "aweq_w8a8_gemm", "aweq_bias_correct",
            "aweq_panel_bytes", "aweq_pack_panels_i8", "aweq_unpack_panels_i8", "aweq_wonly_gemm", "aweq_fold_quant_weight", "aweq_w8a8_gemm_fused",
-           "aweq_calib_stats_static", "aweq_calibrate")
+           "aweq_calib_stats_static", "aweq_calibrate", "aweq_quant_tokens", "aweq_w8a8_gemm_tokens", "aweq_rope_frequencies", "aweq_qk_rope",
+           "aweq_kv_append", "aweq_prefix_attention_ws", "aweq_prefix_attention")
 STATIC_SCRATCH_BYTES = 16 << 20
 
-_vp, _i64, _i32, _u64, _f32, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_uint64, C.c_float, C.c_size_t
+_vp, _i64, _i32, _u64, _f32, _f64, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_uint64, C.c_float, C.c_double, C.c_size_t
 
 
 class AweqError(RuntimeError):
@@ -62,6 +64,10 @@ def load_library():
     lib.aweq_pack_panels_i8.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp]
     lib.aweq_unpack_panels_i8.restype = _i32
     lib.aweq_unpack_panels_i8.argtypes = [_vp, _i64, _i64, _vp, _i64, _vp]
+    lib.aweq_rope_frequencies.restype = _i32
+    lib.aweq_rope_frequencies.argtypes = [_i64, _f64, _i32, _f64, _f64, _f64, _f64, _vp]
+    lib.aweq_prefix_attention_ws.restype = _sz
+    lib.aweq_prefix_attention_ws.argtypes = [_i64] * 8
     spec = importlib.util.spec_from_loader("_native", importlib.machinery.ExtensionFileLoader("_native", _NATIVE_PATH))
     calls = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(calls)
@@ -214,3 +220,42 @@ def aweq_calibrate(layer, weights, stream=None):
     """layer: the fields of aweq_calib_layer in order; weights: a sequence of the fields of aweq_calib_weight in order.  Tensors, addresses,
     integers or None."""
     _check((_calls or _native()).aweq_calibrate(layer, weights, _stream(stream)))
+
+
+def aweq_quant_tokens(X, dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, status=None, stream=None):
+    _check((_calls or _native()).aweq_quant_tokens(X, dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, status, _stream(stream)))
+
+
+def aweq_w8a8_gemm_tokens(X, x_dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, wq, N, step_w, zero_w, w_group, rowsum_w, bias, out, out_dt,
+                          ldo, status=None, stream=None):
+    _check((_calls or _native()).aweq_w8a8_gemm_tokens(X, x_dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, wq, N, step_w, zero_w,
+                                                       int(w_group), rowsum_w, bias, out, out_dt, ldo, status, _stream(stream)))
+
+
+def aweq_rope_frequencies(rot, base, freq, kind=ROPE_PLAIN, factor=1.0, trained=0.0, low=1.0, high=4.0):
+    """freq: a host array or CPU tensor of rot / 2 binary64 values."""
+    address = freq if freq is None or isinstance(freq, int) else freq.ctypes.data if hasattr(freq, "ctypes") else freq.data_ptr()
+    _check(load_library().aweq_rope_frequencies(int(rot), float(base), int(kind), float(factor), float(trained), float(low), float(high), address))
+
+
+def aweq_qk_rope(q, k, dt, T, Hq, Hk, D, ldq, ldk, pos, freq, rot, interleaved, gain, q_norm, k_norm, eps, q_out, ldqo, k_out, ldko, stream=None):
+    _check((_calls or _native()).aweq_qk_rope(q, k, dt, T, Hq, Hk, D, ldq, ldk, pos, freq, rot, interleaved, gain, q_norm, k_norm, eps,
+                                              q_out, ldqo, k_out, ldko, _stream(stream)))
+
+
+def aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, ldq, ldk, ldv, pos, freq, rot, interleaved, gain, q_norm, k_norm, eps, q_out, ldqo, k_cache, v_cache,
+                   k_step, v_step, cache_dt, pages, page_size, slot, status=None, stream=None):
+    _check((_calls or _native()).aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, ldq, ldk, ldv, pos, freq, rot, interleaved, gain, q_norm, k_norm,
+                                                eps, q_out, ldqo, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, slot, status,
+                                                _stream(stream)))
+
+
+def aweq_prefix_attention_ws(T, Hq, Hk, D, B, max_q, prefix_len, max_len):
+    return int(load_library().aweq_prefix_attention_ws(int(T), int(Hq), int(Hk), int(D), int(B), int(max_q), int(prefix_len), int(max_len)))
+
+
+def aweq_prefix_attention(q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, prefix_table, prefix_len, table,
+                          table_ld, lens, q_start, B, max_len, max_q, scale, out, ldo, lse, ws, status=None, stream=None, ws_bytes=None):
+    _check((_calls or _native()).aweq_prefix_attention(
+        q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, prefix_table, prefix_len, table, table_ld, lens,
+        q_start, B, max_len, max_q, scale, out, ldo, lse, ws, _nbytes(ws) if ws_bytes is None else ws_bytes, status, _stream(stream)))

@@ -26,6 +26,7 @@
 // Workgroups are numbered so that the ones resident on one XCD (which share an L2) form a
 // compact patch of the output.
 #include "gemm_i8.hpp"
+#include "gemm_tokens.hpp"
 #include "quant_act.hpp"
 #include "row_reduce.hpp"
 #include <type_traits>
@@ -299,7 +300,8 @@ __device__ __forceinline__ void wait_vm()
 // EPI (with DEQ == 2): bit 0 collects the column statistics of the binary16 output, bit 1 quantises
 // it for the next layer; STORE = false keeps the output itself from being written.
 // Args: GemmArgs, or GroupArgs for several weights.
-template <int MI, bool I32, int DEQ, bool COLSUM, int EPI = 0, bool STORE = true, class Args = GemmArgs>
+// TOK: Step and Z of the activations are a token's (the arrays act_step and act_zero), DEQ 3: bfloat16 output then.
+template <int MI, bool I32, int DEQ, bool COLSUM, int EPI = 0, bool STORE = true, class Args = GemmArgs, bool TOK = false>
 __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
 {
     using TL = Tile<MI>;
@@ -312,7 +314,9 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
     // passes of the general form in one piece: all of them where it is the only form; beside the short ones as many as cost no registers
     // (the next layer's codes with |Z| beyond 4096, 1 -> 4: 1024 tokens 16384 x 4096 85.3 -> 84.3, 2000 x 4096 x 1024 28.1 -> 27.7; 8 spill)
     constexpr int kUnroll = !kQuick ? 8 : EPI != 0 ? 4 : 1;
-    constexpr bool kMayShare = kQuick && DEQ == 2 && EPI == 0 && !COLSUM && MI == 4;   // has the form for rows that share lines (kShared)
+    static_assert(!TOK || (EPI == 0 && STORE && !I32 && !COLSUM && DEQ != 0 && !kGroup), "the output alone");
+    static_assert(TOK || DEQ != 3, "no other form stores bfloat16");
+    constexpr bool kMayShare = kQuick && DEQ >= 2 && EPI == 0 && !COLSUM && MI == 4;   // has the form for rows that share lines (kShared)
     constexpr int kSlot = TL::kSlot, kHalfA = TL::kHalfA, kAhead = TL::kAhead, kLoads = TL::kLoads;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -535,7 +539,8 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
         }
         // everything the epilogue reads from memory is requested before the next tile's panels,
         // so that waiting for it does not wait for them
-        int rsx[MI / 2] = {};   // row sums of this wave's 32 MI tokens, one per lane and 64: token 64 h + lane
+        int rsx[MI / 2] = {};   // row sums of this wave's 32 MI tokens, one per lane and 64: token 64 h + lane (TOK: 256 times that, with Z'x in the low byte)
+        float sxx[MI / 2] = {};   // (TOK) their Steps
         Float4 sw = {{0.f, 0.f, 0.f, 0.f}}, bs = {{0.f, 0.f, 0.f, 0.f}};
         int nzw[4] = {0, 0, 0, 0};          // -Z'w = 128 - Z_w of this lane's channels
         unsigned cn[4] = {0, 0, 0, 0};      // K Z'x Z'w - Z'x rowsum_w, in wrap-around 32-bit arithmetic
@@ -543,10 +548,12 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
         int zx = 0;
         float sxf = 0.f;
         if constexpr (DEQ != 0) {
-            zx = *g.act_zero - 128;
-            sxf = *g.act_step;
-            zx = __builtin_amdgcn_readfirstlane(zx);
-            sxf = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(sxf)));
+            if constexpr (!TOK) {
+                zx = *g.act_zero - 128;
+                sxf = *g.act_step;
+                zx = __builtin_amdgcn_readfirstlane(zx);
+                sxf = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(sxf)));
+            }
             // the integer part is formed in 32-bit arithmetic: exact while it fits, which zero points in
             // [0, 255] guarantee for K <= 32768; anything else is flagged
             if (zx < -128 || zx > 127) est |= AWEQ_ST_ZEROPOINT;
@@ -554,6 +561,10 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
             for (int hh = 0; hh < MI / 2; ++hh) {
                 const int64_t t = cm0 + wm * (32 * MI) + hh * 64 + lane;
                 rsx[hh] = t < g.T ? g.rowsum_x[t] : 0;
+                if constexpr (TOK) {
+                    rsx[hh] = (int)((unsigned)rsx[hh] << 8) | ((t < g.T ? g.act_zero[t] - 128 : 0) & 255);   // (|row sum| <= 2^22)
+                    sxx[hh] = t < g.T ? g.act_step[t] : 0.0f;
+                }
             }
             if (n_ok) {
                 v4i zw4;
@@ -571,14 +582,18 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
                 for (int c = 0; c < 4; ++c) {
                     nzw[c] = 128 - zw4[c];
                     if (zw4[c] < 0 || zw4[c] > 255) est |= AWEQ_ST_ZEROPOINT;
-                    cn[c] = 0u - (unsigned)g.K * (unsigned)zx * (unsigned)nzw[c] - (unsigned)zx * (unsigned)rw4[c];
+                    if constexpr (TOK) cn[c] = (unsigned)rw4[c] + (unsigned)g.K * (unsigned)nzw[c];   // A: the sum of u - Z
+                    else cn[c] = 0u - (unsigned)g.K * (unsigned)zx * (unsigned)nzw[c] - (unsigned)zx * (unsigned)rw4[c];
                 }
                 if (bias) bs = *reinterpret_cast<const Float4*>(bias + n);
             }
             // pin the values in registers here: the compiler's wait for them then sits before the
             // panel requests below, which it cannot see, instead of behind them
 #pragma unroll
-            for (int hh = 0; hh < MI / 2; ++hh) asm volatile("" : "+v"(rsx[hh]));
+            for (int hh = 0; hh < MI / 2; ++hh) {
+                asm volatile("" : "+v"(rsx[hh]));
+                if constexpr (TOK) asm volatile("" : "+v"(sxx[hh]));
+            }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 asm volatile("" : "+v"(sw.f[c]));
@@ -628,7 +643,10 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
         if constexpr (kQuick) {
             if constexpr (DEQ != 0) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) odd = odd || nzw[c] >= (1 << 23) || nzw[c] <= -(1 << 23);
+                for (int c = 0; c < 4; ++c) {
+                    odd = odd || nzw[c] >= (1 << 23) || nzw[c] <= -(1 << 23);
+                    if constexpr (TOK) odd = odd || (int)cn[c] >= (1 << 23) || (int)cn[c] <= -(1 << 23);
+                }
             }
             const bool inside = cm0 + TL::kRows <= g.T && cn0 + BN <= g.N;
             // Rows that do not begin at multiples of 64 bytes share lines with the next tile's, written by another workgroup a little earlier
@@ -679,9 +697,14 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
         uint32_t cq02 = 0, cq13 = 0;   // column sums of the unsigned codes, two channels (16 bits each: 32 rows)
         int cpart[4] = {0, 0, 0, 0};
         // fp64 product and sum of the exact integer, as in the general form; |Z'w| and |row sum| < 2^23: a 24-bit multiply-add
-        auto dequantise = [&](const v4i& o, int rs, float y[4]) {
+        auto dequantise = [&](const v4i& o, int rs, float y[4], float sx = 0.0f) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
+                if constexpr (TOK) {   // (|Z'x| and |A| fit 24 bits as well)
+                    const int iv = (int)((unsigned)o[c] + (unsigned)__mul24(nzw[c], rs >> 8) - (unsigned)__mul24((int)cn[c], (int)(int8_t)rs));
+                    y[c] = DEQ == 1 ? token_scaled_f32(iv, sx, sw.f[c], bs.f[c]) : token_scaled(iv, sx, sw.f[c], bs.f[c]);
+                    continue;
+                }
                 const double div = (double)(int)((unsigned)o[c] + cn[c] + (unsigned)__mul24(nzw[c], rs));
                 if constexpr (DEQ == 1) y[c] = (float)(div * scale[c] + bsd[c]);
                 else y[c] = (float)__builtin_fma(div, scale[c], bsd[c]);
@@ -715,6 +738,9 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
             tie = dmax > nthr;
             return w;
         };
+        auto step_of = [&](int i, int p) {
+            return __int_as_float(__builtin_amdgcn_ds_bpermute(((i & 1) * 32 + 4 * p) * 4 + rd_r * 4, __float_as_int(sxx[i >> 1])));
+        };
         auto row_sum_of = [&](int i, int p) { return __builtin_amdgcn_ds_bpermute(((i & 1) * 32 + 4 * p) * 4 + rd_r * 4, rsx[i >> 1]); };
         auto slab_row = [&](int p) { return *reinterpret_cast<const v4i*>(slab + (4 * p + rd_r) * 256 + ((rd_c ^ (4 * (p & 3) + rd_r)) * 16)); };
         // The eight passes over sub-tile row i of the short forms.  A tile's epilogue is vector operations of 4.5 cycles each
@@ -731,6 +757,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
             // a pass's accumulators and row sum are requested one pass ahead
             v4i next_o = slab_row(0);
             int next_rs = DEQ != 0 ? row_sum_of(i, 0) : 0;
+            float next_sx = TOK ? step_of(i, 0) : 0.0f;
 #pragma unroll 1
             for (int p4 = 0; p4 < 8; p4 += 4)
 #pragma unroll
@@ -739,17 +766,26 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
                 const int pn = p_ < 3 ? p + 1 : (p4 + 4) & 7;   // (after the last one: the first again, not used)
                 const v4i o = next_o;
                 const int rs = next_rs;
+                const float sx = next_sx;
                 next_o = *reinterpret_cast<const v4i*>(slab + pn * 1024 + (rd_r * 256 + ((rd_c ^ (4 * ((p_ + 1) & 3) + rd_r)) * 16)));
                 if constexpr (DEQ != 0) next_rs = row_sum_of(i, pn);
+                if constexpr (TOK) next_sx = step_of(i, pn);
                 SB();
                 const bool in = !EDGE || i * 32 + 4 * p < lim;
                 if constexpr (DEQ != 0) {
                     float y[4];
-                    dequantise(o, rs, y);
+                    dequantise(o, rs, y, sx);
                     if constexpr (DEQ == 1) {
                         typedef float f4 __attribute__((ext_vector_type(4)));
                         if (in) __builtin_nontemporal_store(f4{y[0], y[1], y[2], y[3]}, reinterpret_cast<f4*>(row_deq + (uint64_t)(lane_elt * 4u)));
                         row_deq += 16 * g.ldo;
+                    } else if constexpr (DEQ == 3) {
+                        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                        b4* const d = reinterpret_cast<b4*>(row_deq + (uint64_t)(lane_elt * 2u));
+                        const b4 o4 = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+                        if constexpr (CACHED) { if (in) *d = o4; }
+                        else if (in) __builtin_nontemporal_store(o4, d);
+                        row_deq += 8 * g.ldo;
                     } else {
                         h2 oh[2];
                         rounded(y, oh);
@@ -858,12 +894,18 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
                     // row sum of token 32 i + 4 p + lane / 16 of the wave: held by lane (that % 64), half
                     // i / 2 (fetched with every lane active: a switched-off source lane would read as 0)
                     if constexpr (DEQ != 0) rs = (unsigned)row_sum_of(i, p);
+                    const float sx = TOK ? step_of(i, p) : 0.0f;
                     if (t < g.T && n_ok) {
                         if constexpr (I32) __builtin_nontemporal_store(o, reinterpret_cast<v4i*>(g.out_i32 + t * g.ldo + n));
                         if constexpr (DEQ != 0) {
                             float y[4];
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
+                                if constexpr (TOK) {
+                                    const int iv = token_integer(o[c], (int)(int8_t)rs, cn[c], nzw[c], (int)rs >> 8);
+                                    y[c] = DEQ == 1 ? token_scaled_f32(iv, sx, sw.f[c], bs.f[c]) : token_scaled(iv, sx, sw.f[c], bs.f[c]);
+                                    continue;
+                                }
                                 // |row sum| <= 128 K < 2^23 and |Z'w| < 2^23 for any zero point binary16 weights can
                                 // produce: a 24-bit multiply (full rate); wider zero points take the 32-bit one
                                 const unsigned zr = (nzw[c] < (1 << 23) && nzw[c] > -(1 << 23)) ? (unsigned)__mul24(nzw[c], (int)rs) : (unsigned)nzw[c] * rs;
@@ -923,6 +965,10 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
                                     rsy = __builtin_amdgcn_sdot4((int)w, 0x01010101, 0, false);
                                     *reinterpret_cast<uint32_t*>(yq_lane + t * kPanel) = w;
                                 }
+                            } else if constexpr (DEQ == 3) {
+                                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                                const b4 ob = {(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+                                __builtin_nontemporal_store(ob, reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(out_deq) + t * g.ldo + n));
                             } else {
                                 typedef float f4 __attribute__((ext_vector_type(4)));
                                 f4 of = {y[0], y[1], y[2], y[3]};
@@ -1330,4 +1376,60 @@ extern "C" int aweq_w8a8_gemm_fused(const int8_t* xq, int64_t T, int64_t K, cons
     if (want_stats)
         fused_stats_finish<<<(unsigned)cdiv(N, 256), 256, 0, st>>>(g.ykeys, g.yfix, N, T, ycmin, ycmax, ycsum, ycount, accumulate, status);
     return launch_status();
+}
+
+extern "C" int aweq_w8a8_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, int64_t K, int64_t ldx, const float* inv_s,
+                                     int8_t* xq, float* step_x, int32_t* zero_x, int32_t* rowsum_x,
+                                     const int8_t* wq, int64_t N, const float* step_w, const int32_t* zero_w, int w_group,
+                                     const int32_t* rowsum_w, const float* bias, void* out, aweq_dtype out_dt, int64_t ldo,
+                                     uint32_t* status, void* stream)
+{
+    if (!X || !wq || !step_x || !zero_x || !rowsum_x || !step_w || !zero_w || !rowsum_w || !out) return AWEQ_ERR_NULL;
+    if (w_group != 0 && w_group != -1) return AWEQ_ERR_GROUP;
+    if (out_dt != AWEQ_F32 && out_dt != AWEQ_F16 && out_dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    if (T <= 0 || N <= 0 || K <= 0 || (K % 8) != 0 || K > 32768 || (N % 4) != 0 || ldo < N || (ldo % 4) != 0) return AWEQ_ERR_SHAPE;
+    const bool codes = x_dt == AWEQ_I8;
+    if (codes) {
+        if (ldx != K) return AWEQ_ERR_SHAPE;
+        if (!aligned16(X)) return AWEQ_ERR_ALIGN;
+    } else {
+        const int rc = check_quant_tokens(X, x_dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x);
+        if (rc != AWEQ_OK) return rc;
+    }
+    if (!aligned16(wq) || !aligned16(out) || !aligned16(rowsum_w) || (bias && !aligned16(bias)) || (w_group == 0 && (!aligned16(step_w) || !aligned16(zero_w))))
+        return AWEQ_ERR_ALIGN;
+    GemmArgs g;
+    g.A = codes ? reinterpret_cast<const int8_t*>(X) : xq;
+    g.B = wq; g.T = T; g.N = N; g.K = K;
+    g.out_i32 = nullptr; g.out_deq = out; g.out_f16 = out_dt == AWEQ_F16 ? kOutF16 : out_dt == AWEQ_BF16 ? kOutBf16 : kOutF32; g.ldo = ldo;
+    g.colsum_acc = nullptr;
+    g.act_step = step_x; g.act_zero = zero_x; g.step_w = step_w; g.zero_w = zero_w;
+    g.rowsum_x = rowsum_x; g.rowsum_w = rowsum_w; g.bias = bias;
+    clear_fused(g);
+    g.w_per_tensor = w_group == -1;
+    g.status = status;
+    bool half = false;
+    double tiled_cost = 0.0;
+    int64_t blocks = 0;
+    const int prc = plan_tiled(g, half, tiled_cost, blocks);
+    if (prc != AWEQ_OK) return prc;
+    hipStream_t st = as_stream(stream);
+    if (!codes) {
+        const int rc = launch_quant_tokens(X, x_dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, status, st);
+        if (rc != AWEQ_OK) return rc;
+    }
+    // the form as in aweq_w8a8_gemm
+    const FewPlan few = plan_few(T, N);
+    MidPlan mid = plan_mid(T, N);
+    if (K <= 512 && mid.cost > 43.0) mid.cost *= 1.2;
+    if (few.cost <= mid.cost && few.cost < kTiledRoundCost * tiled_cost) return launch_gemm_i8_few(g, few, st, true);
+    if (mid.cost < kTiledRoundCost * tiled_cost) return launch_gemm_i8_mid(g, mid, st, true);
+    const void* fn = nullptr;
+#define AWEQ_PICK(O, D)                                                                                                \
+    if (g.out_f16 == O)                                                                                                \
+        fn = half ? reinterpret_cast<const void*>(fast::gemm_i8_fast<2, false, D, false, 0, true, GemmArgs, true>)     \
+                  : reinterpret_cast<const void*>(fast::gemm_i8_fast<4, false, D, false, 0, true, GemmArgs, true>);
+    AWEQ_PICK(kOutF32, 1) AWEQ_PICK(kOutF16, 2) AWEQ_PICK(kOutBf16, 3)
+#undef AWEQ_PICK
+    return launch_persistent(fn, fast::kThreads, half ? fast::Tile<2>::kLds : fast::Tile<4>::kLds, &g, g.n_ids, st);
 }

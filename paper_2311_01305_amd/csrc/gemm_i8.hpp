@@ -5,16 +5,18 @@
 
 namespace aweq {
 
+enum { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2 };   // (bfloat16: products with a quantizer a token only)
+
 struct GemmArgs : TileWalk {
     const int8_t* A;   // xq [T x K], K-panel layout
     const int8_t* B;   // wq [N x K], K-panel layout
     int64_t T, N, K;
     int32_t* out_i32;
     void* out_deq;
-    int out_f16;
+    int out_f16;       // kOut*
     int64_t ldo;
     long long* colsum_acc;
-    const float* act_step;
+    const float* act_step;    // one, or one for each token
     const int32_t* act_zero;
     const float* step_w;
     const int32_t* zero_w;
@@ -60,7 +62,7 @@ struct FewPlan {
     double cost;
 };
 FewPlan plan_few(int64_t T, int64_t N);
-int launch_gemm_i8_few(const GemmArgs& g, const FewPlan& p, hipStream_t st);
+int launch_gemm_i8_few(const GemmArgs& g, const FewPlan& p, hipStream_t st, bool tokens = false);   // tokens: act_step and act_zero for each token
 
 // The same for at most kQuantTokens binary16 / binary32 tokens that the launch quantises itself (what the activation quantizer would
 // write goes to xq and rowsum_x; g.A and g.rowsum_x are not read)
@@ -81,7 +83,20 @@ struct MidPlan {
     double cost;
 };
 MidPlan plan_mid(int64_t T, int64_t N);
-int launch_gemm_i8_mid(const GemmArgs& g, const MidPlan& p, hipStream_t st);
+int launch_gemm_i8_mid(const GemmArgs& g, const MidPlan& p, hipStream_t st, bool tokens = false);
+
+// The output of a product whose tokens have scales of their own: acc - Z'x A - Z'w rowsum_x, A = rowsum_w - K Z'w, in wrap-around 32 bits (nzw
+// = -Z'w), and its scaling, the same in every form: binary16 and bfloat16 in fp32 (its roundings, 2^-23 together, are far inside the
+// output's), binary32 in fp64
+__device__ __forceinline__ int token_integer(int acc, int zx, unsigned a, int nzw, int rowsum_x)
+{
+    return (int)((unsigned)acc - (unsigned)zx * a + (unsigned)nzw * (unsigned)rowsum_x);
+}
+__device__ __forceinline__ float token_scaled(int i, float sx, float sw, float bias) { return __builtin_fmaf((float)i, sx * sw, bias); }
+__device__ __forceinline__ float token_scaled_f32(int i, float sx, float sw, float bias)
+{
+    return (float)((double)i * ((double)sx * (double)sw) + (double)bias);
+}
 
 // Time of one round of workgroups at K = 8192 (us; every kernel's time is close to proportional to K): 256 tiles of 256 x 256
 constexpr double kTiledRoundCost = 100.0;

@@ -30,7 +30,8 @@ constexpr int kWaves = kThreads / kWave;
 // requested ahead of the weights; behind them the quantizer waited for the weights first (us a call, weights in the caches, before -> now, with reads of the tokens that
 // leave them in the caches for the other workgroups: one token 4096 x 4096 6.4 -> 5.15, 8192 x 8192 16.0 -> 13.6, 4096 x 16384 18.0 -> 15.6,
 // 11008 x 4096 10.85 -> 9.3; four tokens 16384 x 4096 15.1 -> 12.95).
-template <int TT, int NT, int D, int QX, int TQ>
+// TOK: Step and Z of the activations are a token's.
+template <int TT, int NT, int D, int QX, int TQ, bool TOK>
 __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
 {
     extern __shared__ __attribute__((aligned(16))) int red[];   // [wave][TT NT][lane][4], then (QX) the tokens' codes, K padded to panels
@@ -98,13 +99,17 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
     static_assert(kChannels + kTokens <= kThreads, "a thread each");
     __shared__ double s_scale[kChannels], s_bias[kChannels];
     __shared__ unsigned s_cn[kChannels], s_zw[kChannels], s_rx[kTokens];
+    __shared__ float s_sw[TOK ? kChannels : 1], s_sx[TOK ? kTokens : 1];
+    __shared__ int s_zx[TOK ? kTokens : 1];
     float e_step = 0.0f, e_bias = 0.0f, e_sx = 0.0f;
     int e_zw = 0, e_rw = 0, e_zx = 0;
     const int e_tok = (int)threadIdx.x - kChannels;
     auto request_constants = [&]() {
         if (!g.out_deq) return;
-        e_zx = *g.act_zero;
-        e_sx = *g.act_step;
+        if constexpr (!TOK) {
+            e_zx = *g.act_zero;
+            e_sx = *g.act_step;
+        }
         if ((int)threadIdx.x <= rows_left) {
             const int64_t n = n0 + threadIdx.x, pi = g.w_per_tensor ? 0 : n;
             e_step = g.step_w[pi];
@@ -113,6 +118,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
             if (g.bias) e_bias = g.bias[n];
         } else if (QX == 0 && e_tok >= 0 && e_tok <= tokens_left) {
             e_rw = g.rowsum_x[t0 + e_tok];
+            if constexpr (TOK) { e_sx = g.act_step[t0 + e_tok]; e_zx = g.act_zero[t0 + e_tok]; }
         }
     };
     if constexpr (QX != 0) request_constants();   // (with the tokens, ahead of the weights)
@@ -208,15 +214,18 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
     if (g.out_deq) {
         // the tiled kernel's arithmetic: the integer part in wrap-around 32 bits, scaled and shifted in fp64
         const int zx = e_zx - 128, zw = e_zw - 128;
-        if (zx < -128 || zx > 127) est |= AWEQ_ST_ZEROPOINT;
+        if (!TOK && (zx < -128 || zx > 127)) est |= AWEQ_ST_ZEROPOINT;
         if ((int)threadIdx.x <= rows_left) {
             if (zw < -128 || zw > 127) est |= AWEQ_ST_ZEROPOINT;
-            s_scale[threadIdx.x] = (double)e_sx * (double)e_step;
+            if constexpr (TOK) s_sw[threadIdx.x] = e_step;
+            else s_scale[threadIdx.x] = (double)e_sx * (double)e_step;
             s_bias[threadIdx.x] = (double)e_bias;
-            s_cn[threadIdx.x] = (unsigned)g.K * (unsigned)zx * (unsigned)zw - (unsigned)zx * (unsigned)e_rw;
+            if constexpr (TOK) s_cn[threadIdx.x] = (unsigned)e_rw - (unsigned)g.K * (unsigned)zw;
+            else s_cn[threadIdx.x] = (unsigned)g.K * (unsigned)zx * (unsigned)zw - (unsigned)zx * (unsigned)e_rw;
             s_zw[threadIdx.x] = (unsigned)zw;
         } else if (QX == 0 && e_tok >= 0 && e_tok < kTokens) {
             s_rx[e_tok] = (unsigned)e_rw;
+            if constexpr (TOK) { s_sx[e_tok] = e_sx; s_zx[e_tok] = zx; }
         }
     }
     __syncthreads();
@@ -234,10 +243,19 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
             float y[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
+                if constexpr (TOK) {
+                    const int iv = token_integer(o[c], s_zx[tl], s_cn[nl + c], -(int)s_zw[nl + c], (int)rs);
+                    y[c] = g.out_f16 == kOutF32 ? token_scaled_f32(iv, s_sx[tl], s_sw[nl + c], (float)s_bias[nl + c])
+                                                : token_scaled(iv, s_sx[tl], s_sw[nl + c], (float)s_bias[nl + c]);
+                    continue;
+                }
                 const double div = (double)(int)((unsigned)o[c] + s_cn[nl + c] - s_zw[nl + c] * rs);
                 y[c] = g.out_f16 ? (float)__builtin_fma(div, s_scale[nl + c], s_bias[nl + c]) : (float)(div * s_scale[nl + c] + s_bias[nl + c]);
             }
-            if (g.out_f16) {
+            if (TOK && g.out_f16 == kOutBf16) {
+                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(g.out_deq) + t * g.ldo + n) = b4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+            } else if (g.out_f16) {
                 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
                 *reinterpret_cast<h4*>(reinterpret_cast<_Float16*>(g.out_deq) + t * g.ldo + n) =
                     h4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
@@ -269,13 +287,13 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
 
 // Token tiles ride on the grid's y dimension, at most 65535 to a launch: layers of up to 64 channels come here at any number of tokens
 constexpr int kMaxGridY = 65535;
-template <int TT, int NT, int D, int QX = 0, int TQ = 1>
+template <int TT, int NT, int D, int QX = 0, int TQ = 1, bool TOK = false>
 static int launch_tile(GemmArgs g, hipStream_t st, QuantIn in = {})
 {
     constexpr int kSums = kWaves * TT * NT * kWave * 16;   // partial sums; a launch that quantises has the tokens' codes behind them
     static_assert(QX == 0 || kSums + kQuantFewBytes <= 32768, "a launch that quantises stays below the LDS limit that has to be raised");
     const int lds = kSums + (QX != 0 ? (int)(g.T * panel_count(g.K) * kPanel) : 0);
-    const void* fn = reinterpret_cast<const void*>(gemm_i8_few<TT, NT, D, QX, TQ>);
+    const void* fn = reinterpret_cast<const void*>(gemm_i8_few<TT, NT, D, QX, TQ, TOK>);
     int dev = 0, cus = 0;
     if (lds > 32768 && (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, lds) != AWEQ_OK)) return AWEQ_ERR_LAUNCH;
     void* args[] = {&g, &in};
@@ -319,16 +337,22 @@ int launch_gemm_i8_few_quant(const GemmArgs& g, const FewPlan& p, const QuantIn&
 #undef AWEQ_FQ
 }
 
-int launch_gemm_i8_few(const GemmArgs& g, const FewPlan& p, hipStream_t st)
+template <bool TOK>
+static int launch_few(const GemmArgs& g, const FewPlan& p, hipStream_t st)
 {
     switch (p.tile) {
-    case 0: return few::launch_tile<1, 1, 2>(g, st);
-    case 1: return few::launch_tile<1, 2, 3>(g, st);
-    case 2: return few::launch_tile<2, 1, 3>(g, st);
-    case 3: return few::launch_tile<2, 2, 2>(g, st);
-    case 4: return few::launch_tile<2, 4, 1>(g, st);
-    default: return few::launch_tile<4, 4, 1>(g, st);
+    case 0: return few::launch_tile<1, 1, 2, 0, 1, TOK>(g, st);
+    case 1: return few::launch_tile<1, 2, 3, 0, 1, TOK>(g, st);
+    case 2: return few::launch_tile<2, 1, 3, 0, 1, TOK>(g, st);
+    case 3: return few::launch_tile<2, 2, 2, 0, 1, TOK>(g, st);
+    case 4: return few::launch_tile<2, 4, 1, 0, 1, TOK>(g, st);
+    default: return few::launch_tile<4, 4, 1, 0, 1, TOK>(g, st);
     }
+}
+
+int launch_gemm_i8_few(const GemmArgs& g, const FewPlan& p, hipStream_t st, bool tokens)
+{
+    return tokens ? launch_few<true>(g, p, st) : launch_few<false>(g, p, st);
 }
 
 }  // namespace aweq

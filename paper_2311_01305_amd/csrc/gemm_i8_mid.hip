@@ -50,7 +50,8 @@ __device__ __forceinline__ void wait_vm()
 }
 
 // QUANT: the epilogue also quantises the binary16 output for the next layer (aweq_w8a8_gemm_fused without statistics)
-template <int WM, int WN, int WK, bool QUANT>
+// TOK: Step and Z of the activations are a token's
+template <int WM, int WN, int WK, bool QUANT, bool TOK>
 __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
 {
     using TL = Tile<WM, WN, WK>;
@@ -74,12 +75,15 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
     const int ec = tid % kRowThreads, er = tid / kRowThreads;
     const int64_t n = n0 + ec * 4;
     const bool n_ok = n < g.N;     // N % 4 == 0: all four channels or none
-    int zx = 0, zw[4] = {0, 0, 0, 0}, rw[4] = {0, 0, 0, 0}, rsx[kRows];
+    int zx = 0, zw[4] = {0, 0, 0, 0}, rw[4] = {0, 0, 0, 0}, rsx[kRows], zxx[TOK ? kRows : 1];
+    float sxx[TOK ? kRows : 1];
     float sxf = 0.f, sw[4] = {0.f, 0.f, 0.f, 0.f}, bs[4] = {0.f, 0.f, 0.f, 0.f};
     const bool deq = QUANT || g.out_deq;
     if (deq) {
-        zx = *g.act_zero - 128;
-        sxf = *g.act_step;
+        if constexpr (!TOK) {
+            zx = *g.act_zero - 128;
+            sxf = *g.act_step;
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             if (n_ok) {
@@ -90,7 +94,11 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
                 if (g.bias) bs[c] = g.bias[n + c];
             }
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) rsx[i] = g.rowsum_x[min(m0 + er + i * kRowStep, g.T - 1)];
+        for (int i = 0; i < kRows; ++i) {
+            const int64_t t = min(m0 + er + i * kRowStep, g.T - 1);
+            rsx[i] = g.rowsum_x[t];
+            if constexpr (TOK) { zxx[i] = g.act_zero[t] - 128; sxx[i] = g.act_step[t]; }
+        }
     }
 
     // load q of this wavefront brings 16 rows of one panel of the stage: unit wave kLoads + q of (panel, 16-row group)
@@ -191,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             if (zw[c] < -128 || zw[c] > 127) est |= AWEQ_ST_ZEROPOINT;
-            cn[c] = (unsigned)g.K * (unsigned)zx * (unsigned)zw[c] - (unsigned)zx * (unsigned)rw[c];
+            cn[c] = TOK ? (unsigned)rw[c] - (unsigned)g.K * (unsigned)zw[c] : (unsigned)g.K * (unsigned)zx * (unsigned)zw[c] - (unsigned)zx * (unsigned)rw[c];
             scale[c] = (double)sxf * (double)sw[c];
         }
     }
@@ -230,12 +238,20 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
             float y[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
+                if constexpr (TOK) {
+                    const int iv = token_integer(o[c], zxx[i], cn[c], -zw[c], rsx[i]);
+                    y[c] = g.out_f16 == kOutF32 ? token_scaled_f32(iv, sxx[i], sw[c], bs[c]) : token_scaled(iv, sxx[i], sw[c], bs[c]);
+                    continue;
+                }
                 const double div = (double)(int)((unsigned)o[c] + cn[c] - (unsigned)zw[c] * (unsigned)rsx[i]);
                 y[c] = QUANT || g.out_f16 ? (float)__builtin_fma(div, scale[c], (double)bs[c]) : (float)(div * scale[c] + (double)bs[c]);
                 if (QUANT && g.act == 1) y[c] = fmaxf(y[c], 0.0f);
             }
             const h4 oh = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
-            if (QUANT || g.out_f16) {
+            if (TOK && g.out_f16 == kOutBf16) {
+                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(g.out_deq) + t * g.ldo + n) = b4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+            } else if (QUANT || g.out_f16) {
                 if (g.out_deq) *reinterpret_cast<h4*>(reinterpret_cast<_Float16*>(g.out_deq) + t * g.ldo + n) = oh;
             } else {
                 *reinterpret_cast<Float4*>(reinterpret_cast<float*>(g.out_deq) + t * g.ldo + n) = Float4{{y[0], y[1], y[2], y[3]}};
@@ -301,14 +317,14 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
     raise_status(g.status, est);
 }
 
-template <int WM, int WN, int WK, bool QUANT>
+template <int WM, int WN, int WK, bool QUANT, bool TOK = false>
 static int launch_tile(GemmArgs g, hipStream_t st)
 {
     using TL = Tile<WM, WN, WK>;
     g.tiles_m = (int)cdiv(g.T, TL::kM);
     g.tiles_n = (int)cdiv(g.N, TL::kN);
     g.run = (int)cdiv((int64_t)g.tiles_m * g.tiles_n, kXcdCount);
-    const void* fn = reinterpret_cast<const void*>(gemm_i8_mid<WM, WN, WK, QUANT>);
+    const void* fn = reinterpret_cast<const void*>(gemm_i8_mid<WM, WN, WK, QUANT, TOK>);
     int dev = 0, cus = 0;
     if (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, TL::kLds) != AWEQ_OK) return AWEQ_ERR_LAUNCH;
     void* args[] = {&g};
@@ -329,8 +345,9 @@ MidPlan plan_mid(int64_t T, int64_t N)
     return c12 <= c22 ? MidPlan{false, c12} : MidPlan{true, c22};
 }
 
-int launch_gemm_i8_mid(const GemmArgs& g, const MidPlan& p, hipStream_t st)
+int launch_gemm_i8_mid(const GemmArgs& g, const MidPlan& p, hipStream_t st, bool tokens)
 {
+    if (tokens) return p.square ? mid::launch_tile<2, 2, 2, false, true>(g, st) : mid::launch_tile<1, 2, 4, false, true>(g, st);
     if (g.yq) return p.square ? mid::launch_tile<2, 2, 2, true>(g, st) : mid::launch_tile<1, 2, 4, true>(g, st);
     return p.square ? mid::launch_tile<2, 2, 2, false>(g, st) : mid::launch_tile<1, 2, 4, false>(g, st);
 }

@@ -1,4 +1,4 @@
-// Calls of the C ABI from Python: converts the arguments (a tensor by its data_ptr(), an address, None, an integer), releases the
+// Calls of the C ABI from Python: converts the arguments (a tensor by its data_ptr(), an address, None, a number), releases the
 // interpreter lock and calls the entry point.  One decoded token's GEMM takes 5 us on the device and 27 arguments; converted by ctypes
 // and in Python they took longer than that.  The entry points' addresses come from binding.py, which loads the library.
 #define PY_SSIZE_T_CLEAN
@@ -30,6 +30,10 @@ bool convert(PyObject* o, T& v)
         }
         if (a == (unsigned long long)-1 && PyErr_Occurred()) return false;
         v = reinterpret_cast<T>((uintptr_t)a);
+    } else if constexpr (std::is_floating_point<T>::value) {
+        const double a = PyFloat_AsDouble(o);
+        if (a == -1.0 && PyErr_Occurred()) return false;
+        v = (T)a;
     } else {
         const unsigned long long a = PyLong_AsUnsignedLongLongMask(o);   // (the low bits, whatever the integer's sign and size: as ctypes converts)
         if (a == (unsigned long long)-1 && PyErr_Occurred()) return false;
@@ -62,7 +66,8 @@ struct Entry<int (*)(A...)> {
 
 #define ENTRIES(X)                                                                                                     \
     X(aweq_calib_stats) X(aweq_calib_stats_static) X(aweq_equalize) X(aweq_quant_weight) X(aweq_fold_quant_weight)     \
-    X(aweq_quant_act) X(aweq_w8a8_gemm) X(aweq_w8a8_gemm_fused) X(aweq_bias_correct) X(aweq_wonly_gemm)
+    X(aweq_quant_act) X(aweq_w8a8_gemm) X(aweq_w8a8_gemm_fused) X(aweq_bias_correct) X(aweq_wonly_gemm)                \
+    X(aweq_quant_tokens) X(aweq_w8a8_gemm_tokens) X(aweq_qk_rope) X(aweq_kv_append) X(aweq_prefix_attention)
 
 #define X(name)                                                                                                        \
     decltype(&::name) p_##name;                                                                                        \
