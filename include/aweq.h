@@ -417,7 +417,8 @@ int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, i
  * The prefix is read once for all the batch's queries, which multiply its keys together; long key ranges are split between
  * workgroups whose partial results (fp32, in ws) a second launch joins.  Scores and softmax in fp32, with products of the stored
  * type exact in fp32; the probabilities are rounded to F16 / BF16 for the product with v (BF16 queries over an 8-bit cache: both
- * products in F16, the queries scaled by a power of two).  D 64, 128 or 256; Hq a multiple of Hk; cache as above.
+ * products in F16, the queries scaled by a power of two).  D 64, 128 or 256; Hq a multiple of Hk; scale > 0;
+ * cache as above.
  * ws: aweq_prefix_attention_ws(...) bytes, 16-byte aligned (host function). */
 size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len);
 int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int64_t D, int64_t ldq,

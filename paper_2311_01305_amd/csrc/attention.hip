@@ -6,19 +6,22 @@
 // of each of those tokens, row r = token r / G, head r % G: the prefix is read once for all rows of the batch.
 //
 // A wavefront has 16 MT rows and takes the keys in tiles.  It forms S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32: the weights' side of
-// both products comes from the cache, a lane has one row of Q in its column, so that maximum and sum of a row need two exchanges across the
+// both products comes from the cache, a lane has one row of Q in its column, so that a row's maximum and sum need two exchanges across the
 // wavefront, and the four consecutive keys that a lane holds of a 16 x 16 tile of S^T are, two tiles at a time, the eight it has to supply of P^T: the order
 // of the keys inside a product is free as long as V^T's is the same.  V^T's is made by the transposing LDS reads.
+// The maximum is taken up lazily: any m gives the same quotient, so sum and O are only rescaled when a score is more than 2^8 above it.
 //
-// Tiles of K and V are filled by LDS-DMA loads, 16 bytes a lane, two tiles in turn.  16 neighbouring tokens lie in one page (its size is a
-// multiple of 16), so a group of 16 rows has one base address.  Chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.
-// A tile's rows past the range repeat its last token: what a page holds past the range is never read.
-//
-// WR = wavefronts that share a tile and have rows of their own (many rows: the prefix, prompts); WR = 1: every wavefront has tiles of its own and all
-// have the same 16 rows (decoding: one token's heads), whose results meet in LDS at the end.
+// Two forms:
+//  - tall (many rows: the prefix, prompts): four wavefronts with rows of their own share tiles of 64 keys, filled by LDS-DMA loads of 16 bytes a
+//    lane, two tiles in turn; chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.
+//  - wide (up to 16 rows: one token's heads): four wavefronts have the same rows and tiles of 32 keys of their own, whose results meet in
+//    LDS at the end.  K goes from memory to registers in the operand's order, V to registers and through the wavefront's own LDS; the next
+//    tile is requested as soon as this one's registers are free.
+// 16 neighbouring tokens lie in one page (its size is a multiple of 16), so a group of 16 rows has one base address.  A tile's rows past the range
+// repeat its last token: what a page holds past the range is never read.
 //
 // An 8-bit cache is multiplied as binary16 codes.  The step of a key goes to its score.  The step of a value goes into the exponent:
-// p' = exp(s + log step - m') is at most 1 and is what multiplies the codes; the sum takes p' / step back.
+// p' = exp(s + log step - m') stays in range and is what multiplies the codes; the sum takes p' / step back.
 #include "wide_unit.hpp"
 
 #include <cmath>
@@ -31,8 +34,23 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLazy = 8.0f;       // log2 of what a probability may be over 1
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
+constexpr int kWideRows = 16, kWideKeys = 32, kTallKeys = 64;
+
+// Workgroups of one kind in a launch: which rows, which keys
+struct Work {
+    int blocks;         // of the grid
+    int tall;           // form
+    int row_tiles;      // workgroups that cover a sequence's (the batch's) rows
+    int splits;         // ranges of the keys
+    int chunk;          // keys of a range; 0: an equal share of the tiles (tall, prefix and own keys in one list)
+    int combos;         // (sequence, range, key head)
+    int first_part;
+};
 
 struct Args {
     const void *q, *k_cache, *v_cache;
@@ -44,17 +62,20 @@ struct Args {
     float2* part_ml;    // [part][T Hq]: maximum (log2), sum
     uint32_t* status;
     int64_t T, ldq, ldo, table_ld;
-    int64_t prefix_len, max_len;
-    int64_t page_elts;  // values of one page: Hk page_size D
+    int prefix_len, max_len;
     int pages, page_size, page_shift;
-    int Hq, Hk, G, B, max_q;
-    int q_bf16;         // type of q and out (an 8-bit cache: any)
+    int Hq, Hk, G, max_q;
+    int q_bf16;         // type of q and out (an 8-bit cache: either)
     int parts;          // of a row: 1: the result itself
-    int first_part;     // this launch's first part
-    int splits;         // this launch's ranges
-    int row_tiles;
+    int fused;          // a sequence's rows take the prefix along
     float scale_log2e;
+    Work shared, own;   // the prefix for all rows; a sequence's keys for its own
 };
+
+// Tables and lengths do not change during a launch and are read at uniform places: through the scalar cache, whose loads do not wait for
+// the vector ones in flight
+typedef const __attribute__((address_space(4))) int32_t* ConstInts;
+__device__ __forceinline__ int scalar_at(const int32_t* p, int64_t i) { return ((ConstInts)(uintptr_t)p)[i]; }
 
 template <int N>
 __device__ __forceinline__ void wait_vm()
@@ -71,7 +92,18 @@ __device__ __forceinline__ void dma4(const float* at, uint32_t lds_addr)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr), "v"(at) : "memory");
 }
 
-// E: type of the cache (int8_t: codes).  M: type of the products
+// over the four lanes that hold a row's keys: lanes l, l ^ 16, l ^ 32, l ^ 48
+template <class Op>
+__device__ __forceinline__ float row_reduce(float v, Op op)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+struct Larger { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+
+// E: type of the cache (int8_t: codes)
 template <class E> struct Mfma;
 template <> struct Mfma<_Float16> {
     typedef f16x8 V;
@@ -86,43 +118,42 @@ template <> struct Mfma<__bf16> {
 };
 
 // 8 codes to binary16: the byte u = code + 128 under the exponent of 1024 is 1024 + u
-__device__ __forceinline__ f16x8 codes_to_f16(i32x2 w)
+__device__ __forceinline__ f16x8 codes_to_f16(int w0, int w1)
 {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
     union { uint32_t u[4]; h2 h[4]; f16x8 v; } r;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t u = (uint32_t)w[i] ^ 0x80808080u;
-        r.u[2 * i] = __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u);
-        r.u[2 * i + 1] = __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u);
-    }
+    const uint32_t u0 = (uint32_t)w0 ^ 0x80808080u, u1 = (uint32_t)w1 ^ 0x80808080u;
+    r.u[0] = __builtin_amdgcn_perm(0x64646464u, u0, 0x04010400u);
+    r.u[1] = __builtin_amdgcn_perm(0x64646464u, u0, 0x04030402u);
+    r.u[2] = __builtin_amdgcn_perm(0x64646464u, u1, 0x04010400u);
+    r.u[3] = __builtin_amdgcn_perm(0x64646464u, u1, 0x04030402u);
 #pragma unroll
     for (int i = 0; i < 4; ++i) r.h[i] = r.h[i] - h2{(_Float16)1152.0f, (_Float16)1152.0f};
     return r.v;
 }
 
-template <class E, int D, int WR>
-struct Tile {
-    static constexpr int kWaves = WR > 1 ? WR : (D == 256 && sizeof(E) == 2 ? 2 : 4);
-    static constexpr int kThreads = kWaves * kWave;
-    static constexpr int kKeys = WR > 1 ? 64 : 32;
+template <class E, int D>
+struct Shape {
+    static constexpr bool kCodes = sizeof(E) == 1;
     static constexpr int kRow = D * (int)sizeof(E);            // bytes of a token's head
     static constexpr int kChunks = kRow / 16;
-    static constexpr int kHalf = kKeys * kRow;                 // K, then V
-    static constexpr bool kSteps = sizeof(E) == 1;
-    static constexpr int kStepBytes = kSteps ? kKeys / 16 * 256 : 0;   // of a group of 16 keys: 16 steps of K, 16 of V (and 32 unused)
-    static constexpr int kSlot = 2 * kHalf + kStepBytes;
-    static constexpr int kStages = 2;
-    static constexpr int kRing = kStages * kSlot;              // of the wavefronts that share tiles
-    static constexpr int kGroups = kKeys / 16;
-    static constexpr int kMine = WR > 1 ? kGroups / WR : kGroups;      // groups of 16 keys that a wavefront fetches
     static constexpr int kLoads = kRow * 16 / 1024;            // load instructions for 16 rows
-    static constexpr int kMerge = WR > 1 ? 0 : kWaves * (16 * D * 4 + 128);
-    static constexpr int kLds = WR > 1 ? kRing : (kWaves * kRing > kMerge ? kWaves * kRing : kMerge);
+    static constexpr int kRowsPerLoad = 1024 / kRow;
+    // tall: K, V, and (codes) for each group of 16 keys 16 steps of K, 16 of V (and 32 unused)
+    static constexpr int kHalf = kTallKeys * kRow;
+    static constexpr int kSlot = 2 * kHalf + (kCodes ? kTallKeys / 16 * 256 : 0);
+    static constexpr int kStages = 2;
+    static constexpr int kTallLds = kStages * kSlot;
+    // wide: V of a tile and (codes) its steps for each wavefront; at the end their O, maximum and sum
+    static constexpr int kWideV = kWideKeys * kRow;
+    static constexpr int kWideSlot = kWideV + (kCodes ? 2 * kWideKeys * 4 : 0);
+    static constexpr int kMerge = kWaves * (kWideRows * D * 4 + kWideRows * 8);
+    static constexpr int kWideLds = kWaves * kWideSlot > kMerge ? kWaves * kWideSlot : kMerge;
+    static constexpr int lds(bool tall) { return tall && kTallLds > kWideLds ? kTallLds : kWideLds; }
 };
 
-// Swizzles of the 16-byte chunks of a row: reads of one chunk of 16 rows (K), and the transposing reads of V (binary16: 8 rows x 2 chunks,
-// codes: rows 0 - 7 and 16 - 23 of one chunk) fall on different banks
+// Swizzles of the 16-byte chunks of a row (C of them): reads of one chunk of 16 rows (K), and the transposing reads of V (binary16: 8 rows x 2
+// chunks, codes: rows 0 - 7 and 16 - 23 of one chunk) fall on different banks
 template <int C>
 __device__ __forceinline__ int swz_k(int row)
 {
@@ -131,426 +162,654 @@ __device__ __forceinline__ int swz_k(int row)
 template <int C, bool CODES>
 __device__ __forceinline__ int swz_v(int row)
 {
+    constexpr int span = C >= 16 ? 1 : 16 / C;
     if constexpr (CODES) {
-        constexpr int span = C >= 16 ? 1 : 16 / C, low = 8 / span;
+        constexpr int low = 8 / span;
         return ((row / span) & (low - 1)) + low * ((row >> 4) & 1);
     } else {
-        constexpr int span = C >= 16 ? 1 : 16 / C;
         return 2 * ((row / span) & (8 / span - 1));
     }
 }
 
-// PREFIX: the range is the prefix and rows are those of all tokens; else the sequence's own keys.
-template <class E, int D, int WR, int MT, bool PREFIX>
-__global__ __launch_bounds__((Tile<E, D, WR>::kThreads)) void attention_kernel(Args g)
-{
-    using TL = Tile<E, D, WR>;
+// What a workgroup has to do
+struct Job {
+    int64_t t0;         // first token of its rows
+    int rows;           // rows in all: tokens times G
+    int row0;           // the workgroup's first row
+    int kvh;
+    int pa, pb;         // keys of the prefix
+    int oa, ob;         // keys of the sequence, up to what the workgroup's last row sees
+    int sees0;          // row r sees sees0 + r / G of the sequence's keys
+    const int32_t* table;
+    int64_t part;
+};
+
+template <class E, int D, int MT>
+struct Rows {
     using M = Mfma<E>;
     using V = typename M::V;
-    constexpr int C = TL::kChunks;
-    constexpr bool kCodes = TL::kSteps;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-    const int col = lane & 15, grp = lane >> 4;
+    static constexpr bool kCodes = Shape<E, D>::kCodes;
 
-    // ---- which rows and keys
-    unsigned id = blockIdx.x;
-    const int split = id % (unsigned)g.splits; id /= (unsigned)g.splits;
-    const int row_tile = id % (unsigned)g.row_tiles; id /= (unsigned)g.row_tiles;
-    const int kvh = id % (unsigned)g.Hk;
-    const int b = id / (unsigned)g.Hk;
-    uint32_t est = 0;
-    int64_t t0 = 0;
-    int tokens, len;
-    const int32_t* table;
-    if constexpr (PREFIX) {
-        tokens = (int)g.T;
-        len = (int)g.prefix_len;
-        table = g.prefix_table;
-    } else {
-        int64_t t1;
-        if (g.q_start) {
-            t0 = g.q_start[b];
-            t1 = g.q_start[b + 1];
-            if (t0 < 0 || t1 < t0 || t1 > g.T || t1 - t0 > g.max_q) est |= AWEQ_ST_INDEX;
-            t0 = min(max(t0, (int64_t)0), g.T);
-            t1 = min(max(t1, t0), min(g.T, t0 + g.max_q));
-        } else {
-            t0 = b;
-            t1 = b + 1;
-        }
-        tokens = (int)(t1 - t0);
-        len = g.lens[b];
-        const int most = (int)min(g.max_len, g.table_ld * g.page_size);
-        if (len < 0 || len > most) est |= AWEQ_ST_INDEX;
-        len = min(max(len, 0), most);
-        table = g.table + (int64_t)b * g.table_ld;
-    }
-    const int rows = tokens * g.G;
-    const int row0 = row_tile * (16 * MT * WR) + (WR > 1 ? wave * 16 * MT : 0);   // this wavefront's first row
-    if (row_tile * (16 * MT * WR) >= rows) {
-        if (threadIdx.x == 0) raise_status(g.status, est);
-        return;
-    }
-    // the keys of this range: an equal number of tiles of the splits, up to what the tile's last row sees
-    const int last_token = min(((row_tile + 1) * (16 * MT * WR) - 1) / g.G, tokens - 1);
-    const int seen = PREFIX ? len : min(len, len - tokens + 1 + last_token);    // (not positive: the row sees none)
-    const int per = ((len + g.splits - 1) / g.splits + TL::kKeys - 1) / TL::kKeys * TL::kKeys;
-    const int begin = split * per, end = min(min(begin + per, len), seen);
-
-    // ---- Q: column `col` of the wavefront's row tile i, eight values of its head at a time
-    V qf[MT][D / 32];
-    float row_scale[MT];
-    int limit[MT];      // keys that the row sees
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int r = min(row0 + 16 * i + col, rows - 1);
-        const int64_t t = t0 + r / g.G;
-        limit[i] = PREFIX ? len : min(len, len - tokens + 1 + r / g.G);
-        const char* src = reinterpret_cast<const char*>(g.q) + (t * g.ldq + (int64_t)(kvh * g.G + r % g.G) * D) * 2;
-        row_scale[i] = g.scale_log2e;
-        if (kCodes && g.q_bf16) {
-            // bfloat16 queries as binary16: scaled by a power of two, the largest value below 2^15
-            float x[D / 32][8], big = 0.0f;
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk) {
-                widen<__bf16>(*reinterpret_cast<const bf16x8*>(src + (kk * 32 + grp * 8) * 2), x[kk]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(x[kk][j]));
-            }
-            big = fmaxf(big, partner<5>(big));
-            big = fmaxf(big, partner<4>(big));
-            const int e = big > 0.0f ? 14 - ilogbf(big) : 0;
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) qf[i][kk][j] = (typename M::S)ldexpf(x[kk][j], e);
-            row_scale[i] = ldexpf(g.scale_log2e, -e);
-        } else {
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk) qf[i][kk] = *reinterpret_cast<const V*>(src + (kk * 32 + grp * 8) * 2);
-        }
-    }
-
+    V q[MT][D / 32];
+    float scale[MT];        // to log2
+    int sees[MT];           // own keys that the row sees
     f32x4 o[MT][D / 16];
-    float m[MT], l[MT];
+    float m[MT], l[MT];     // (l: of this lane's keys)
+
+    // Column lane % 16 of row tile i is row `row0` + 16 i + that; eight values of its head at a time, in the order that K is read in: 32 kk + 8 grp, or for
+    // codes, whose 16-byte chunks are two operands, 64 (kk / 2) + 16 grp + 8 (kk % 2)
+    __device__ __forceinline__ void load(const Args& g, const Job& j, int row0)
+    {
+        const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        m[i] = -INFINITY;
-        l[i] = 0.0f;
+        for (int i = 0; i < MT; ++i) {
+            const int r = min(row0 + 16 * i + col, j.rows - 1);
+            sees[i] = j.sees0 + r / g.G;
+            const char* src = reinterpret_cast<const char*>(g.q) + ((j.t0 + r / g.G) * g.ldq + (int64_t)(j.kvh * g.G + r % g.G) * D) * 2;
+            auto at = [&](int kk) { return src + (kCodes ? 64 * (kk / 2) + 16 * grp + 8 * (kk % 2) : 32 * kk + 8 * grp) * 2; };
+            scale[i] = g.scale_log2e;
+            if (kCodes && g.q_bf16) {
+                // bfloat16 queries as binary16: scaled by a power of two, the largest value below 2^15
+                float x[D / 32][8], big = 0.0f;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) o[i][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int kk = 0; kk < D / 32; ++kk) {
+                    widen<__bf16>(*reinterpret_cast<const bf16x8*>(at(kk)), x[kk]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[kk][e]));
+                }
+                big = row_reduce(big, Larger());
+                const int e2 = big > 0.0f ? 14 - ilogbf(big) : 0;
+#pragma unroll
+                for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) q[i][kk][e] = (typename M::S)ldexpf(x[kk][e], e2);
+                scale[i] = ldexpf(g.scale_log2e, -e2);
+            } else {
+#pragma unroll
+                for (int kk = 0; kk < D / 32; ++kk) q[i][kk] = *reinterpret_cast<const V*>(at(kk));
+            }
+            m[i] = -INFINITY;
+            l[i] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) o[i][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
     }
 
-    // ---- the ring
-    const int tile_step = WR > 1 ? TL::kKeys : TL::kKeys * TL::kWaves;           // between this wavefront's tiles
-    const int first = begin + (WR > 1 ? 0 : wave * TL::kKeys);
-    const int tiles = end > first ? (end - first + tile_step - 1) / tile_step : 0;
-    char* const ring = lds + (WR > 1 ? 0 : wave * TL::kRing);
-    const uint32_t ring_addr = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring);
-    constexpr int kRowsPerLoad = 1024 / TL::kRow;    // rows of one load instruction
-    auto fetch = [&](int tile) {
-        const uint32_t slot = ring_addr + (uint32_t)(tile % TL::kStages) * TL::kSlot;
+    // Scores s[i][n] of 16 keys each to probabilities for the second product; key0: the tile's first key, end: the range's, own: of the sequence.
+    // ks, vs: (codes) the steps of this lane's keys.
+    template <int N>
+    __device__ __forceinline__ void softmax(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], int key0, int end, bool own, const float (&ks)[N][4], const float (&vs)[N][4])
+    {
+        const int grp = (threadIdx.x & (kWave - 1)) >> 4;
+        float lv[N][4], rv[N][4];
+        if constexpr (kCodes) {
 #pragma unroll
-        for (int q = 0; q < TL::kMine; ++q) {
-            const int group = (WR > 1 ? wave * TL::kMine : 0) + q;
-            const int key0 = first + tile * tile_step + group * 16;              // a multiple of 16: the group lies in one page
-            const int base_key = min(key0, end - 1);
-            int page = __builtin_amdgcn_readfirstlane(table[base_key >> g.page_shift]);
-            if ((unsigned)page >= (unsigned)g.pages) { est |= AWEQ_ST_INDEX; page = 0; }
-            const int64_t head_row = ((int64_t)page * g.Hk + kvh) << g.page_shift;   // row of the cache where this head's page begins
-            const char* const kb = reinterpret_cast<const char*>(g.k_cache) + head_row * TL::kRow;
-            const char* const vb = reinterpret_cast<const char*>(g.v_cache) + head_row * TL::kRow;
-            const int in_page = g.page_size - 1;
+            for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int j = 0; j < TL::kLoads; ++j) {
-                const int sub = j * kRowsPerLoad + lane / C;                         // row of the 16
-                const int row = min(key0 + sub, end - 1) & in_page;
-                const int trow = group * 16 + sub;                                   // of the tile: the swizzle's
-                const uint32_t at = slot + (uint32_t)(group * 16 * TL::kRow + j * 1024);
-                dma16(kb, (uint32_t)(row * TL::kRow + ((lane % C) ^ swz_k<C>(trow)) * 16), at);
-                dma16(vb, (uint32_t)(row * TL::kRow + ((lane % C) ^ swz_v<C, kCodes>(trow)) * 16), at + TL::kHalf);
-            }
+                for (int v = 0; v < 4; ++v) { lv[n][v] = __builtin_amdgcn_logf(vs[n][v]); rv[n][v] = __builtin_amdgcn_rcpf(vs[n][v]); }
+        }
+        float top[MT];
+        bool high = false;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int lim = own ? min(end, sees[i]) : end;
             if constexpr (kCodes) {
-                const int row = min(key0 + col, end - 1) & in_page;
-                dma4((grp & 1 ? g.v_step : g.k_step) + head_row + row, slot + 2 * TL::kHalf + (uint32_t)group * 256);
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) s[i][n][v] = __builtin_fmaf(s[i][n][v], ks[n][v] * scale[i], lv[n][v]);
             }
+            if (__builtin_amdgcn_ballot_w64(key0 + 16 * N > lim) != 0) {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) s[i][n][v] = key0 + n * 16 + grp * 4 + v < lim ? s[i][n][v] : -INFINITY;
+            }
+            float t = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) t = fmaxf(t, s[i][n][v]);
+            top[i] = kCodes ? t : t * scale[i];    // (scale > 0)
+            high = high || top[i] > m[i] + kLazy;
+        }
+        if (__builtin_amdgcn_ballot_w64(high) != 0) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const float m_new = fmaxf(m[i], row_reduce(top[i], Larger()));
+                const float a = __builtin_amdgcn_exp2f(m[i] - (m_new == -INFINITY ? 0.0f : m_new));
+                m[i] = m_new;
+                l[i] *= a;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) o[i][d] *= a;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const float use = m[i] == -INFINITY ? 0.0f : m[i];
+            float sum = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float x = __builtin_amdgcn_exp2f(kCodes ? s[i][n][v] - use : __builtin_fmaf(s[i][n][v], scale[i], -use));
+                    if constexpr (kCodes) sum = __builtin_fmaf(x, rv[n][v], sum);
+                    else sum += x;
+                    p[i][n / 2][(n & 1) * 4 + v] = (typename M::S)x;
+                }
+            l[i] += sum;
+        }
+    }
+
+    // O^T += V^T P^T for keys 32 u .. 32 u + 31 of the tile at vt
+    __device__ __forceinline__ void values(const char* vt, int u, const V (&p)[MT])
+    {
+        constexpr int C = Shape<E, D>::kChunks, kRow = Shape<E, D>::kRow;
+        const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+            V vf;
+            if constexpr (kCodes) {
+                const int r = col >> 1, row = u * 32 + 16 * (r >> 2) + 4 * grp + (r & 3);
+                const char* const at = vt + row * kRow + ((d ^ swz_v<C, true>(row)) * 16) + (col & 1) * 8;
+                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)at);
+                vf = codes_to_f16(w[0], w[1]);
+            } else {
+                union { s16x4 h[2]; V v; } f;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int row = u * 32 + half * 16 + 4 * grp + (col >> 2);
+                    const char* const at = vt + row * kRow + (((2 * d + ((col & 3) >> 1)) ^ swz_v<C, false>(row)) * 16) + (col & 1) * 8;
+                    f.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+                }
+                vf = f.v;
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) o[i][d] = M::mul(vf, p[i], o[i][d]);
+        }
+    }
+};
+
+// four consecutive values of one row: the result, or a part's share of it
+template <int D>
+__device__ __forceinline__ void store_row(const Args& g, const Job& j, int r, int d, const f32x4& v, float m, float l)
+{
+    const int64_t t = j.t0 + r / g.G;
+    const int h = j.kvh * g.G + r % g.G;
+    if (g.parts == 1) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        if (g.q_bf16) {
+            typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(g.out) + t * g.ldo + (int64_t)h * D + d) =
+                b4{(__bf16)(v[0] * inv), (__bf16)(v[1] * inv), (__bf16)(v[2] * inv), (__bf16)(v[3] * inv)};
+        } else {
+            *reinterpret_cast<f16x4*>(reinterpret_cast<_Float16*>(g.out) + t * g.ldo + (int64_t)h * D + d) =
+                f16x4{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
+        }
+        if (d == 0 && g.lse) g.lse[t * g.Hq + h] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    } else {
+        const int64_t at = j.part * (g.T * g.Hq) + t * g.Hq + h;
+        if (l > 0.0f) *reinterpret_cast<f32x4*>(g.part_o + at * D + d) = v;   // (a part without keys is not read)
+        if (d == 0) g.part_ml[at] = make_float2(m, l);
+    }
+}
+
+template <class E, int D, int MT>
+__device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* lds)
+{
+    using SH = Shape<E, D>;
+    using R = Rows<E, D, MT>;
+    using V = typename R::V;
+    constexpr int C = SH::kChunks, kRow = SH::kRow, N = kTallKeys / 16;
+    constexpr bool kCodes = SH::kCodes;
+    const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const int row0 = j.row0 + wave * 16 * MT;
+
+    // tiles: the prefix's, then the sequence's
+    const int np = j.pb > j.pa ? (j.pb - j.pa + kTallKeys - 1) / kTallKeys : 0;
+    const int tiles = np + (j.ob > j.oa ? (j.ob - j.oa + kTallKeys - 1) / kTallKeys : 0);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
+    uint32_t est = 0;
+    auto first_key = [&](int tile) { return tile < np ? j.pa + tile * kTallKeys : j.oa + (tile - np) * kTallKeys; };
+    auto page_of = [&](int tile) {    // of this wavefront's 16 keys
+        const int key = min(first_key(tile) + wave * 16, (tile < np ? j.pb : j.ob) - 1);
+        return scalar_at(tile < np ? g.prefix_table : j.table, key >> g.page_shift);
+    };
+    int next_page = tiles > 0 ? page_of(0) : 0;
+    auto fetch = [&](int tile) {
+        int page = next_page;
+        if (tile + 1 < tiles) next_page = page_of(tile + 1);
+        if ((unsigned)page >= (unsigned)g.pages) { est |= AWEQ_ST_INDEX; page = 0; }
+        const int key0 = first_key(tile) + wave * 16, end = tile < np ? j.pb : j.ob;    // a multiple of 16: the group lies in one page
+        const uint32_t slot = lds0 + (uint32_t)(tile % SH::kStages) * SH::kSlot;
+        const int64_t head_row = ((int64_t)page * g.Hk + j.kvh) << g.page_shift;        // row of the cache where this head's page begins
+        const char* const kb = reinterpret_cast<const char*>(g.k_cache) + head_row * kRow;
+        const char* const vb = reinterpret_cast<const char*>(g.v_cache) + head_row * kRow;
+        const int in_page = g.page_size - 1;
+#pragma unroll
+        for (int q = 0; q < SH::kLoads; ++q) {
+            const int sub = q * SH::kRowsPerLoad + lane / C, trow = wave * 16 + sub;    // row of the 16, of the tile (the swizzle's)
+            const int row = min(key0 + sub, end - 1) & in_page;
+            const uint32_t at = slot + (uint32_t)(wave * 16 * kRow + q * 1024);
+            dma16(kb, (uint32_t)(row * kRow + ((lane % C) ^ swz_k<C>(trow)) * 16), at);
+            dma16(vb, (uint32_t)(row * kRow + ((lane % C) ^ swz_v<C, kCodes>(trow)) * 16), at + SH::kHalf);
+        }
+        if constexpr (kCodes) {
+            const int row = min(key0 + col, end - 1) & in_page;
+            dma4((grp & 1 ? g.v_step : g.k_step) + head_row + row, slot + 2 * SH::kHalf + (uint32_t)wave * 256);
         }
     };
 
     if (tiles > 0) fetch(0);
+    R rows;
+    rows.load(g, j, row0);
     for (int tile = 0; tile < tiles; ++tile) {
         wait_vm<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // this wavefront's reads of the tile before are done: its slot is filled next
-        if constexpr (WR > 1) __builtin_amdgcn_s_barrier();       // and everyone's, and the tile has landed for everyone
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();     // the tile has landed for everyone, and everyone is done with the one before
         if (tile + 1 < tiles) fetch(tile + 1);
-        const char* const kt = ring + (tile % TL::kStages) * TL::kSlot;
-        const char* const vt = kt + TL::kHalf;
-        const int key0 = first + tile * tile_step;
+        const char* const kt = lds + (tile % SH::kStages) * SH::kSlot;
+        const char* const vt = kt + SH::kHalf;
 
-        // S^T: 16 keys x 16 rows at a time
-        f32x4 s[MT][TL::kGroups];
+        f32x4 s[MT][N];
 #pragma unroll
-        for (int n = 0; n < TL::kGroups; ++n) {
+        for (int n = 0; n < N; ++n) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) s[i][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             const int row = n * 16 + col;
+            if constexpr (kCodes) {
 #pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk) {
-                V kf;
-                if constexpr (kCodes) {
-                    const int chunk = kk * 2 + (grp >> 1);
-                    kf = codes_to_f16(*reinterpret_cast<const i32x2*>(kt + row * TL::kRow + ((chunk ^ swz_k<C>(row)) * 16) + (grp & 1) * 8));
-                } else {
-                    kf = *reinterpret_cast<const V*>(kt + row * TL::kRow + (((kk * 4 + grp) ^ swz_k<C>(row)) * 16));
+                for (int kk = 0; kk < D / 64; ++kk) {
+                    const i32x4 w = *reinterpret_cast<const i32x4*>(kt + row * kRow + (((kk * 4 + grp) ^ swz_k<C>(row)) * 16));
+                    const V a = codes_to_f16(w[0], w[1]), b = codes_to_f16(w[2], w[3]);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(a, rows.q[i][2 * kk], s[i][n]);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(b, rows.q[i][2 * kk + 1], s[i][n]);
                 }
+            } else {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) s[i][n] = M::mul(kf, qf[i][kk], s[i][n]);
+                for (int kk = 0; kk < D / 32; ++kk) {
+                    const V kf = *reinterpret_cast<const V*>(kt + row * kRow + (((kk * 4 + grp) ^ swz_k<C>(row)) * 16));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(kf, rows.q[i][kk], s[i][n]);
+                }
             }
         }
-
-        // scores in units of log2, those past the row's keys minus infinity; the running maximum and sum
-        float lv[TL::kGroups][4], rv[TL::kGroups][4], ks[TL::kGroups][4];
+        float ks[N][4], vs[N][4];
         if constexpr (kCodes) {
 #pragma unroll
-            for (int n = 0; n < TL::kGroups; ++n) {
-                const Float4 a = *reinterpret_cast<const Float4*>(kt + 2 * TL::kHalf + n * 256 + grp * 16);
-                const Float4 c = *reinterpret_cast<const Float4*>(kt + 2 * TL::kHalf + n * 256 + 64 + grp * 16);
+            for (int n = 0; n < N; ++n) {
+                const Float4 a = *reinterpret_cast<const Float4*>(kt + 2 * SH::kHalf + n * 256 + grp * 16);
+                const Float4 c = *reinterpret_cast<const Float4*>(kt + 2 * SH::kHalf + n * 256 + 64 + grp * 16);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) { ks[n][v] = a.f[v]; lv[n][v] = __builtin_amdgcn_logf(c.f[v]); rv[n][v] = 1.0f / c.f[v]; }
+                for (int v = 0; v < 4; ++v) { ks[n][v] = a.f[v]; vs[n][v] = c.f[v]; }
             }
         }
-        V pf[MT][TL::kGroups / 2];
+        V p[MT][N / 2];
+        rows.template softmax<N>(s, p, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, ks, vs);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const bool edge = key0 + TL::kKeys > end || (!PREFIX && key0 + TL::kKeys > limit[i]);
-            float top = -INFINITY;
+        for (int u = 0; u < N / 2; ++u) {
+            V pu[MT];
 #pragma unroll
-            for (int n = 0; n < TL::kGroups; ++n)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    float x = s[i][n][v] * row_scale[i];
-                    if constexpr (kCodes) x = __builtin_fmaf(x, ks[n][v], lv[n][v]);
-                    if (edge) {
-                        const int key = key0 + n * 16 + grp * 4 + v;
-                        if (key >= end || key >= limit[i]) x = -INFINITY;
-                    }
-                    s[i][n][v] = x;
-                    top = fmaxf(top, x);
-                }
-            top = fmaxf(top, partner<4>(top));
-            top = fmaxf(top, partner<5>(top));
-            const float m_new = fmaxf(m[i], top);
-            const float m_use = m_new == -INFINITY ? 0.0f : m_new;
-            const float alpha = __builtin_amdgcn_exp2f(m[i] - m_use);
-            m[i] = m_new;
-            float sum = 0.0f;
-#pragma unroll
-            for (int n = 0; n < TL::kGroups; ++n)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float p = __builtin_amdgcn_exp2f(s[i][n][v] - m_use);
-                    if constexpr (kCodes) sum = __builtin_fmaf(p, rv[n][v], sum);
-                    else sum += p;
-                    pf[i][n / 2][(n & 1) * 4 + v] = (typename M::S)p;
-                }
-            l[i] = l[i] * alpha + sum;      // (of this lane's keys: added up across the wavefront at the end)
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) o[i][d] *= alpha;
+            for (int i = 0; i < MT; ++i) pu[i] = p[i][u];
+            rows.values(vt, u, pu);
         }
-
-        // O^T: 16 values x 16 rows at a time, 32 keys to a product
-#pragma unroll
-        for (int u = 0; u < TL::kGroups / 2; ++u)
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-                V vf;
-                if constexpr (kCodes) {
-                    const int r = col >> 1, row = u * 32 + 16 * (r >> 2) + 4 * grp + (r & 3);
-                    const char* const at = vt + row * TL::kRow + ((d ^ swz_v<C, true>(row)) * 16) + (col & 1) * 8;
-                    vf = codes_to_f16(__builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)at));
-                } else {
-                    union { s16x4 h[2]; V v; } f;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const int row = u * 32 + half * 16 + 4 * grp + (col >> 2);
-                        const char* const at = vt + row * TL::kRow + (((2 * d + ((col & 3) >> 1)) ^ swz_v<C, false>(row)) * 16) + (col & 1) * 8;
-                        f.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-                    }
-                    vf = f.v;
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) o[i][d] = M::mul(vf, pf[i][u], o[i][d]);
-            }
     }
     if (est && lane == 0) raise_status(g.status, est);
-
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        l[i] += partner<4>(l[i]);
-        l[i] += partner<5>(l[i]);
-    }
-
-    const int64_t all_rows = g.T * g.Hq;
-    // four consecutive values of one row: the result, or a part's share of it
-    auto store = [&](int r, int d, const f32x4& v, float mm, float ll) {
-        const int64_t t = t0 + r / g.G;
-        const int h = kvh * g.G + r % g.G;
-        if (g.parts == 1) {
-            const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-            if (g.q_bf16) {
-                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(g.out) + t * g.ldo + (int64_t)h * D + d) =
-                    b4{(__bf16)(v[0] * inv), (__bf16)(v[1] * inv), (__bf16)(v[2] * inv), (__bf16)(v[3] * inv)};
-            } else {
-                *reinterpret_cast<f16x4*>(reinterpret_cast<_Float16*>(g.out) + t * g.ldo + (int64_t)h * D + d) =
-                    f16x4{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
-            }
-            if (d == 0 && g.lse) g.lse[t * g.Hq + h] = ll > 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
-        } else {
-            const int64_t at = (int64_t)(g.first_part + split) * all_rows + t * g.Hq + h;
-            *reinterpret_cast<f32x4*>(g.part_o + at * D + d) = v;
-            if (d == 0) g.part_ml[at] = make_float2(mm, ll);
-        }
-    };
-
-    if constexpr (WR > 1) {
+        const float l = row_reduce(rows.l[i], OpAdd());
+        const int r = row0 + 16 * i + col;
+        if (r < j.rows) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int r = row0 + 16 * i + col;
-            if (r < rows) {
-#pragma unroll
-                for (int d = 0; d < D / 16; ++d) store(r, d * 16 + grp * 4, o[i][d], m[i], l[i]);
-            }
-        }
-    } else {
-        // the wavefronts' ranges of the same 16 rows
-        __syncthreads();   // (every wavefront is done with its ring)
-        float* const so = reinterpret_cast<float*>(lds);                         // [wave][row][D]
-        float* const sm = so + TL::kWaves * 16 * D;                              // [wave][row][2]
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(so + (wave * 16 + col) * D + d * 16 + grp * 4) = o[0][d];
-        if (grp == 0) { sm[(wave * 16 + col) * 2] = m[0]; sm[(wave * 16 + col) * 2 + 1] = l[0]; }
-        __syncthreads();
-        for (int e = threadIdx.x; e < 16 * D / 4; e += TL::kThreads) {
-            const int r = e / (D / 4), d = e % (D / 4) * 4;
-            if (row0 + r >= rows) continue;
-            float mm = -INFINITY, ll = 0.0f;
-#pragma unroll
-            for (int w = 0; w < TL::kWaves; ++w) mm = fmaxf(mm, sm[(w * 16 + r) * 2]);
-            const float use = mm == -INFINITY ? 0.0f : mm;
-            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < TL::kWaves; ++w) {
-                const float a = __builtin_amdgcn_exp2f(sm[(w * 16 + r) * 2] - use);
-                ll += a * sm[(w * 16 + r) * 2 + 1];
-                v += a * *reinterpret_cast<const f32x4*>(so + (w * 16 + r) * D + d);
-            }
-            store(row0 + r, d, v, mm, ll);
+            for (int d = 0; d < D / 16; ++d) store_row<D>(g, j, r, d * 16 + grp * 4, rows.o[i][d], rows.m[i], l);
         }
     }
 }
 
-// A row's parts joined: one wavefront each
+template <class E, int D>
+__device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* lds)
+{
+    using SH = Shape<E, D>;
+    using R = Rows<E, D, 1>;
+    using V = typename R::V;
+    constexpr int C = SH::kChunks, kRow = SH::kRow, N = kWideKeys / 16;
+    constexpr bool kCodes = SH::kCodes;
+    const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+
+    // one range: the prefix's or the sequence's
+    const bool own = j.ob > j.oa;
+    const int begin = own ? j.oa : j.pa, end = own ? j.ob : j.pb;
+    const int32_t* const table = own ? j.table : g.prefix_table;
+    const int first = begin + wave * kWideKeys, step = kWaves * kWideKeys;
+    const int tiles = end > first ? (end - first + step - 1) / step : 0;
+    uint32_t est = 0;
+    char* const vt = lds + wave * SH::kWideSlot;
+
+    // a tile as it is in flight: K in the operand's order, V 16 bytes a lane, rows across the lanes
+    constexpr int kK = N * D / (kCodes ? 64 : 32), kV = N * SH::kLoads;
+    i32x4 kr[kK], vr[kV];
+    Float4 kst[N], vst[N];
+    int next_page[N];
+    auto pages_of = [&](int tile) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) next_page[n] = scalar_at(table, min(first + tile * step + n * 16, end - 1) >> g.page_shift);
+    };
+    auto request = [&](int tile) {
+        const int in_page = g.page_size - 1;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            int page = next_page[n];
+            if ((unsigned)page >= (unsigned)g.pages) { est |= AWEQ_ST_INDEX; page = 0; }
+            const int64_t head_row = ((int64_t)page * g.Hk + j.kvh) << g.page_shift;
+            const int key0 = first + tile * step + n * 16;
+            const char* const kb = reinterpret_cast<const char*>(g.k_cache) + head_row * kRow;
+            const char* const vb = reinterpret_cast<const char*>(g.v_cache) + head_row * kRow;
+            const int krow = min(key0 + col, end - 1) & in_page;
+#pragma unroll
+            for (int kk = 0; kk < kK / N; ++kk) kr[n * (kK / N) + kk] = *reinterpret_cast<const i32x4*>(kb + (uint32_t)(krow * kRow + (kk * 4 + grp) * 16));
+#pragma unroll
+            for (int q = 0; q < SH::kLoads; ++q) {
+                const int row = min(key0 + q * SH::kRowsPerLoad + lane / C, end - 1) & in_page;
+                vr[n * SH::kLoads + q] = *reinterpret_cast<const i32x4*>(vb + (uint32_t)(row * kRow + (lane % C) * 16));
+            }
+            if constexpr (kCodes) {   // (those past the end are 1 below: what lies there may be anything)
+                const int row = ((key0 < end ? key0 : (end - 1) & ~15) & in_page) + grp * 4;
+                kst[n] = *reinterpret_cast<const Float4*>(g.k_step + head_row + row);
+                vst[n] = *reinterpret_cast<const Float4*>(g.v_step + head_row + row);
+            }
+        }
+    };
+    if (tiles > 0) {
+        pages_of(0);
+        request(0);
+        if (tiles > 1) pages_of(1);
+    }
+    R rows;
+    rows.load(g, j, j.row0);
+    for (int tile = 0; tile < tiles; ++tile) {
+        f32x4 s[1][N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            s[0][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kk = 0; kk < kK / N; ++kk) {
+                const i32x4 w = kr[n * (kK / N) + kk];
+                if constexpr (kCodes) {
+                    s[0][n] = R::M::mul(codes_to_f16(w[0], w[1]), rows.q[0][2 * kk], s[0][n]);
+                    s[0][n] = R::M::mul(codes_to_f16(w[2], w[3]), rows.q[0][2 * kk + 1], s[0][n]);
+                } else {
+                    s[0][n] = R::M::mul(__builtin_bit_cast(V, w), rows.q[0][kk], s[0][n]);
+                }
+            }
+        }
+        wave_lds_fence();     // (the reads of the tile before are ahead of these writes)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int q = 0; q < SH::kLoads; ++q) {
+                const int row = n * 16 + q * SH::kRowsPerLoad + lane / C;
+                *reinterpret_cast<i32x4*>(vt + row * kRow + (((lane % C) ^ swz_v<C, kCodes>(row)) * 16)) = vr[n * SH::kLoads + q];
+            }
+        wave_lds_fence();
+        float ks[N][4], vs[N][4];
+        if constexpr (kCodes) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const bool in = first + tile * step + n * 16 + grp * 4 + v < end;
+                    ks[n][v] = in ? kst[n].f[v] : 1.0f;
+                    vs[n][v] = in ? vst[n].f[v] : 1.0f;
+                }
+        }
+        if (tile + 1 < tiles) {
+            request(tile + 1);
+            if (tile + 2 < tiles) pages_of(tile + 2);
+        }
+        V p[1][N / 2];
+        rows.template softmax<N>(s, p, first + tile * step, end, own, ks, vs);
+#pragma unroll
+        for (int u = 0; u < N / 2; ++u) {
+            const V pu[1] = {p[0][u]};
+            rows.values(vt, u, pu);
+        }
+    }
+    if (est && lane == 0) raise_status(g.status, est);
+
+    // the wavefronts' keys of the same 16 rows
+    const float l = row_reduce(rows.l[0], OpAdd());
+    __syncthreads();   // (every wavefront is done with its tiles)
+    float* const so = reinterpret_cast<float*>(lds);                         // [wave][row][D]
+    float* const sm = so + kWaves * kWideRows * D;                           // [wave][row][2]
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(so + (wave * 16 + col) * D + ((d * 4 + grp) ^ col) * 4) = rows.o[0][d];
+    if (grp == 0) { sm[(wave * 16 + col) * 2] = rows.m[0]; sm[(wave * 16 + col) * 2 + 1] = l; }
+    __syncthreads();
+    for (int e = threadIdx.x; e < kWideRows * D / 4; e += kThreads) {
+        const int r = e / (D / 4), d = e % (D / 4);
+        if (j.row0 + r >= j.rows) continue;
+        float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, sm[(w * 16 + r) * 2]);
+        const float use = mm == -INFINITY ? 0.0f : mm;
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float a = __builtin_amdgcn_exp2f(sm[(w * 16 + r) * 2] - use);
+            ll += a * sm[(w * 16 + r) * 2 + 1];
+            v += a * *reinterpret_cast<const f32x4*>(so + (w * 16 + r) * D + (d ^ r) * 4);
+        }
+        store_row<D>(g, j, j.row0 + r, d * 4, v, mm, ll);
+    }
+}
+
+// Wavefronts a SIMD that the registers have to allow
+constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : 1; }
+
+// MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it
+template <class E, int D, int MT>
+__global__ __launch_bounds__(kThreads, waves_wanted(D, MT)) void attention_kernel(Args g)
+{
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    const bool shared = (int)blockIdx.x < g.shared.blocks;
+    const Work& w = shared ? g.shared : g.own;
+    const int id = (int)blockIdx.x - (shared ? 0 : g.shared.blocks);
+    // Workgroup ids go round-robin over the XCDs: all row tiles of one range of a key head to the same one, whose L2 then has the range's K and V
+    const int seq = id / kXcdCount, combo = seq / w.row_tiles * kXcdCount + id % kXcdCount;
+    if (combo >= w.combos) return;
+    const int split = combo / g.Hk % w.splits, b = combo / g.Hk / w.splits;
+    const int tile_rows = w.tall ? kWaves * 16 * MT : kWideRows;
+    Job j;
+    j.kvh = combo % g.Hk;
+    j.row0 = seq % w.row_tiles * tile_rows;
+    j.part = w.first_part + split;
+    j.pa = j.pb = j.oa = j.ob = 0;
+    j.sees0 = 0;
+    j.table = g.table;
+    uint32_t est = 0;
+    if (shared) {
+        j.t0 = 0;
+        j.rows = (int)g.T * g.G;
+        j.pa = split * w.chunk;
+        j.pb = min(j.pa + w.chunk, g.prefix_len);
+    } else {
+        int64_t t0 = b, t1 = b + 1;
+        if (g.q_start) {
+            t0 = scalar_at(g.q_start, b);
+            t1 = scalar_at(g.q_start, b + 1);
+            if (t0 < 0 || t1 < t0 || t1 > g.T || t1 - t0 > g.max_q) est |= AWEQ_ST_INDEX;
+            t0 = min(max(t0, (int64_t)0), g.T);
+            t1 = min(max(t1, t0), min(g.T, t0 + g.max_q));
+        }
+        const int tokens = (int)(t1 - t0);
+        int len = scalar_at(g.lens, b);
+        const int most = (int)min((int64_t)g.max_len, g.table_ld << g.page_shift);
+        if (len < 0 || len > most) est |= AWEQ_ST_INDEX;
+        len = min(max(len, 0), most);
+        if (est && threadIdx.x == 0) raise_status(g.status, est);
+        j.t0 = t0;
+        j.rows = tokens * g.G;
+        if (j.row0 >= j.rows) return;
+        j.sees0 = len - tokens + 1;
+        j.table = g.table + (int64_t)b * g.table_ld;
+        const int seen = max(0, min(len, j.sees0 + min((j.row0 + tile_rows - 1) / g.G, tokens - 1)));   // by the workgroup's last row
+        if (w.chunk) {
+            j.oa = split * w.chunk;
+            j.ob = min(j.oa + w.chunk, seen);
+        } else {
+            // a share of the tiles of the prefix and the sequence together
+            const int np = g.fused ? (g.prefix_len + kTallKeys - 1) / kTallKeys : 0, all = np + (seen + kTallKeys - 1) / kTallKeys;
+            const int lo = (int)((int64_t)all * split / w.splits), hi = (int)((int64_t)all * (split + 1) / w.splits);
+            j.pa = min(lo, np) * kTallKeys;
+            j.pb = min(min(hi, np) * kTallKeys, g.fused ? g.prefix_len : 0);
+            j.oa = (max(lo, np) - np) * kTallKeys;
+            j.ob = min((max(hi, np) - np) * kTallKeys, seen);
+        }
+    }
+    if constexpr (MT > 0) {
+        if (w.tall) tall_block<E, D, MT>(g, j, lds);
+        else wide_block<E, D>(g, j, lds);
+    } else {
+        wide_block<E, D>(g, j, lds);
+    }
+}
+
+// A row's parts joined, a wavefront each: lane p has the maximum and sum of part p, the values are read D / 4 lanes to a part
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(Args g)
 {
     const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave, all_rows = g.T * g.Hq;
     if (row >= all_rows) return;
     const int lane = threadIdx.x & (kWave - 1);
-    float mm = -INFINITY;
-    for (int p = 0; p < g.parts; ++p) mm = fmaxf(mm, g.part_ml[p * all_rows + row].x);
-    const float use = mm == -INFINITY ? 0.0f : mm;
-    constexpr int N = D / kWave;
-    float ll = 0.0f, v[N] = {};
-    for (int p = 0; p < g.parts; ++p) {
-        const float2 ml = g.part_ml[p * all_rows + row];
-        if (!(ml.y > 0.0f)) continue;
-        const float a = __builtin_amdgcn_exp2f(ml.x - use);
-        ll += a * ml.y;
-        const float* const src = g.part_o + (p * all_rows + row) * D + lane * N;
+    constexpr int kLanes = D / 4, kAtOnce = kWave / kLanes;
+    const int sub = lane / kLanes, at = lane % kLanes * 4;
+    float2 ml = make_float2(-INFINITY, 0.0f);
+    if (lane < g.parts) ml = g.part_ml[lane * all_rows + row];
+    const float mm = wave_allreduce(ml.x, Larger());
+    const float w = ml.y > 0.0f ? __builtin_amdgcn_exp2f(ml.x - mm) : 0.0f;
+    const float ll = wave_allreduce(w * ml.y, OpAdd());
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kFlight = 4;
+    for (int p0 = 0; p0 < g.parts; p0 += kAtOnce * kFlight) {
+        f32x4 x[kFlight];
+        float a[kFlight];
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += a * src[i];
+        for (int f = 0; f < kFlight; ++f) {
+            const int p = p0 + f * kAtOnce + sub;
+            a[f] = __shfl(w, p & (kWave - 1));
+            if (p >= g.parts) a[f] = 0.0f;
+            x[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (a[f] != 0.0f) x[f] = *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)p * all_rows + row) * D + at);
+        }
+#pragma unroll
+        for (int f = 0; f < kFlight; ++f) v += a[f] * x[f];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (kAtOnce > 2) v[e] += __shfl_xor(v[e], 16);
+        if constexpr (kAtOnce > 1) v[e] += __shfl_xor(v[e], 32);
     }
     const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-    const int64_t t = row / g.Hq, at = t * g.ldo + row % g.Hq * D + lane * N;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if (g.q_bf16) reinterpret_cast<__bf16*>(g.out)[at + i] = (__bf16)(v[i] * inv);
-        else reinterpret_cast<_Float16*>(g.out)[at + i] = (_Float16)(v[i] * inv);
+    if (sub == 0) {
+        const int64_t to = row / g.Hq * g.ldo + row % g.Hq * D + at;
+        if (g.q_bf16) {
+            typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(g.out) + to) = b4{(__bf16)(v[0] * inv), (__bf16)(v[1] * inv), (__bf16)(v[2] * inv), (__bf16)(v[3] * inv)};
+        } else {
+            *reinterpret_cast<f16x4*>(reinterpret_cast<_Float16*>(g.out) + to) = f16x4{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
+        }
     }
     if (lane == 0 && g.lse) g.lse[row] = ll > 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
 }
 
 // How a call is cut up
 struct Plan {
-    int prefix_rows, own_rows;        // rows of a workgroup: 16, 64 or 128
-    int prefix_splits, own_splits;    // 0: no such keys
-    int parts() const { return prefix_splits + own_splits; }
+    int mt;             // row tiles of a wavefront of the tall form, 0: none
+    int fused;
+    Work shared, own;   // splits 0: no such work
+    int parts() const { return shared.splits + own.splits; }
 };
 
-static int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 64 ? 64 : 128; }
+constexpr int kMostSplits = 32;   // (64 parts at most: a lane each where they are joined)
 
-static int split_count(int64_t items, int64_t len, int64_t least)
+// ranges of `len` keys so that `items` of them each make up about `want` workgroups, of `least` keys or more
+static int split_count(int64_t items, int64_t len, int64_t want, int64_t least)
 {
-    const int64_t want = cdiv(512, items), most = cdiv(len, least);
-    const int64_t n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    const int64_t n = cdiv(want, items), most = cdiv(len, least);
+    const int64_t k = n < most ? n : most;
+    return (int)(k < 1 ? 1 : k > kMostSplits ? kMostSplits : k);
+}
+static void set_work(Work& w, int64_t rows, int mt, int64_t splits, int64_t len, int64_t items)
+{
+    const int tile = w.tall ? kWaves * 16 * mt : kWideRows, unit = w.tall ? kTallKeys : kWaves * kWideKeys;
+    w.row_tiles = (int)cdiv(rows, tile);
+    w.chunk = (int)(cdiv(cdiv(len, splits), unit) * unit);
+    if (w.chunk < unit) w.chunk = unit;
+    w.splits = len > 0 ? (int)cdiv(len, w.chunk) : 1;
+    w.combos = (int)(items * w.splits);
 }
 
 static Plan plan(int64_t T, int64_t Hq, int64_t Hk, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len)
 {
-    const int64_t G = Hq / Hk;
-    Plan p = {16, 16, 0, 0};
-    if (prefix_len > 0) {
-        p.prefix_rows = tile_rows(T * G);
-        p.prefix_splits = split_count(Hk * cdiv(T * G, p.prefix_rows), prefix_len, 256);
+    const int64_t G = Hq / Hk, all_rows = T * G, most_rows = max_q * G;
+    Plan p = {};
+    const bool own_tall = most_rows > kWideRows, shared_tall = all_rows > kWideRows;
+    // Where sequences have a tile's rows each, on average, they take the prefix along: every row tile reads it once either way, and nothing is
+    // left to join
+    p.fused = prefix_len > 0 && own_tall && all_rows >= B * 128;
+    const bool has_shared = prefix_len > 0 && !p.fused, has_own = max_len > 0 || prefix_len == 0 || p.fused;
+    p.mt = has_own && own_tall ? (most_rows > 64 ? 2 : 1) : 0;
+    if (has_shared && shared_tall && p.mt < 2) p.mt = all_rows > 64 || p.mt == 2 ? 2 : 1;
+    if (has_shared) {
+        p.shared.tall = shared_tall;
+        const int64_t tile = shared_tall ? kWaves * 16 * p.mt : kWideRows;
+        set_work(p.shared, all_rows, p.mt, split_count(Hk * cdiv(all_rows, tile), prefix_len, 256, 512), prefix_len, Hk);
     }
-    if (max_len > 0 || prefix_len == 0) {
-        p.own_rows = tile_rows(max_q * G);
-        p.own_splits = split_count(B * Hk * cdiv(max_q * G, p.own_rows), max_len, 256);
+    if (has_own) {
+        p.own.tall = own_tall;
+        const int64_t tile = own_tall ? kWaves * 16 * p.mt : kWideRows, items = B * Hk * cdiv(most_rows, tile);
+        const int64_t keys = max_len + (p.fused ? prefix_len : 0);
+        set_work(p.own, most_rows, p.mt, split_count(items, keys, own_tall ? 512 : 2048, 256), keys, B * Hk);
+        if (own_tall) p.own.chunk = 0;
     }
     return p;
 }
 
-template <class E, int D, int WR, int MT, bool PREFIX>
-static int launch_one(Args g, int64_t blocks, hipStream_t st)
+template <class E, int D, int MT>
+static int launch_one(const Args& g, int64_t blocks, hipStream_t st)
 {
-    using TL = Tile<E, D, WR>;
-    const void* fn = reinterpret_cast<const void*>(attention_kernel<E, D, WR, MT, PREFIX>);
+    constexpr int lds = Shape<E, D>::lds(MT > 0);
+    const void* fn = reinterpret_cast<const void*>(attention_kernel<E, D, MT>);
     int dev = 0, cus = 0;
-    if (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, TL::kLds) != AWEQ_OK) return AWEQ_ERR_LAUNCH;
-    void* args[] = {&g};
-    if (hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(TL::kThreads), args, TL::kLds, st) != hipSuccess) return AWEQ_ERR_LAUNCH;
-    return AWEQ_OK;
-}
-
-template <class E, int D, bool PREFIX>
-static int launch_rows(Args g, int rows, int64_t most_rows, int splits, int first_part, hipStream_t st)
-{
-    g.splits = splits;
-    g.first_part = first_part;
-    g.row_tiles = (int)cdiv(most_rows, rows);
-    const int64_t blocks = (int64_t)splits * g.row_tiles * g.Hk * (PREFIX ? 1 : g.B);
-    if (blocks > (1 << 24) - 1) return AWEQ_ERR_SHAPE;
-    if (rows == 16) return launch_one<E, D, 1, 1, PREFIX>(g, blocks, st);
-    if (rows == 64) return launch_one<E, D, 4, 1, PREFIX>(g, blocks, st);
-    return launch_one<E, D, 4, 2, PREFIX>(g, blocks, st);
+    if (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, lds) != AWEQ_OK) return AWEQ_ERR_LAUNCH;
+    void* args[] = {const_cast<Args*>(&g)};
+    return hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(kThreads), args, lds, st) == hipSuccess ? AWEQ_OK : AWEQ_ERR_LAUNCH;
 }
 
 template <class E, int D>
-static int launch(const Args& g, const Plan& p, hipStream_t st)
+static int launch(Args& g, const Plan& p, hipStream_t st)
 {
-    int rc = AWEQ_OK;
-    if (p.prefix_splits) rc = launch_rows<E, D, true>(g, p.prefix_rows, g.T * g.G, p.prefix_splits, 0, st);
-    if (rc == AWEQ_OK && p.own_splits) rc = launch_rows<E, D, false>(g, p.own_rows, (int64_t)g.max_q * g.G, p.own_splits, p.prefix_splits, st);
-    if (rc == AWEQ_OK && p.parts() > 1) join_kernel<D><<<(unsigned)cdiv(g.T * g.Hq, 4), 256, 0, st>>>(g);
+    int64_t blocks = 0;
+    g.shared = p.shared;
+    g.own = p.own;
+    g.own.first_part = p.shared.splits;
+    for (Work* w : {&g.shared, &g.own}) {
+        const int64_t n = w->splits ? cdiv(w->combos, kXcdCount) * kXcdCount * w->row_tiles : 0;
+        blocks += n;
+        if (blocks > (1 << 24) - 1) return AWEQ_ERR_SHAPE;   // 2^32 threads
+        w->blocks = (int)n;
+    }
+    const int rc = p.mt == 0 ? launch_one<E, D, 0>(g, blocks, st) : p.mt == 1 ? launch_one<E, D, 1>(g, blocks, st) : launch_one<E, D, 2>(g, blocks, st);
+    if (rc == AWEQ_OK && g.parts > 1) join_kernel<D><<<(unsigned)cdiv(g.T * g.Hq, 4), 256, 0, st>>>(g);
     return rc != AWEQ_OK ? rc : launch_status();
 }
 
 template <class E>
-static int launch_head(const Args& g, const Plan& p, int64_t D, hipStream_t st)
+static int launch_head(Args& g, const Plan& p, int64_t D, hipStream_t st)
 {
     if (D == 64) return launch<E, 64>(g, p, st);
     if (D == 128) return launch<E, 128>(g, p, st);
@@ -560,8 +819,8 @@ static int launch_head(const Args& g, const Plan& p, int64_t D, hipStream_t st)
 static bool shapes_ok(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len)
 {
     if (T <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (D != 64 && D != 128 && D != 256) || B <= 0 || max_q <= 0) return false;
-    if (prefix_len < 0 || max_len < 0 || prefix_len > (1 << 30) || max_len > (1 << 30)) return false;
-    return T <= (1 << 24) && B <= (1 << 24) && Hq <= (1 << 16) && T * Hq <= (1 << 25);
+    if (prefix_len < 0 || max_len < 0 || prefix_len > (1 << 29) || max_len > (1 << 29)) return false;
+    return T <= (1 << 24) && B <= (1 << 20) && Hq <= (1 << 16) && T * Hq <= (1 << 25) && B * Hk <= (1 << 24);
 }
 
 }  // namespace attn
@@ -590,6 +849,7 @@ extern "C" int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, in
     if (!attn::shapes_ok(T, Hq, Hk, D, B, max_q, prefix_len, max_len)) return AWEQ_ERR_SHAPE;
     max_q = max_q < T ? max_q : T;
     if (pages <= 0 || pages > 0x7fffffff || page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0) return AWEQ_ERR_SHAPE;
+    if (!(scale > 0.0f) || std::isinf(scale)) return AWEQ_ERR_SHAPE;
     if (ldq < Hq * D || ldo < Hq * D || (!q_start && (T != B || max_q != 1)) || (max_len > 0 && table_ld < 1)) return AWEQ_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(out) || (ldq % 8) != 0 || (ldo % 8) != 0 || !aligned16(k_cache) || !aligned16(v_cache) ||
         (cache_dt == AWEQ_I8 && (!aligned16(k_step) || !aligned16(v_step))))
@@ -602,11 +862,12 @@ extern "C" int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, in
     g.q = q; g.k_cache = k_cache; g.v_cache = v_cache; g.k_step = k_step; g.v_step = v_step;
     g.prefix_table = prefix_table; g.table = table; g.lens = lens; g.q_start = q_start;
     g.out = out; g.lse = lse; g.status = status;
-    g.T = T; g.ldq = ldq; g.ldo = ldo; g.table_ld = table_ld; g.prefix_len = prefix_len; g.max_len = max_len;
+    g.T = T; g.ldq = ldq; g.ldo = ldo; g.table_ld = table_ld; g.prefix_len = (int)prefix_len; g.max_len = (int)max_len;
     g.pages = (int)pages; g.page_size = (int)page_size; g.page_shift = __builtin_ctz((unsigned)page_size);
-    g.Hq = (int)Hq; g.Hk = (int)Hk; g.G = (int)(Hq / Hk); g.B = (int)B; g.max_q = (int)max_q;
+    g.Hq = (int)Hq; g.Hk = (int)Hk; g.G = (int)(Hq / Hk); g.max_q = (int)max_q;
     g.q_bf16 = dt == AWEQ_BF16;
     g.parts = p.parts();
+    g.fused = p.fused;
     g.scale_log2e = scale * attn::kLog2e;
     g.part_o = reinterpret_cast<float*>(ws);
     g.part_ml = reinterpret_cast<float2*>(g.part_o + (size_t)g.parts * (size_t)(T * Hq) * (size_t)D);
