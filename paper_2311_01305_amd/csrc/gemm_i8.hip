@@ -1414,15 +1414,18 @@ extern "C" int aweq_w8a8_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, 
     const int prc = plan_tiled(g, half, tiled_cost, blocks);
     if (prc != AWEQ_OK) return prc;
     hipStream_t st = as_stream(stream);
-    if (!codes) {
-        const int rc = launch_quant_tokens(X, x_dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, status, st);
-        if (rc != AWEQ_OK) return rc;
-    }
     // the form as in aweq_w8a8_gemm
     const FewPlan few = plan_few(T, N);
     MidPlan mid = plan_mid(T, N);
     if (K <= 512 && mid.cost > 43.0) mid.cost *= 1.2;
-    if (few.cost <= mid.cost && few.cost < kTiledRoundCost * tiled_cost) return launch_gemm_i8_few(g, few, st, true);
+    const bool by_few = few.cost <= mid.cost && few.cost < kTiledRoundCost * tiled_cost;
+    if (by_few && !codes && x_dt != AWEQ_F32 && T <= kQuantTokens && T * panel_count(K) * kPanel <= kQuantFewBytes)
+        return launch_gemm_i8_few_tokens(g, few, TokenIn{{X, ldx, inv_s, xq, rowsum_x}, step_x, zero_x}, x_dt == AWEQ_F16, st);
+    if (!codes) {
+        const int rc = launch_quant_tokens(X, x_dt, T, K, ldx, inv_s, xq, step_x, zero_x, rowsum_x, status, st);
+        if (rc != AWEQ_OK) return rc;
+    }
+    if (by_few) return launch_gemm_i8_few(g, few, st, true);
     if (mid.cost < kTiledRoundCost * tiled_cost) return launch_gemm_i8_mid(g, mid, st, true);
     const void* fn = nullptr;
 #define AWEQ_PICK(O, D)                                                                                                \

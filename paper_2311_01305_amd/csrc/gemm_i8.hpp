@@ -73,7 +73,12 @@ struct QuantIn {
     int8_t* xq;
     int32_t* rowsum_x;
 };
+struct TokenIn : QuantIn {   // a quantizer a token, which the launch finds; inv_s may be null
+    float* step;
+    int32_t* zero;
+};
 int launch_gemm_i8_few_quant(const GemmArgs& g, const FewPlan& p, const QuantIn& in, bool f16, hipStream_t st);
+int launch_gemm_i8_few_tokens(const GemmArgs& g, const FewPlan& p, const TokenIn& in, bool f16, hipStream_t st);   // binary16 or bfloat16 tokens
 constexpr int kQuantTokens = 4;
 constexpr int64_t kQuantFewBytes = 16384;   // codes such a launch may hold
 

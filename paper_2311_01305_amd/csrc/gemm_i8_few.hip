@@ -15,6 +15,9 @@
 // (22016 x 8192 at one token: 180 MB, 5.9 TB/s.)
 #include "act_unit.hpp"
 #include "gemm_i8.hpp"
+#include "token_range.hpp"
+
+#include <type_traits>
 
 namespace aweq {
 namespace few {
@@ -30,9 +33,10 @@ constexpr int kWaves = kThreads / kWave;
 // requested ahead of the weights; behind them the quantizer waited for the weights first (us a call, weights in the caches, before -> now, with reads of the tokens that
 // leave them in the caches for the other workgroups: one token 4096 x 4096 6.4 -> 5.15, 8192 x 8192 16.0 -> 13.6, 4096 x 16384 18.0 -> 15.6,
 // 11008 x 4096 10.85 -> 9.3; four tokens 16384 x 4096 15.1 -> 12.95).
-// TOK: Step and Z of the activations are a token's.
+// TOK: Step and Z of the activations are a token's.  With QX (1: binary16, 3: bfloat16) every workgroup finds them too, one exchange over the workgroup
+// more, before it quantises, and the first one writes them.
 template <int TT, int NT, int D, int QX, int TQ, bool TOK>
-__global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
+__global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std::conditional<TOK, TokenIn, QuantIn>::type in)
 {
     extern __shared__ __attribute__((aligned(16))) int red[];   // [wave][TT NT][lane][4], then (QX) the tokens' codes, K padded to panels
     __shared__ int s_rs[kQuantTokens];
@@ -79,9 +83,25 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
     constexpr int kRounds = TQ == 1 ? 4 : 2;
     static_assert(QX == 0 || TQ * kRounds * kThreads * 8 >= kQuantFewBytes, "every code has a thread");
     const int units = (int)(g.K / 8), padded = np * (kPanel / 8);
-    RawUnit<QX == 1> raw[QX != 0 ? kRounds : 1][QX != 0 ? TQ : 1];
+    RawUnit<QX == 1> raw[QX != 0 && !TOK ? kRounds : 1][QX != 0 && !TOK ? TQ : 1];
     Float4 is[QX != 0 ? kRounds : 1][2];
-    if constexpr (QX != 0) {
+    typedef typename std::conditional<QX == 3, __bf16, _Float16>::type TokE;
+    Unit<TokE> traw[TOK && QX != 0 ? kRounds : 1][TOK && QX != 0 ? TQ : 1];
+    if constexpr (QX != 0 && TOK) {
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            if (i * kThreads >= padded) break;
+            const int u = min(i * kThreads + (int)threadIdx.x, units - 1);   // (past K the last unit again: nothing new in its range, its codes are not kept)
+#pragma unroll
+            for (int t = 0; t < TQ; ++t)
+                if (TQ <= 2 || t < (int)g.T) traw[i][t] = load_unit(reinterpret_cast<const TokE*>(in.X) + t * in.ldx + u * 8);
+            is[i][0] = is[i][1] = Float4{{1.0f, 1.0f, 1.0f, 1.0f}};
+            if (in.inv_s) {
+                is[i][0] = *reinterpret_cast<const Float4*>(in.inv_s + u * 8);
+                is[i][1] = *reinterpret_cast<const Float4*>(in.inv_s + u * 8 + 4);
+            }
+        }
+    } else if constexpr (QX != 0) {
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
             if (i * kThreads >= padded) break;
@@ -132,7 +152,83 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
     }
     if constexpr (QX == 0) request_constants();
     int8_t* const codes = reinterpret_cast<int8_t*>(red + kWaves * TT * NT * kWave * 4);
-    if constexpr (QX != 0) {
+    if constexpr (QX != 0 && TOK) {
+        __shared__ float s_lo[kWaves][TQ], s_hi[kWaves][TQ];
+        const int T = (int)g.T;
+        float lo[TQ], hi[TQ];
+        bool finite = true;
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) lo[t] = hi[t] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            if (i * kThreads >= padded) break;
+            float isf[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { isf[e] = is[i][0].f[e]; isf[4 + e] = is[i][1].f[e]; }
+#pragma unroll
+            for (int t = 0; t < TQ; ++t) {
+                if (TQ > 2 && t >= T) break;
+                float xf[8];
+                widen<TokE>(traw[i][t], xf);
+                token_extremes(xf, isf, lo[t], hi[t], finite);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) {
+            lo[t] = wave_allreduce(lo[t], OpMin());
+            hi[t] = wave_allreduce(hi[t], OpMax());
+            if (lane == 0) { s_lo[wave][t] = lo[t]; s_hi[wave][t] = hi[t]; }
+        }
+        if (threadIdx.x < kQuantTokens) s_rs[threadIdx.x] = 0;
+        __syncthreads();
+        ActParams ap[TQ];
+        int rs[TQ];
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) { lo[t] = fminf(lo[t], s_lo[w][t]); hi[t] = fmaxf(hi[t], s_hi[w][t]); }
+            float step;
+            int zero;
+            token_params(lo[t], hi[t], step, zero);
+            ap[t] = quot_params(step, zero);
+            rs[t] = 0;
+            if (threadIdx.x == 0) {
+                s_sx[t] = step;
+                s_zx[t] = zero - 128;
+                if (blockIdx.x == 0 && t < T) { in.step[t] = step; in.zero[t] = zero; }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            if (i * kThreads >= padded) break;
+            const int u = i * kThreads + (int)threadIdx.x;
+            float isf[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { isf[e] = is[i][0].f[e]; isf[4 + e] = is[i][1].f[e]; }
+#pragma unroll
+            for (int t = 0; t < TQ; ++t) {
+                if (TQ > 2 && t >= T) break;
+                float xf[8];
+                widen<TokE>(traw[i][t], xf);
+                int r8 = 0;
+                uint2 c = token_unit(xf, isf, ap[t], r8);
+                if (u >= units) { c = make_uint2(0u, 0u); r8 = 0; }   // (the zero fill of the last panel)
+                rs[t] += r8;
+                if (u >= padded) continue;
+                *reinterpret_cast<uint2*>(codes + (t * padded + u) * 8) = c;
+                if (blockIdx.x == 0) *reinterpret_cast<uint2*>(in.xq + ((int64_t)(u >> 3) * T + t) * kPanel + (u & 7) * 8) = c;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) {
+            if (TQ > 2 && t >= T) break;
+            rs[t] = wave_allreduce(rs[t], OpAdd());
+            if (lane == 0) atomicAdd(&s_rs[t], rs[t]);
+        }
+        if (blockIdx.x == 0) raise_status(g.status, finite ? 0u : (uint32_t)AWEQ_ST_NONFINITE);
+        __syncthreads();
+        if (blockIdx.x == 0 && (int)threadIdx.x < T) in.rowsum_x[threadIdx.x] = s_rs[threadIdx.x];
+    } else if constexpr (QX != 0) {
         const ActParams ap = quot_params(*g.act_step, *g.act_zero);
         uint32_t st = 0;
         float big = 0.0f;
@@ -288,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, QuantIn in)
 // Token tiles ride on the grid's y dimension, at most 65535 to a launch: layers of up to 64 channels come here at any number of tokens
 constexpr int kMaxGridY = 65535;
 template <int TT, int NT, int D, int QX = 0, int TQ = 1, bool TOK = false>
-static int launch_tile(GemmArgs g, hipStream_t st, QuantIn in = {})
+static int launch_tile(GemmArgs g, hipStream_t st, typename std::conditional<TOK, TokenIn, QuantIn>::type in = {})
 {
     constexpr int kSums = kWaves * TT * NT * kWave * 16;   // partial sums; a launch that quantises has the tokens' codes behind them
     static_assert(QX == 0 || kSums + kQuantFewBytes <= 32768, "a launch that quantises stays below the LDS limit that has to be raised");
@@ -335,6 +431,16 @@ int launch_gemm_i8_few_quant(const GemmArgs& g, const FewPlan& p, const QuantIn&
     if (p.tile == 0) return f16 ? AWEQ_FQ(1, 4, 1) : AWEQ_FQ(1, 4, 2);
     return f16 ? AWEQ_FQ(2, 3, 1) : AWEQ_FQ(2, 3, 2);
 #undef AWEQ_FQ
+}
+
+int launch_gemm_i8_few_tokens(const GemmArgs& g, const FewPlan& p, const TokenIn& in, bool f16, hipStream_t st)
+{
+#define AWEQ_FT(NT, D, Q)                                                                                              \
+    (g.T == 1 ? few::launch_tile<1, NT, D, Q, 1, true>(g, st, in)                                                      \
+              : g.T == 2 ? few::launch_tile<1, NT, D, Q, 2, true>(g, st, in) : few::launch_tile<1, NT, D, Q, 4, true>(g, st, in))
+    if (p.tile == 0) return f16 ? AWEQ_FT(1, 4, 1) : AWEQ_FT(1, 4, 3);
+    return f16 ? AWEQ_FT(2, 3, 1) : AWEQ_FT(2, 3, 3);
+#undef AWEQ_FT
 }
 
 template <bool TOK>
