@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
         __shared__ float s_lo[kWaves][TQ], s_hi[kWaves][TQ];
         const int T = (int)g.T;
         float lo[TQ], hi[TQ];
-        bool finite = true;
+        uint32_t st = 0;
 #pragma unroll
         for (int t = 0; t < TQ; ++t) lo[t] = hi[t] = 0.0f;
 #pragma unroll
@@ -168,15 +168,13 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
 #pragma unroll
             for (int t = 0; t < TQ; ++t) {
                 if (TQ > 2 && t >= T) break;
-                float xf[8];
-                widen<TokE>(traw[i][t], xf);
-                token_extremes(xf, isf, lo[t], hi[t], finite);
+                token_extremes<true, TokE>(traw[i][t], isf, lo[t], hi[t]);
             }
         }
 #pragma unroll
         for (int t = 0; t < TQ; ++t) {
-            lo[t] = wave_allreduce(lo[t], OpMin());
-            hi[t] = wave_allreduce(hi[t], OpMax());
+            lo[t] = wave_allreduce(lo[t], OpMinimum());
+            hi[t] = wave_allreduce(hi[t], OpMaximum());
             if (lane == 0) { s_lo[wave][t] = lo[t]; s_hi[wave][t] = hi[t]; }
         }
         if (threadIdx.x < kQuantTokens) s_rs[threadIdx.x] = 0;
@@ -186,10 +184,10 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
 #pragma unroll
         for (int t = 0; t < TQ; ++t) {
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) { lo[t] = fminf(lo[t], s_lo[w][t]); hi[t] = fmaxf(hi[t], s_hi[w][t]); }
+            for (int w = 0; w < kWaves; ++w) { lo[t] = OpMinimum()(lo[t], s_lo[w][t]); hi[t] = OpMaximum()(hi[t], s_hi[w][t]); }
             float step;
             int zero;
-            token_params(lo[t], hi[t], step, zero);
+            token_params(lo[t], hi[t], step, zero, st);
             ap[t] = quot_params(step, zero);
             rs[t] = 0;
             if (threadIdx.x == 0) {
@@ -208,10 +206,8 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
 #pragma unroll
             for (int t = 0; t < TQ; ++t) {
                 if (TQ > 2 && t >= T) break;
-                float xf[8];
-                widen<TokE>(traw[i][t], xf);
                 int r8 = 0;
-                uint2 c = token_unit(xf, isf, ap[t], r8);
+                uint2 c = token_unit<true, TokE>(traw[i][t], isf, ap[t], r8);
                 if (u >= units) { c = make_uint2(0u, 0u); r8 = 0; }   // (the zero fill of the last panel)
                 rs[t] += r8;
                 if (u >= padded) continue;
@@ -225,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
             rs[t] = wave_allreduce(rs[t], OpAdd());
             if (lane == 0) atomicAdd(&s_rs[t], rs[t]);
         }
-        if (blockIdx.x == 0) raise_status(g.status, finite ? 0u : (uint32_t)AWEQ_ST_NONFINITE);
+        if (blockIdx.x == 0 && threadIdx.x == 0) raise_status(g.status, st);
         __syncthreads();
         if (blockIdx.x == 0 && (int)threadIdx.x < T) in.rowsum_x[threadIdx.x] = s_rs[threadIdx.x];
     } else if constexpr (QX != 0) {

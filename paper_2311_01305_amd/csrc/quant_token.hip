@@ -1,6 +1,6 @@
 // Quantizer of Eq. 1-2 with b = 8 whose slice is a token: Step and Z from the token's own range, widened to contain 0.
 //
-// HBM-bound: 2 bytes in (binary16 / bfloat16), 1 byte out per value.  The range has to be known before the first code, so a workgroup keeps the values
+// HBM-bound: 2 bytes in (binary16 / bfloat16), 1 byte out per value, and 7 vector operations a value beside that (11 with scales).  The range has to be known before the first code, so a workgroup keeps the values
 // of its tokens in registers between the two: every value is read once.
 #include "gemm_tokens.hpp"
 #include "token_range.hpp"
@@ -24,7 +24,7 @@ struct Args {
 };
 
 // R tokens a workgroup, U units of 8 values of each a thread (unit threadIdx + 256 i)
-template <class E, int U, int R>
+template <class E, int U, int R, bool FOLD>
 __global__ __launch_bounds__(kThreads) void quant_token_kernel(Args g)
 {
     __shared__ float s_lo[kWaves][R], s_hi[kWaves][R];
@@ -46,37 +46,32 @@ __global__ __launch_bounds__(kThreads) void quant_token_kernel(Args g)
     float lo[R], hi[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) lo[r] = hi[r] = 0.0f;
-    bool finite = true;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int u = i * kThreads + (int)threadIdx.x;
         if (u >= units) break;
         float is[8];
-        load_scales(g.inv_s, u, is);
+        load_scales<FOLD>(g.inv_s, u, is);
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (r < tokens) {
-                float x[8];
-                widen<E>(raw[r][i], x);
-                token_extremes(x, is, lo[r], hi[r], finite);
-            }
+            if (r < tokens) token_extremes<FOLD, E>(raw[r][i], is, lo[r], hi[r]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        lo[r] = wave_allreduce(lo[r], OpMin());
-        hi[r] = wave_allreduce(hi[r], OpMax());
+        lo[r] = wave_allreduce(lo[r], OpMinimum());
+        hi[r] = wave_allreduce(hi[r], OpMaximum());
         if (lane == 0) { s_lo[wave][r] = lo[r]; s_hi[wave][r] = hi[r]; }
     }
     __syncthreads();
     ActParams p[R];
-    uint32_t st = finite ? 0u : (uint32_t)AWEQ_ST_NONFINITE;
+    uint32_t st = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) { lo[r] = fminf(lo[r], s_lo[w][r]); hi[r] = fmaxf(hi[r], s_hi[w][r]); }
+        for (int w = 0; w < kWaves; ++w) { lo[r] = OpMinimum()(lo[r], s_lo[w][r]); hi[r] = OpMaximum()(hi[r], s_hi[w][r]); }
         float step;
         int zero;
-        token_params(lo[r], hi[r], step, zero);
+        token_params(lo[r], hi[r], step, zero, st);
         p[r] = quot_params(step, zero);
         if (threadIdx.x == 0 && r < tokens) { g.step[t0 + r] = step; g.zero[t0 + r] = zero; }
     }
@@ -88,16 +83,12 @@ __global__ __launch_bounds__(kThreads) void quant_token_kernel(Args g)
         const int u = i * kThreads + (int)threadIdx.x;
         if (u >= padded) break;
         float is[8];
-        load_scales(u < units ? g.inv_s : nullptr, u, is);
+        load_scales<FOLD>(g.inv_s, u < units ? u : 0, is);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < tokens) {
                 uint2 c = make_uint2(0u, 0u);
-                if (u < units) {
-                    float x[8];
-                    widen<E>(raw[r][i], x);
-                    c = token_unit(x, is, p[r], sum[r]);
-                }
+                if (u < units) c = token_unit<FOLD, E>(raw[r][i], is, p[r], sum[r]);
                 *reinterpret_cast<uint2*>(g.xq + ((int64_t)(u >> 3) * g.T + t0 + r) * kPanel + (u & 7) * 8) = c;
             }
     }
@@ -113,28 +104,48 @@ __global__ __launch_bounds__(kThreads) void quant_token_kernel(Args g)
         for (int w = 0; w < kWaves; ++w) s += s_sum[w][threadIdx.x];
         g.rowsum[t0 + threadIdx.x] = s;
     }
-    raise_status(g.status, st);
+    if (threadIdx.x == 0) raise_status(g.status, st);
 }
 
-template <class E, int U, int R>
+template <class E, int U, int R, bool FOLD>
 static int launch_rows(Args g, hipStream_t st)
 {
     const int64_t blocks = cdiv(g.T, R), most = (1ll << 32) / kThreads - 1;   // fewer than 2^32 threads to a launch
     for (int64_t b = 0; b < blocks; b += most) {
         g.first = b * R;
-        quant_token_kernel<E, U, R><<<(unsigned)(blocks - b < most ? blocks - b : most), kThreads, 0, st>>>(g);
+        quant_token_kernel<E, U, R, FOLD><<<(unsigned)(blocks - b < most ? blocks - b : most), kThreads, 0, st>>>(g);
     }
     return launch_status();
+}
+
+template <class E, int U, int R>
+static int launch_units(const Args& g, hipStream_t st)
+{
+    return g.inv_s ? launch_rows<E, U, R, true>(g, st) : launch_rows<E, U, R, false>(g, st);
+}
+
+// Two tokens a workgroup from 1024 on: a panel's rows of two tokens are a whole line, and the scales are read once for both (us, one token -> two, four:
+// 1777 x 11008 with scales 23.4 -> 18.3, 20.2; 8192 x 4096 30.1 -> 21.7, 24.9; 8192 x 8192 55.7 -> 42.3 (4.8 TB/s), 43.3; 8192 x 22016 130 -> 122, 127; but
+// 256 x 4096 4.1 -> 4.5, 29 x 8192 4.6 -> 5.6).  Values of binary32 take twice the registers: one token in the longest rows.
+template <class E, int U>
+static int launch_tokens(const Args& g, hipStream_t st)
+{
+    if constexpr (U * sizeof(E) <= 32) {
+        if (g.T >= 1024) return launch_units<E, U, 2>(g, st);
+    }
+    return launch_units<E, U, 1>(g, st);
 }
 
 template <class E>
 static int launch(const Args& g, hipStream_t st)
 {
     const int64_t units = panel_count(g.K) * (kPanel / 8);
-    if (units <= 2 * kThreads) return launch_rows<E, 2, 1>(g, st);
-    if (units <= 4 * kThreads) return launch_rows<E, 4, 1>(g, st);
-    if (units <= 8 * kThreads) return launch_rows<E, 8, 1>(g, st);
-    return launch_rows<E, 16, 1>(g, st);
+    if (units <= 2 * kThreads) return launch_tokens<E, 2>(g, st);
+    if (units <= 4 * kThreads) return launch_tokens<E, 4>(g, st);
+    if (units <= 6 * kThreads) return launch_tokens<E, 6>(g, st);
+    if (units <= 8 * kThreads) return launch_tokens<E, 8>(g, st);
+    if (units <= 11 * kThreads) return launch_tokens<E, 11>(g, st);
+    return launch_tokens<E, 16>(g, st);
 }
 
 }  // namespace tok

@@ -40,6 +40,28 @@ __device__ __forceinline__ void store_unit(E* p, const float x[8])
     }
 }
 
+// The same past the caches (16-bit types): for calls whose data does not fit them anyway
+template <class E>
+__device__ __forceinline__ Unit<E> stream_unit(const E* p)
+{
+    typedef int v4 __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(E) == 4) return load_unit(p);
+    else return __builtin_bit_cast(Unit<E>, __builtin_nontemporal_load(reinterpret_cast<const v4*>(p)));
+}
+template <class E>
+__device__ __forceinline__ void stream_unit(E* p, const float x[8])
+{
+    typedef int v4 __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(E) == 4) {
+        store_unit(p, x);
+    } else {
+        Unit<E> u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = (E)x[i];
+        __builtin_nontemporal_store(__builtin_bit_cast(v4, u), reinterpret_cast<v4*>(p));
+    }
+}
+
 template <class E>
 __device__ __forceinline__ void widen(const Unit<E>& u, float x[8])
 {
