@@ -142,8 +142,7 @@ struct Shape {
     // tall: K, V, and (codes) for each group of 16 keys 16 steps of K, 16 of V (and 32 unused)
     static constexpr int kHalf = kTallKeys * kRow;
     static constexpr int kSlot = 2 * kHalf + (kCodes ? kTallKeys / 16 * 256 : 0);
-    static constexpr int kStages = 2;
-    static constexpr int kTallLds = kStages * kSlot;
+    static constexpr int kTallLds = 2 * kSlot;
     // wide: V of a tile and (codes) its steps for each wavefront; at the end their O, maximum and sum
     static constexpr int kWideV = kWideKeys * kRow;
     static constexpr int kWideSlot = kWideV + (kCodes ? 2 * kWideKeys * 4 : 0);
@@ -235,6 +234,19 @@ struct Rows {
         }
     }
 
+    // The queries have arrived: said before the loop over the keys, whose waits would be for them and, with them, for the keys in flight
+    __device__ __forceinline__ void arrived()
+    {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk) {
+                i32x4 w = __builtin_bit_cast(i32x4, q[i][kk]);
+                asm volatile("" : "+v"(w));
+                q[i][kk] = __builtin_bit_cast(V, w);
+            }
+    }
+
     // Scores s[i][n] of 16 keys each to probabilities for the second product; key0: the tile's first key, end: the range's, own: of the sequence.
     // ks, vs: (codes) the steps of this lane's keys.
     template <int N>
@@ -260,10 +272,11 @@ struct Rows {
                     for (int v = 0; v < 4; ++v) s[i][n][v] = __builtin_fmaf(s[i][n][v], ks[n][v] * scale[i], lv[n][v]);
             }
             if (__builtin_amdgcn_ballot_w64(key0 + 16 * N > lim) != 0) {
+                const int mine = lim - key0 - grp * 4;
 #pragma unroll
                 for (int n = 0; n < N; ++n)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) s[i][n][v] = key0 + n * 16 + grp * 4 + v < lim ? s[i][n][v] : -INFINITY;
+                    for (int v = 0; v < 4; ++v) s[i][n][v] = n * 16 + v < mine ? s[i][n][v] : -INFINITY;
             }
             float t = -INFINITY;
 #pragma unroll
@@ -301,27 +314,36 @@ struct Rows {
         }
     }
 
-    // O^T += V^T P^T for keys 32 u .. 32 u + 31 of the tile at vt
-    __device__ __forceinline__ void values(const char* vt, int u, const V (&p)[MT])
+    // Where a lane's transposing reads of V begin, for 16 values at d: keys 4 grp .. of the first 16 (codes: and of the second) of a tile
+    static __device__ __forceinline__ int value_offset(int d)
     {
         constexpr int C = Shape<E, D>::kChunks, kRow = Shape<E, D>::kRow;
         const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+        if constexpr (kCodes) {
+            const int r = col >> 1, row = 16 * (r >> 2) + 4 * grp + (r & 3);
+            return row * kRow + ((d ^ swz_v<C, true>(row)) * 16) + (col & 1) * 8;
+        } else {
+            const int row = 4 * grp + (col >> 2);
+            return row * kRow + (((2 * d + ((col & 3) >> 1)) ^ swz_v<C, false>(row)) * 16) + (col & 1) * 8;
+        }
+    }
+
+    // O^T += V^T P^T for keys 32 u .. 32 u + 31 of the tile at vt (the swizzles repeat every 16 rows, the codes' every 32)
+    __device__ __forceinline__ void values(const char* vt, int u, const V (&p)[MT], const int (&at)[D / 16])
+    {
+        constexpr int kRow = Shape<E, D>::kRow;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
             V vf;
+            const char* const from = vt + at[d] + u * 32 * kRow;
             if constexpr (kCodes) {
-                const int r = col >> 1, row = u * 32 + 16 * (r >> 2) + 4 * grp + (r & 3);
-                const char* const at = vt + row * kRow + ((d ^ swz_v<C, true>(row)) * 16) + (col & 1) * 8;
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)at);
+                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)from);
                 vf = codes_to_f16(w[0], w[1]);
             } else {
                 union { s16x4 h[2]; V v; } f;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int row = u * 32 + half * 16 + 4 * grp + (col >> 2);
-                    const char* const at = vt + row * kRow + (((2 * d + ((col & 3) >> 1)) ^ swz_v<C, false>(row)) * 16) + (col & 1) * 8;
-                    f.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
-                }
+                for (int half = 0; half < 2; ++half)
+                    f.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from + half * 16 * kRow));
                 vf = f.v;
             }
 #pragma unroll
@@ -377,39 +399,52 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
         return scalar_at(tile < np ? g.prefix_table : j.table, key >> g.page_shift);
     };
     int next_page = tiles > 0 ? page_of(0) : 0;
-    auto fetch = [&](int tile) {
+    // this lane's 16 bytes of the load instructions of K and V, from the first of the 16 rows
+    auto fetch_offset = [&](int q, bool v, int last) {
+        const int sub = q * SH::kRowsPerLoad + lane / C, trow = wave * 16 + sub;    // row of the 16, of the tile (the swizzle's)
+        return (uint32_t)(min(sub, last) * kRow + ((lane % C) ^ (v ? swz_v<C, kCodes>(trow) : swz_k<C>(trow))) * 16);
+    };
+    constexpr bool kKept = D < 256;   // (no registers left for them with longer heads)
+    uint32_t from_k[SH::kLoads], from_v[SH::kLoads];
+#pragma unroll
+    for (int q = 0; q < SH::kLoads; ++q) { from_k[q] = fetch_offset(q, false, 15); from_v[q] = fetch_offset(q, true, 15); }
+    auto fetch = [&](int tile, uint32_t slot) {
         int page = next_page;
         if (tile + 1 < tiles) next_page = page_of(tile + 1);
         if ((unsigned)page >= (unsigned)g.pages) { est |= AWEQ_ST_INDEX; page = 0; }
-        const int key0 = first_key(tile) + wave * 16, end = tile < np ? j.pb : j.ob;    // a multiple of 16: the group lies in one page
-        const uint32_t slot = lds0 + (uint32_t)(tile % SH::kStages) * SH::kSlot;
-        const int64_t head_row = ((int64_t)page * g.Hk + j.kvh) << g.page_shift;        // row of the cache where this head's page begins
-        const char* const kb = reinterpret_cast<const char*>(g.k_cache) + head_row * kRow;
-        const char* const vb = reinterpret_cast<const char*>(g.v_cache) + head_row * kRow;
-        const int in_page = g.page_size - 1;
+        // the group's first key, a multiple of 16, so that it lies in one page; past the end the last group that has a key
+        const int end = tile < np ? j.pb : j.ob, key0 = min(first_key(tile) + wave * 16, (end - 1) & ~15), last = end - 1 - key0;
+        const int64_t row0 = (((int64_t)page * g.Hk + j.kvh) << g.page_shift) + (key0 & (g.page_size - 1));   // its row of the cache
+        const char* const kb = reinterpret_cast<const char*>(g.k_cache) + row0 * kRow;
+        const char* const vb = reinterpret_cast<const char*>(g.v_cache) + row0 * kRow;
+        const uint32_t to = lds0 + slot + (uint32_t)(wave * 16 * kRow);
+        if (kKept && last >= 15) {
 #pragma unroll
-        for (int q = 0; q < SH::kLoads; ++q) {
-            const int sub = q * SH::kRowsPerLoad + lane / C, trow = wave * 16 + sub;    // row of the 16, of the tile (the swizzle's)
-            const int row = min(key0 + sub, end - 1) & in_page;
-            const uint32_t at = slot + (uint32_t)(wave * 16 * kRow + q * 1024);
-            dma16(kb, (uint32_t)(row * kRow + ((lane % C) ^ swz_k<C>(trow)) * 16), at);
-            dma16(vb, (uint32_t)(row * kRow + ((lane % C) ^ swz_v<C, kCodes>(trow)) * 16), at + SH::kHalf);
+            for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, from_k[q], to + q * 1024); dma16(vb, from_v[q], to + q * 1024 + SH::kHalf); }
+        } else {
+#pragma unroll
+            for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, fetch_offset(q, false, last), to + q * 1024); dma16(vb, fetch_offset(q, true, last), to + q * 1024 + SH::kHalf); }
         }
-        if constexpr (kCodes) {
-            const int row = min(key0 + col, end - 1) & in_page;
-            dma4((grp & 1 ? g.v_step : g.k_step) + head_row + row, slot + 2 * SH::kHalf + (uint32_t)wave * 256);
-        }
+        if constexpr (kCodes) dma4((grp & 1 ? g.v_step : g.k_step) + row0 + min(col, last), lds0 + slot + 2 * SH::kHalf + (uint32_t)wave * 256);
     };
 
-    if (tiles > 0) fetch(0);
     R rows;
     rows.load(g, j, row0);
-    for (int tile = 0; tile < tiles; ++tile) {
+    if (tiles > 0) fetch(0, 0);
+    constexpr int kSteps = kCodes ? D / 64 : D / 32;
+    int at_k[kSteps], at_v[D / 16];
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) at_k[kk] = col * kRow + (((kk * 4 + grp) ^ swz_k<C>(col)) * 16);   // (repeats every 16 rows)
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) at_v[d] = R::value_offset(d);
+    rows.arrived();
+    auto step = [&](int tile, auto slot_c) {
+        constexpr int slot = decltype(slot_c)::value * SH::kSlot;
         wait_vm<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();     // the tile has landed for everyone, and everyone is done with the one before
-        if (tile + 1 < tiles) fetch(tile + 1);
-        const char* const kt = lds + (tile % SH::kStages) * SH::kSlot;
+        if (tile + 1 < tiles) fetch(tile + 1, SH::kSlot - slot);
+        const char* const kt = lds + slot;
         const char* const vt = kt + SH::kHalf;
 
         f32x4 s[MT][N];
@@ -417,23 +452,18 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
         for (int n = 0; n < N; ++n) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) s[i][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const int row = n * 16 + col;
-            if constexpr (kCodes) {
 #pragma unroll
-                for (int kk = 0; kk < D / 64; ++kk) {
-                    const i32x4 w = *reinterpret_cast<const i32x4*>(kt + row * kRow + (((kk * 4 + grp) ^ swz_k<C>(row)) * 16));
+            for (int kk = 0; kk < kSteps; ++kk) {
+                const i32x4 w = *reinterpret_cast<const i32x4*>(kt + at_k[kk] + n * 16 * kRow);
+                if constexpr (kCodes) {
                     const V a = codes_to_f16(w[0], w[1]), b = codes_to_f16(w[2], w[3]);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(a, rows.q[i][2 * kk], s[i][n]);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(b, rows.q[i][2 * kk + 1], s[i][n]);
-                }
-            } else {
+                } else {
 #pragma unroll
-                for (int kk = 0; kk < D / 32; ++kk) {
-                    const V kf = *reinterpret_cast<const V*>(kt + row * kRow + (((kk * 4 + grp) ^ swz_k<C>(row)) * 16));
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(kf, rows.q[i][kk], s[i][n]);
+                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(__builtin_bit_cast(V, w), rows.q[i][kk], s[i][n]);
                 }
             }
         }
@@ -454,8 +484,12 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
             V pu[MT];
 #pragma unroll
             for (int i = 0; i < MT; ++i) pu[i] = p[i][u];
-            rows.values(vt, u, pu);
+            rows.values(vt, u, pu, at_v);
         }
+    };
+    for (int tile = 0; tile < tiles; tile += 2) {
+        step(tile, std::integral_constant<int, 0>{});
+        if (tile + 1 < tiles) step(tile + 1, std::integral_constant<int, 1>{});
     }
     if (est && lane == 0) raise_status(g.status, est);
 #pragma unroll
@@ -523,13 +557,17 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
             }
         }
     };
+    R rows;
+    if (tiles > 0) pages_of(0);
+    rows.load(g, j, j.row0);
     if (tiles > 0) {
-        pages_of(0);
         request(0);
         if (tiles > 1) pages_of(1);
     }
-    R rows;
-    rows.load(g, j, j.row0);
+    int at_v[D / 16];
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) at_v[d] = R::value_offset(d);
+    rows.arrived();
     for (int tile = 0; tile < tiles; ++tile) {
         f32x4 s[1][N];
 #pragma unroll
@@ -575,7 +613,7 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
 #pragma unroll
         for (int u = 0; u < N / 2; ++u) {
             const V pu[1] = {p[0][u]};
-            rows.values(vt, u, pu);
+            rows.values(vt, u, pu, at_v);
         }
     }
     if (est && lane == 0) raise_status(g.status, est);
@@ -625,7 +663,7 @@ __global__ __launch_bounds__(kThreads, waves_wanted(D, MT)) void attention_kerne
     const int tile_rows = w.tall ? kWaves * 16 * MT : kWideRows;
     Job j;
     j.kvh = combo % g.Hk;
-    j.row0 = seq % w.row_tiles * tile_rows;
+    j.row0 = (w.row_tiles - 1 - seq % w.row_tiles) * tile_rows;   // (a prompt's last rows, which see most keys, first)
     j.part = w.first_part + split;
     j.pa = j.pb = j.oa = j.ob = 0;
     j.sees0 = 0;
