@@ -716,40 +716,66 @@ __global__ __launch_bounds__(kThreads, waves_wanted(D, MT)) void attention_kerne
     }
 }
 
-// A row's parts joined, a wavefront each: lane p has the maximum and sum of part p, the values are read D / 4 lanes to a part
-template <int D>
+constexpr int kJoinParts = 256;
+
+// A row's parts joined by W wavefronts: a lane has the maximum and sum of the parts lane, lane + 64, .., wavefront v takes the values of the parts 64 c + W i
+// + v, D / 4 lanes to a part, kFlight of them in flight
+template <int D, int W>
 __global__ __launch_bounds__(256) void join_kernel(Args g)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave, all_rows = g.T * g.Hq;
-    if (row >= all_rows) return;
-    const int lane = threadIdx.x & (kWave - 1);
-    constexpr int kLanes = D / 4, kAtOnce = kWave / kLanes;
+    constexpr int kRowsOf = 4 / W;   // rows of a workgroup
+    __shared__ f32x4 s_part[W > 1 ? W : 1][W > 1 ? D / 4 : 1];
+    const int wave = threadIdx.x / kWave, slice = wave % W, lane = threadIdx.x & (kWave - 1);
+    const int64_t row = (int64_t)blockIdx.x * kRowsOf + wave / W, all_rows = g.T * g.Hq;
+    if (row >= all_rows) return;     // (W > 1: all of the workgroup or nobody)
+    constexpr int kLanes = D / 4, kAtOnce = kWave / kLanes, kOf = W > 1 ? kJoinParts / kWave : 1, kFlight = 8;
     const int sub = lane / kLanes, at = lane % kLanes * 4;
-    float2 ml = make_float2(-INFINITY, 0.0f);
-    if (lane < g.parts) ml = g.part_ml[lane * all_rows + row];
-    const float mm = wave_allreduce(ml.x, Larger());
-    const float w = ml.y > 0.0f ? __builtin_amdgcn_exp2f(ml.x - mm) : 0.0f;
-    const float ll = wave_allreduce(w * ml.y, OpAdd());
+    float2 ml[kOf];
+    float mm = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < kOf; ++c) {
+        ml[c] = make_float2(-INFINITY, 0.0f);
+        if (c * kWave + lane < g.parts) ml[c] = g.part_ml[(int64_t)(c * kWave + lane) * all_rows + row];
+        mm = fmaxf(mm, ml[c].x);
+    }
+    mm = wave_allreduce(mm, Larger());
+    float w[kOf], ll = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kOf; ++c) {
+        w[c] = ml[c].y > 0.0f ? __builtin_amdgcn_exp2f(ml[c].x - mm) : 0.0f;
+        ll += w[c] * ml[c].y;
+    }
+    ll = wave_allreduce(ll, OpAdd());
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kFlight = 4;
-    for (int p0 = 0; p0 < g.parts; p0 += kAtOnce * kFlight) {
-        f32x4 x[kFlight];
-        float a[kFlight];
 #pragma unroll
-        for (int f = 0; f < kFlight; ++f) {
-            const int p = p0 + f * kAtOnce + sub;
-            a[f] = __shfl(w, p & (kWave - 1));
-            if (p >= g.parts) a[f] = 0.0f;
-            x[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (a[f] != 0.0f) x[f] = *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)p * all_rows + row) * D + at);
+    for (int c = 0; c < kOf; ++c) {
+        const int n = min(g.parts - c * kWave, kWave);
+        for (int p0 = slice * kAtOnce; p0 < n; p0 += W * kAtOnce * kFlight) {
+            f32x4 x[kFlight];
+            float a[kFlight];
+#pragma unroll
+            for (int f = 0; f < kFlight; ++f) {
+                const int p = p0 + f * W * kAtOnce + sub;
+                a[f] = __shfl(w[c], p & (kWave - 1));
+                if (p >= n) a[f] = 0.0f;
+                x[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (a[f] != 0.0f) x[f] = *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)(c * kWave + p) * all_rows + row) * D + at);
+            }
+#pragma unroll
+            for (int f = 0; f < kFlight; ++f) v += a[f] * x[f];
         }
-#pragma unroll
-        for (int f = 0; f < kFlight; ++f) v += a[f] * x[f];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if constexpr (kAtOnce > 2) v[e] += __shfl_xor(v[e], 16);
         if constexpr (kAtOnce > 1) v[e] += __shfl_xor(v[e], 32);
+    }
+    if constexpr (W > 1) {
+        if (sub == 0) s_part[slice][at / 4] = v;
+        __syncthreads();
+        if (slice != 0) return;
+#pragma unroll
+        for (int o = 1; o < W; ++o) v += s_part[o][at / 4];
     }
     const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
     if (sub == 0) {
@@ -772,14 +798,35 @@ struct Plan {
     int parts() const { return shared.splits + own.splits; }
 };
 
-constexpr int kMostSplits = 32;   // (64 parts at most: a lane each where they are joined)
+constexpr int kMostSplits = 128;
+static_assert(2 * kMostSplits <= kJoinParts, "the join has room for them");
 
 // ranges of `len` keys so that `items` of them each make up about `want` workgroups, of `least` keys or more
-static int split_count(int64_t items, int64_t len, int64_t want, int64_t least)
+static int64_t split_count(int64_t items, int64_t len, int64_t want, int64_t least)
 {
     const int64_t n = cdiv(want, items), most = cdiv(len, least);
     const int64_t k = n < most ? n : most;
-    return (int)(k < 1 ? 1 : k > kMostSplits ? kMostSplits : k);
+    return k < 1 ? 1 : k > kMostSplits ? kMostSplits : k;
+}
+// Tall workgroups: one for each compute unit, of 512 keys or more, or two, which overlap one's products with the other's exponentials, where that leaves
+// 1024 keys: a range's rows are written and read once more to be joined (us, one -> two: 1024 rows a key head against 16384 keys 95 -> 82, but 256 rows
+// against 8192 23.1 -> 25.1, and with the batch's own keys in the same launch 38.2 -> 47.1).  Ranges of 256 keys where most compute units had none.
+static int64_t tall_splits(int64_t items, int64_t len)
+{
+    const int64_t one = split_count(items, len, 256, 512), two = split_count(items, len, 512, 1024);
+    if (items * one < 64) return split_count(items, len, 256, 256);
+    return one > two ? one : two;
+}
+// Wide workgroups: eight for each compute unit (sequences differ in length; two for a single range), of 512 keys or more, or of less where most compute units had none (us, 256 ->
+// 512: 64 sequences of up to 500 keys 20.4 -> 15.0, 128 of up to 400 40.4 -> 31.5, 8 of up to 4000 28.6 -> 25.3; but one of 1900 with 32 key heads 12.0 -> 13.0)
+static int64_t wide_splits(int64_t items, int64_t len, bool one)
+{
+    int64_t n = 1;
+    for (int64_t least = 512; least >= 128; least /= 2) {
+        n = split_count(items, len, one ? 512 : 2048, least);
+        if (items * n >= 256) break;
+    }
+    return n;
 }
 static void set_work(Work& w, int64_t rows, int mt, int64_t splits, int64_t len, int64_t items)
 {
@@ -805,13 +852,14 @@ static Plan plan(int64_t T, int64_t Hq, int64_t Hk, int64_t B, int64_t max_q, in
     if (has_shared) {
         p.shared.tall = shared_tall;
         const int64_t tile = shared_tall ? kWaves * 16 * p.mt : kWideRows;
-        set_work(p.shared, all_rows, p.mt, split_count(Hk * cdiv(all_rows, tile), prefix_len, 256, 512), prefix_len, Hk);
+        const int64_t items = Hk * cdiv(all_rows, tile);
+        set_work(p.shared, all_rows, p.mt, shared_tall ? tall_splits(items, prefix_len) : wide_splits(items, prefix_len, true), prefix_len, Hk);
     }
     if (has_own) {
         p.own.tall = own_tall;
         const int64_t tile = own_tall ? kWaves * 16 * p.mt : kWideRows, items = B * Hk * cdiv(most_rows, tile);
         const int64_t keys = max_len + (p.fused ? prefix_len : 0);
-        set_work(p.own, most_rows, p.mt, split_count(items, keys, own_tall ? 512 : 2048, 256), keys, B * Hk);
+        set_work(p.own, most_rows, p.mt, own_tall ? tall_splits(items, keys) : wide_splits(items, keys, B == 1), keys, B * Hk);
         if (own_tall) p.own.chunk = 0;
     }
     return p;
@@ -842,7 +890,12 @@ static int launch(Args& g, const Plan& p, hipStream_t st)
         w->blocks = (int)n;
     }
     const int rc = p.mt == 0 ? launch_one<E, D, 0>(g, blocks, st) : p.mt == 1 ? launch_one<E, D, 1>(g, blocks, st) : launch_one<E, D, 2>(g, blocks, st);
-    if (rc == AWEQ_OK && g.parts > 1) join_kernel<D><<<(unsigned)cdiv(g.T * g.Hq, 4), 256, 0, st>>>(g);
+    if (rc == AWEQ_OK && g.parts > 1) {
+        const int64_t rows = g.T * g.Hq;
+        // (up to 64 parts a wavefront is as fast as four or faster: 2048 rows of 18 parts 35.1 us with the attention, four each 44.7)
+        if (g.parts > kWave) join_kernel<D, 4><<<(unsigned)rows, 256, 0, st>>>(g);
+        else join_kernel<D, 1><<<(unsigned)cdiv(rows, 4), 256, 0, st>>>(g);
+    }
     return rc != AWEQ_OK ? rc : launch_status();
 }
 
@@ -858,7 +911,7 @@ static bool shapes_ok(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, i
 {
     if (T <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (D != 64 && D != 128 && D != 256) || B <= 0 || max_q <= 0) return false;
     if (prefix_len < 0 || max_len < 0 || prefix_len > (1 << 29) || max_len > (1 << 29)) return false;
-    return T <= (1 << 24) && B <= (1 << 20) && Hq <= (1 << 16) && T * Hq <= (1 << 25) && B * Hk <= (1 << 24);
+    return T <= (1 << 24) && B <= (1 << 20) && Hq <= (1 << 16) && T * Hq < (1 << 24) && B * Hk <= (1 << 24);
 }
 
 }  // namespace attn

@@ -433,8 +433,10 @@ int launch_gemm_i8_few_tokens(const GemmArgs& g, const FewPlan& p, const TokenIn
 {
 #define AWEQ_FT(NT, D, Q)                                                                                              \
     (g.T == 1 ? few::launch_tile<1, NT, D, Q, 1, true>(g, st, in)                                                      \
-              : g.T == 2 ? few::launch_tile<1, NT, D, Q, 2, true>(g, st, in) : few::launch_tile<1, NT, D, Q, 4, true>(g, st, in))
-    if (p.tile == 0) return f16 ? AWEQ_FT(1, 4, 1) : AWEQ_FT(1, 4, 3);
+              : g.T == 2 ? few::launch_tile<1, NT, D, Q, 2, true>(g, st, in) : few::launch_tile<1, NT, NT == 2 ? 2 : D, Q, 4, true>(g, st, in))
+    // (us, depth 4 -> 3 of 16 channels: one token 4096 x 4096 7.0 -> 6.75, 4096 x 16384 16.5 -> 15.9, four tokens 4096 x 4096 9.9 -> 9.6; of 32 channels
+    // with registers for three or four tokens too, 3 -> 2: four tokens 11008 x 4096 18.8 -> 13.0, but one token 9.96 -> 10.2)
+    if (p.tile == 0) return f16 ? AWEQ_FT(1, 3, 1) : AWEQ_FT(1, 3, 3);
     return f16 ? AWEQ_FT(2, 3, 1) : AWEQ_FT(2, 3, 3);
 #undef AWEQ_FT
 }
