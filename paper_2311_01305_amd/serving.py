@@ -1,0 +1,186 @@
+"""The attention block of a served decoder on the quantised layers that the calibration leaves: the projections as int8 products whose tokens
+are quantised on the way, norm and rotation of the heads on the way into a paged cache, attention over the sequences' own pages and a prefix
+that all of them share.  Four calls of the library for a step of any tokens, one of each sequence or whole prompts:
+
+    aweq_w8a8_gemm_tokens (q, k, v)  ->  aweq_kv_append  ->  aweq_prefix_attention  ->  aweq_w8a8_gemm_tokens (output)
+
+`python -m paper_2311_01305_amd.serving` calibrates a block's projections on synthetic activations, runs a shared prompt once and decodes a batch
+behind it.  No arithmetic of the operators happens here.
+"""
+import argparse
+import time
+from dataclasses import dataclass
+from typing import List, Optional
+
+import torch
+
+from . import binding as B
+from . import pipeline
+
+DTYPES = {torch.float16: B.AWEQ_F16, torch.bfloat16: B.AWEQ_BF16}
+
+
+@dataclass
+class QuantLinear:
+    """An 8-bit layer as pipeline.calibrate_layer leaves it.  inv_s: the equalization's 1 / s, or None where what produces the input has it folded in."""
+    N: int
+    K: int
+    codes: torch.Tensor
+    step_w: torch.Tensor
+    zero_w: torch.Tensor
+    rowsum_w: torch.Tensor
+    bias: Optional[torch.Tensor] = None
+    inv_s: Optional[torch.Tensor] = None
+    w_group: int = 0
+
+    @classmethod
+    def from_layer(cls, buf: pipeline.LayerBuffers, fold: bool = True):
+        t = buf.t
+        if buf.bits != 8 or buf.group > 0:
+            raise ValueError("8-bit weights with a scale for each output channel or the tensor")
+        return cls(buf.N, buf.K, t["codes"], t["step_w"], t["zero_w"], t["rowsum_w"], t["bias_out"], t["inv_s"] if fold else None, buf.group)
+
+
+class PagedCache:
+    """Pages of keys and values of one layer and which of them are free.  codes: 8-bit, with a step for each token and head."""
+
+    def __init__(self, pages: int, page_size: int, heads: int, head_dim: int, dtype=torch.float16, codes: bool = False, device="cuda:0"):
+        self.pages, self.page_size, self.heads, self.head_dim, self.dtype = pages, page_size, heads, head_dim, dtype
+        self.kind = B.AWEQ_I8 if codes else DTYPES[dtype]
+        new = lambda *shape, dtype: torch.empty(shape, dtype=dtype, device=device)
+        self.k, self.v = (new(pages, heads, page_size, head_dim, dtype=torch.int8 if codes else dtype) for _ in range(2))
+        self.k_step, self.v_step = (new(pages, heads, page_size, dtype=torch.float32) for _ in range(2)) if codes else (None, None)
+        self.free = list(range(pages - 1, -1, -1))
+
+    def take(self, tokens: int) -> List[int]:
+        """Pages for that many tokens."""
+        n = -(-tokens // self.page_size)
+        if n > len(self.free):
+            raise RuntimeError(f"{n} pages wanted, {len(self.free)} free")
+        return [self.free.pop() for _ in range(n)]
+
+    def give_back(self, pages: List[int]):
+        self.free.extend(pages)
+
+    def slots(self, pages: List[int], first: int, count: int) -> List[int]:
+        """Where the tokens first .. first + count - 1 of a sequence with these pages go."""
+        s = self.page_size
+        return [pages[i // s] * s + i % s for i in range(first, first + count)]
+
+
+class AttentionBlock:
+    """qkv [(Hq + 2 Hk) D x hidden] and out [hidden x Hq D]; buffers for max_tokens tokens of a step, allocated once."""
+
+    def __init__(self, qkv: QuantLinear, out: QuantLinear, q_heads: int, cache: PagedCache, freq: Optional[torch.Tensor], rot: int, max_tokens: int,
+                 interleaved: bool = False, gain: float = 1.0, q_norm=None, k_norm=None, eps: float = 1e-6, device="cuda:0"):
+        D, Hk = cache.head_dim, cache.heads
+        if qkv.N != (q_heads + 2 * Hk) * D or out.K != q_heads * D:
+            raise ValueError("the projections' sizes are not those of the heads")
+        self.qkv_layer, self.out_layer, self.q_heads, self.cache = qkv, out, q_heads, cache
+        self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm, self.eps = freq, rot, interleaved, gain, q_norm, k_norm, eps
+        self.max_tokens, self.device = max_tokens, device
+        new = lambda *shape, dtype: torch.empty(shape, dtype=dtype, device=device)
+        self.xq = new(max(B.aweq_panel_bytes(max_tokens, qkv.K), B.aweq_panel_bytes(max_tokens, out.K)), dtype=torch.int8)
+        self.step, self.zero, self.rowsum = new(max_tokens, dtype=torch.float32), new(max_tokens, dtype=torch.int32), new(max_tokens, dtype=torch.int32)
+        self.qkv = new(max_tokens, qkv.N, dtype=cache.dtype)
+        self.q = new(max_tokens, q_heads * D, dtype=cache.dtype)
+        self.attended = new(max_tokens, q_heads * D, dtype=cache.dtype)
+        self.y = new(max_tokens, out.N, dtype=cache.dtype)
+        self.ws = new(16, dtype=torch.uint8)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def reserve(self, tokens, batch, max_q, prefix_len, max_len):
+        """Scratch memory for steps of these bounds, so that none is allocated later (a captured graph keeps its address)."""
+        need = B.aweq_prefix_attention_ws(tokens, self.q_heads, self.cache.heads, self.cache.head_dim, batch, max_q, prefix_len, max_len)
+        if need > self.ws.numel():
+            self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def _product(self, layer, x, out):
+        T, dt = x.shape[0], DTYPES[x.dtype]
+        B.aweq_w8a8_gemm_tokens(x, dt, T, layer.K, x.stride(0), layer.inv_s, self.xq, self.step, self.zero, self.rowsum, layer.codes, layer.N,
+                                layer.step_w, layer.zero_w, layer.w_group, layer.rowsum_w, layer.bias, out, dt, layer.N, self.status)
+
+    def __call__(self, x, pos, slot, lens, table, q_start, max_len, max_q, prefix_table=None, prefix_len=0):
+        """x [T, hidden]: the step's tokens, sequence after sequence (q_start [B + 1], None: one each); pos [T] int32, slot [T] int64; lens [B]: the
+        sequences' own keys with these tokens; table [B, ..]: their pages.  Returns [T, hidden], a buffer of the block's."""
+        T, c = x.shape[0], self.cache
+        if T > self.max_tokens or x.dtype != c.dtype:
+            raise ValueError("more tokens than max_tokens, or another type than the cache's")
+        dt = DTYPES[x.dtype]
+        Hq, Hk, D = self.q_heads, c.heads, c.head_dim
+        width = self.qkv_layer.N
+        self._product(self.qkv_layer, x, self.qkv)
+        q, k, v = self.qkv[:T].split([Hq * D, Hk * D, Hk * D], 1)
+        B.aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, width, width, width, pos, self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm,
+                         self.eps, self.q, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, slot, self.status)
+        batch = lens.shape[0]
+        self.reserve(T, batch, max_q, prefix_len, max_len)
+        B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
+                                table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
+        self._product(self.out_layer, self.attended[:T], self.y)
+        return self.y[:T]
+
+
+def frequencies(rot: int, base: float = 10000.0, kind: int = B.ROPE_PLAIN, device="cuda:0", **scaling) -> Optional[torch.Tensor]:
+    """The rotation's frequencies on the device; kind and scaling (factor, trained, low, high) as in aweq_rope_frequencies."""
+    if rot == 0:
+        return None
+    host = torch.empty(rot // 2, dtype=torch.float64)
+    B.aweq_rope_frequencies(rot, base, host, kind, **scaling)
+    return host.to(device)
+
+
+def calibrated(N, K, seed, tokens=512, dtype=torch.float16, device="cuda:0") -> QuantLinear:
+    """A random layer calibrated on random activations with loud channels."""
+    g = torch.Generator(device=device)
+    g.manual_seed(seed)
+    x = torch.randn(tokens, K, generator=g, device=device)
+    x[:, torch.randint(0, K, (max(1, K // 1000),), generator=g, device=device)] *= 50.0
+    w = torch.randn(N, K, generator=g, device=device) * K ** -0.5
+    buf = pipeline.LayerBuffers(tokens, K, N, torch.float16, want_out_i32=False, device=device)
+    pipeline.calibrate_layer(x.half(), w.half(), None, buf, forward=False)
+    layer = QuantLinear.from_layer(buf)
+    layer.bias = None
+    return layer
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--hidden", type=int, default=4096)
+    ap.add_argument("--heads", type=int, default=32)
+    ap.add_argument("--key-heads", type=int, default=32)
+    ap.add_argument("--prefix", type=int, default=2048, help="tokens of the prompt that all sequences share")
+    ap.add_argument("--batch", type=int, default=32)
+    ap.add_argument("--steps", type=int, default=32)
+    ap.add_argument("--codes", action="store_true", help="8-bit cache")
+    a = ap.parse_args(argv)
+    dev, D = "cuda:0", 128
+    width = (a.heads + 2 * a.key_heads) * D
+    per = -(-a.steps // 64) + 1
+    cache = PagedCache(-(-a.prefix // 64) + a.batch * per, 64, a.key_heads, D, codes=a.codes, device=dev)
+    block = AttentionBlock(calibrated(width, a.hidden, 1), calibrated(a.hidden, a.heads * D, 2), a.heads, cache, frequencies(D, device=dev), D,
+                           max(a.prefix, a.batch), device=dev)
+    ints = lambda v, dtype=torch.int32: torch.tensor(v, dtype=dtype, device=dev)
+    # the prompt once, as one sequence of its own
+    pages = cache.take(a.prefix)
+    x = torch.randn(a.prefix, a.hidden, device=dev).half()
+    block(x, torch.arange(a.prefix, dtype=torch.int32, device=dev), ints(cache.slots(pages, 0, a.prefix), torch.int64), ints([a.prefix]), ints([pages]),
+          ints([0, a.prefix]), a.prefix, a.prefix)
+    # then the batch behind it, a token each
+    own = [cache.take(a.steps) for _ in range(a.batch)]
+    table, shared = ints(own), ints(pages)
+    plan = [(ints([a.prefix + i] * a.batch), ints([cache.slots(p, i, 1)[0] for p in own], torch.int64), ints([i + 1] * a.batch)) for i in range(a.steps)]
+    x = torch.randn(a.batch, a.hidden, device=dev).half()
+    block.reserve(a.batch, a.batch, 1, a.prefix, a.steps)
+    torch.cuda.synchronize()
+    began = time.perf_counter()
+    for pos, slot, lens in plan:
+        x = block(x, pos, slot, lens, table, None, a.steps, 1, shared, a.prefix).clone()
+    torch.cuda.synchronize()
+    took = (time.perf_counter() - began) / a.steps
+    print(f"{a.batch} sequences behind {a.prefix} shared tokens: {took * 1e6:.1f} us a step of the block, status {int(block.status.item())}, "
+          f"output rms {x.float().pow(2).mean().sqrt().item():.3g}")
+
+
+if __name__ == "__main__":
+    main()
