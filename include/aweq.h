@@ -391,7 +391,8 @@ int aweq_qk_rope(const void* q, const void* k, aweq_dtype dt, int64_t T, int64_t
 
 /* ---- A paged cache of keys and values.  k_cache and v_cache hold `pages` pages of Hk heads of page_size tokens of D values each,
  * [pages][Hk][page_size][D], in the queries' type (F16 or BF16), or as 8-bit codes (cache_dt = AWEQ_I8) with k_step and v_step
- * [pages][Hk][page_size] fp32: the value is code * step, step = max |x| / 127 of the token's head (1 if that is 0), code = round(x / step).
+ * [pages][Hk][page_size] fp32: the value is code * step, step = max |x| / 127 of the token's head (the smallest normal number at least; 1 for a head of
+ * zeros; always positive), code = round(x / step).
  * (Symmetric, unlike the quantizers above: a zero point would cost a correction of every score.)  page_size: a power of two from 16 to 256.
  *
  * aweq_kv_append: aweq_qk_rope, with the keys, and the values v[T][Hk][D] (pitch ldv) as they are, going to the cache: token t to row slot[t] %
@@ -413,7 +414,7 @@ int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, i
  *   out[t][h] = sum_j p_j v_j,  p = softmax(scale * q k_j);   lse[t][h] (fp32, nullable) = log sum_j exp(scale * q k_j).
  * A token without any key gets zeros, and lse -inf.  max_len and max_q (HOST): no lens[b] and no sequence's count of new tokens is larger; the launch is
  * laid out for them.  A page outside [0, pages), a length over max_len or over what table_ld pages hold, or rows of q_start out of order
- * raise AWEQ_ST_INDEX and are clamped (results unspecified, no access out of range).
+ * raise AWEQ_ST_INDEX and are clamped (results unspecified, no access out of range).  Rows of out and lse past q_start[B] are unspecified.
  * The prefix is read once for all the batch's queries, which multiply its keys together; long key ranges are split between
  * workgroups whose partial results (fp32, in ws) a second launch joins.  Scores and softmax in fp32, with products of the stored
  * type exact in fp32; the probabilities are rounded to F16 / BF16 for the product with v (BF16 queries over an 8-bit cache: both

@@ -143,11 +143,10 @@ struct Shape {
     static constexpr int kHalf = kTallKeys * kRow;
     static constexpr int kSlot = 2 * kHalf + (kCodes ? kTallKeys / 16 * 256 : 0);
     static constexpr int kTallLds = 2 * kSlot;
-    // wide: V of a tile and (codes) its steps for each wavefront; at the end their O, maximum and sum
+    // wide: V of a tile for each wavefront; at the end their O, maximum and sum
     static constexpr int kWideV = kWideKeys * kRow;
-    static constexpr int kWideSlot = kWideV + (kCodes ? 2 * kWideKeys * 4 : 0);
     static constexpr int kMerge = kWaves * (kWideRows * D * 4 + kWideRows * 8);
-    static constexpr int kWideLds = kWaves * kWideSlot > kMerge ? kWaves * kWideSlot : kMerge;
+    static constexpr int kWideLds = kWaves * kWideV > kMerge ? kWaves * kWideV : kMerge;
     static constexpr int lds(bool tall) { return tall && kTallLds > kWideLds ? kTallLds : kWideLds; }
 };
 
@@ -258,7 +257,11 @@ struct Rows {
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) { lv[n][v] = __builtin_amdgcn_logf(vs[n][v]); rv[n][v] = __builtin_amdgcn_rcpf(vs[n][v]); }
+                for (int v = 0; v < 4; ++v) {
+                    const float x = fmaxf(vs[n][v], 1.17549435e-38f);   // (both operations take a subnormal number for 0)
+                    lv[n][v] = __builtin_amdgcn_logf(x);
+                    rv[n][v] = __builtin_amdgcn_rcpf(x);
+                }
         }
         float top[MT];
         bool high = false;
@@ -503,7 +506,8 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
     }
 }
 
-template <class E, int D>
+// STREAM: past the caches
+template <class E, int D, bool STREAM>
 __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* lds)
 {
     using SH = Shape<E, D>;
@@ -521,7 +525,7 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
     const int first = begin + wave * kWideKeys, step = kWaves * kWideKeys;
     const int tiles = end > first ? (end - first + step - 1) / step : 0;
     uint32_t est = 0;
-    char* const vt = lds + wave * SH::kWideSlot;
+    char* const vt = lds + wave * SH::kWideV;
 
     // a tile as it is in flight: K in the operand's order, V 16 bytes a lane, rows across the lanes
     constexpr int kK = N * D / (kCodes ? 64 : 32), kV = N * SH::kLoads;
@@ -531,6 +535,11 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
     auto pages_of = [&](int tile) {
 #pragma unroll
         for (int n = 0; n < N; ++n) next_page[n] = scalar_at(table, min(first + tile * step + n * 16, end - 1) >> g.page_shift);
+    };
+    auto value_at = [](const char* p) {
+        const i32x4* const at = reinterpret_cast<const i32x4*>(p);
+        if constexpr (STREAM) return __builtin_nontemporal_load(at);
+        else return *at;
     };
     auto request = [&](int tile) {
         const int in_page = g.page_size - 1;
@@ -544,11 +553,11 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
             const char* const vb = reinterpret_cast<const char*>(g.v_cache) + head_row * kRow;
             const int krow = min(key0 + col, end - 1) & in_page;
 #pragma unroll
-            for (int kk = 0; kk < kK / N; ++kk) kr[n * (kK / N) + kk] = *reinterpret_cast<const i32x4*>(kb + (uint32_t)(krow * kRow + (kk * 4 + grp) * 16));
+            for (int kk = 0; kk < kK / N; ++kk) kr[n * (kK / N) + kk] = value_at(kb + (uint32_t)(krow * kRow + (kk * 4 + grp) * 16));
 #pragma unroll
             for (int q = 0; q < SH::kLoads; ++q) {
                 const int row = min(key0 + q * SH::kRowsPerLoad + lane / C, end - 1) & in_page;
-                vr[n * SH::kLoads + q] = *reinterpret_cast<const i32x4*>(vb + (uint32_t)(row * kRow + (lane % C) * 16));
+                vr[n * SH::kLoads + q] = value_at(vb + (uint32_t)(row * kRow + (lane % C) * 16));
             }
             if constexpr (kCodes) {   // (those past the end are 1 below: what lies there may be anything)
                 const int row = ((key0 < end ? key0 : (end - 1) & ~15) & in_page) + grp * 4;
@@ -648,8 +657,8 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
 // Wavefronts a SIMD that the registers have to allow
 constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : 1; }
 
-// MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it
-template <class E, int D, int MT>
+// MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it.  STREAM (MT 0): keys and values past the caches (rule and figures at the launch)
+template <class E, int D, int MT, bool STREAM>
 __global__ __launch_bounds__(kThreads, waves_wanted(D, MT)) void attention_kernel(Args g)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -710,9 +719,9 @@ __global__ __launch_bounds__(kThreads, waves_wanted(D, MT)) void attention_kerne
     }
     if constexpr (MT > 0) {
         if (w.tall) tall_block<E, D, MT>(g, j, lds);
-        else wide_block<E, D>(g, j, lds);
+        else wide_block<E, D, false>(g, j, lds);
     } else {
-        wide_block<E, D>(g, j, lds);
+        wide_block<E, D, STREAM>(g, j, lds);
     }
 }
 
@@ -865,11 +874,11 @@ static Plan plan(int64_t T, int64_t Hq, int64_t Hk, int64_t B, int64_t max_q, in
     return p;
 }
 
-template <class E, int D, int MT>
+template <class E, int D, int MT, bool STREAM = false>
 static int launch_one(const Args& g, int64_t blocks, hipStream_t st)
 {
     constexpr int lds = Shape<E, D>::lds(MT > 0);
-    const void* fn = reinterpret_cast<const void*>(attention_kernel<E, D, MT>);
+    const void* fn = reinterpret_cast<const void*>(attention_kernel<E, D, MT, STREAM>);
     int dev = 0, cus = 0;
     if (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, lds) != AWEQ_OK) return AWEQ_ERR_LAUNCH;
     void* args[] = {const_cast<Args*>(&g)};
@@ -889,7 +898,10 @@ static int launch(Args& g, const Plan& p, hipStream_t st)
         if (blocks > (1 << 24) - 1) return AWEQ_ERR_SHAPE;   // 2^32 threads
         w->blocks = (int)n;
     }
-    const int rc = p.mt == 0 ? launch_one<E, D, 0>(g, blocks, st) : p.mt == 1 ? launch_one<E, D, 1>(g, blocks, st) : launch_one<E, D, 2>(g, blocks, st);
+    // Past the caches where the sequences' own keys may not fit them (us, through -> past them: 368 MB of codes 100 -> 95, 737 MB 173 -> 162, 245 MB 51 -> 46, 209 MB
+    // 31.6 -> 28.4, but 131 MB 14.9 -> 16.4)
+    const bool stream = p.mt == 0 && (int64_t)p.own.combos / (p.own.splits ? p.own.splits : 1) * g.max_len * 2 * D * (int64_t)sizeof(E) > kCacheBytes / 4 * 3;
+    const int rc = stream ? launch_one<E, D, 0, true>(g, blocks, st) : p.mt == 0 ? launch_one<E, D, 0>(g, blocks, st) : p.mt == 1 ? launch_one<E, D, 1>(g, blocks, st) : launch_one<E, D, 2>(g, blocks, st);
     if (rc == AWEQ_OK && g.parts > 1) {
         const int64_t rows = g.T * g.Hq;
         // (up to 64 parts a wavefront is as fast as four or faster: 2048 rows of 18 parts 35.1 us with the attention, four each 44.7)

@@ -52,14 +52,14 @@ __device__ __forceinline__ void store_codes(int8_t* dst, float* step_at, const f
 #pragma unroll
     for (int i = 0; i < 8; ++i) big = fmaxf(big, fmaxf(fabsf(a[i]), fabsf(b[i])));
     big = group_allreduce<G>(big, OpMax());
-    float step = big / 127.0f;
-    if (!(step > 0.0f) || isinf(step)) step = 1.0f;
+    float step = fmaxf(big / 127.0f, 1.17549435e-38f);   // (not subnormal: what reads it takes such a number for 0)
+    if (!(big > 0.0f) || isinf(step)) step = 1.0f;
     if (writes_step) *step_at = step;
     auto pack = [&](const float x[8]) {
         uint32_t w[2] = {0u, 0u};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = (int)rintf(__builtin_amdgcn_fmed3f(x[i] / step, -127.0f, 127.0f));   // (a subnormal step can be off by half)
+            const int c = (int)rintf(__builtin_amdgcn_fmed3f(x[i] / step, -127.0f, 127.0f));
             w[i >> 2] |= (uint32_t)(c & 0xff) << (8 * (i & 3));
         }
         return make_uint2(w[0], w[1]);
