@@ -12,7 +12,7 @@
 // The maximum is taken up lazily: any m gives the same quotient, so sum and O are only rescaled when a score is more than 2^8 above it.
 //
 // Two forms:
-//  - tall (many rows: the prefix, prompts): four wavefronts with rows of their own share tiles of 64 keys, filled by LDS-DMA loads of 16 bytes a
+//  - tall (many rows: the prefix, prompts): four wavefronts with rows of their own share tiles of 64 keys (32 of 512 bytes), filled by LDS-DMA loads of 16 bytes a
 //    lane, two tiles in turn; chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.
 //  - wide (up to 16 rows: one token's heads): four wavefronts have the same rows and tiles of 32 keys of their own, whose results meet in
 //    LDS at the end.  K goes from memory to registers in the operand's order, V to registers and through the wavefront's own LDS; the next
@@ -139,9 +139,10 @@ struct Shape {
     static constexpr int kChunks = kRow / 16;
     static constexpr int kLoads = kRow * 16 / 1024;            // load instructions for 16 rows
     static constexpr int kRowsPerLoad = 1024 / kRow;
-    // tall: K, V, and (codes) for each group of 16 keys 16 steps of K, 16 of V (and 32 unused)
-    static constexpr int kHalf = kTallKeys * kRow;
-    static constexpr int kSlot = 2 * kHalf + (kCodes ? kTallKeys / 16 * 256 : 0);
+    // tall: K, V, and (codes) for each group of 16 keys 16 steps of K, 16 of V (and 32 unused); tiles that leave room for two workgroups
+    static constexpr int kTile = kRow == 512 ? 32 : kTallKeys, kGroups = kTile / 16;
+    static constexpr int kHalf = kTile * kRow;
+    static constexpr int kSlot = 2 * kHalf + (kCodes ? kGroups * 256 : 0);
     static constexpr int kTallLds = 2 * kSlot;
     // wide: V of a tile for each wavefront; at the end their O, maximum and sum
     static constexpr int kWideV = kWideKeys * kRow;
@@ -385,48 +386,57 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
     using SH = Shape<E, D>;
     using R = Rows<E, D, MT>;
     using V = typename R::V;
-    constexpr int C = SH::kChunks, kRow = SH::kRow, N = kTallKeys / 16;
+    constexpr int C = SH::kChunks, kRow = SH::kRow, N = SH::kGroups, kTile = SH::kTile;
+    static_assert(N == kWaves || (N == 2 && !SH::kCodes), "a wavefront fetches a group of K and of V, or one of the two");
     constexpr bool kCodes = SH::kCodes;
     const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const int row0 = j.row0 + wave * 16 * MT;
+    const int group = N == kWaves ? wave : wave & 1;   // of 16 keys of a tile, which this wavefront fetches
 
     // tiles: the prefix's, then the sequence's
-    const int np = j.pb > j.pa ? (j.pb - j.pa + kTallKeys - 1) / kTallKeys : 0;
-    const int tiles = np + (j.ob > j.oa ? (j.ob - j.oa + kTallKeys - 1) / kTallKeys : 0);
+    const int np = j.pb > j.pa ? (j.pb - j.pa + kTile - 1) / kTile : 0;
+    const int tiles = np + (j.ob > j.oa ? (j.ob - j.oa + kTile - 1) / kTile : 0);
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
     uint32_t est = 0;
-    auto first_key = [&](int tile) { return tile < np ? j.pa + tile * kTallKeys : j.oa + (tile - np) * kTallKeys; };
+    auto first_key = [&](int tile) { return tile < np ? j.pa + tile * kTile : j.oa + (tile - np) * kTile; };
     auto page_of = [&](int tile) {    // of this wavefront's 16 keys
-        const int key = min(first_key(tile) + wave * 16, (tile < np ? j.pb : j.ob) - 1);
+        const int key = min(first_key(tile) + group * 16, (tile < np ? j.pb : j.ob) - 1);
         return scalar_at(tile < np ? g.prefix_table : j.table, key >> g.page_shift);
     };
     int next_page = tiles > 0 ? page_of(0) : 0;
     // this lane's 16 bytes of the load instructions of K and V, from the first of the 16 rows
     auto fetch_offset = [&](int q, bool v, int last) {
-        const int sub = q * SH::kRowsPerLoad + lane / C, trow = wave * 16 + sub;    // row of the 16, of the tile (the swizzle's)
+        const int sub = q * SH::kRowsPerLoad + lane / C, trow = group * 16 + sub;    // row of the 16, of the tile (the swizzle's)
         return (uint32_t)(min(sub, last) * kRow + ((lane % C) ^ (v ? swz_v<C, kCodes>(trow) : swz_k<C>(trow))) * 16);
     };
     constexpr bool kKept = D < 256;   // (no registers left for them with longer heads)
     uint32_t from_k[SH::kLoads], from_v[SH::kLoads];
 #pragma unroll
     for (int q = 0; q < SH::kLoads; ++q) { from_k[q] = fetch_offset(q, false, 15); from_v[q] = fetch_offset(q, true, 15); }
+    const bool fetches_k = N == kWaves || wave < 2, fetches_v = N == kWaves || wave >= 2;
     auto fetch = [&](int tile, uint32_t slot) {
         int page = next_page;
         if (tile + 1 < tiles) next_page = page_of(tile + 1);
         if ((unsigned)page >= (unsigned)g.pages) { est |= AWEQ_ST_INDEX; page = 0; }
         // the group's first key, a multiple of 16, so that it lies in one page; past the end the last group that has a key
-        const int end = tile < np ? j.pb : j.ob, key0 = min(first_key(tile) + wave * 16, (end - 1) & ~15), last = end - 1 - key0;
+        const int end = tile < np ? j.pb : j.ob, key0 = min(first_key(tile) + group * 16, (end - 1) & ~15), last = end - 1 - key0;
         const int64_t row0 = (((int64_t)page * g.Hk + j.kvh) << g.page_shift) + (key0 & (g.page_size - 1));   // its row of the cache
         const char* const kb = reinterpret_cast<const char*>(g.k_cache) + row0 * kRow;
         const char* const vb = reinterpret_cast<const char*>(g.v_cache) + row0 * kRow;
-        const uint32_t to = lds0 + slot + (uint32_t)(wave * 16 * kRow);
+        const uint32_t to = lds0 + slot + (uint32_t)(group * 16 * kRow);
         if (kKept && last >= 15) {
 #pragma unroll
-            for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, from_k[q], to + q * 1024); dma16(vb, from_v[q], to + q * 1024 + SH::kHalf); }
+            for (int q = 0; q < SH::kLoads; ++q) {
+                if (fetches_k) dma16(kb, from_k[q], to + q * 1024);
+                if (fetches_v) dma16(vb, from_v[q], to + q * 1024 + SH::kHalf);
+            }
         } else {
 #pragma unroll
-            for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, fetch_offset(q, false, last), to + q * 1024); dma16(vb, fetch_offset(q, true, last), to + q * 1024 + SH::kHalf); }
+            for (int q = 0; q < SH::kLoads; ++q) {
+                if (fetches_k) dma16(kb, fetch_offset(q, false, last), to + q * 1024);
+                if (fetches_v) dma16(vb, fetch_offset(q, true, last), to + q * 1024 + SH::kHalf);
+            }
         }
         if constexpr (kCodes) dma4((grp & 1 ? g.v_step : g.k_step) + row0 + min(col, last), lds0 + slot + 2 * SH::kHalf + (uint32_t)wave * 256);
     };
@@ -655,7 +665,7 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
 }
 
 // Wavefronts a SIMD that the registers have to allow
-constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : 1; }
+constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : MT == 1 ? 2 : 1; }
 
 // MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it.  STREAM (MT 0): keys and values past the caches (rule and figures at the launch)
 template <class E, int D, int MT, bool STREAM>
@@ -847,7 +857,7 @@ static void set_work(Work& w, int64_t rows, int mt, int64_t splits, int64_t len,
     w.combos = (int)(items * w.splits);
 }
 
-static Plan plan(int64_t T, int64_t Hq, int64_t Hk, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len)
+static Plan plan(int64_t D, bool codes, int64_t T, int64_t Hq, int64_t Hk, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len)
 {
     const int64_t G = Hq / Hk, all_rows = T * G, most_rows = max_q * G;
     Plan p = {};
@@ -856,8 +866,11 @@ static Plan plan(int64_t T, int64_t Hq, int64_t Hk, int64_t B, int64_t max_q, in
     // left to join
     p.fused = prefix_len > 0 && own_tall && all_rows >= B * 128;
     const bool has_shared = prefix_len > 0 && !p.fused, has_own = max_len > 0 || prefix_len == 0 || p.fused;
-    p.mt = has_own && own_tall ? (most_rows > 64 ? 2 : 1) : 0;
-    if (has_shared && shared_tall && p.mt < 2) p.mt = all_rows > 64 || p.mt == 2 ? 2 : 1;
+    // Row tiles of 16 a wavefront: one of 256 values, so that two workgroups share a compute unit (us, two -> one: 190-token chunks of 4 sequences of 4000 - 8000
+    // keys 288 -> 213, 2048 tokens behind 4096 keys 271 -> 219); but where single tokens' workgroups have the launch in common, which hold 16-bit keys in the
+    // registers of two (decode of 64 behind 8192 62 -> 84), not
+    p.mt = has_own && own_tall ? (most_rows > 64 && D < 256 ? 2 : 1) : 0;
+    if (has_shared && shared_tall && p.mt < 2) p.mt = D == 256 ? (has_own && !own_tall && !codes ? 2 : 1) : all_rows > 64 || p.mt == 2 ? 2 : 1;
     if (has_shared) {
         p.shared.tall = shared_tall;
         const int64_t tile = shared_tall ? kWaves * 16 * p.mt : kWideRows;
@@ -901,7 +914,7 @@ static int launch(Args& g, const Plan& p, hipStream_t st)
     // Past the caches where the sequences' own keys may not fit them (us, through -> past them: 368 MB of codes 100 -> 95, 737 MB 173 -> 162, 245 MB 51 -> 46, 209 MB
     // 31.6 -> 28.4, but 131 MB 14.9 -> 16.4)
     const bool stream = p.mt == 0 && (int64_t)p.own.combos / (p.own.splits ? p.own.splits : 1) * g.max_len * 2 * D * (int64_t)sizeof(E) > kCacheBytes / 4 * 3;
-    const int rc = stream ? launch_one<E, D, 0, true>(g, blocks, st) : p.mt == 0 ? launch_one<E, D, 0>(g, blocks, st) : p.mt == 1 ? launch_one<E, D, 1>(g, blocks, st) : launch_one<E, D, 2>(g, blocks, st);
+    const int rc = stream ? launch_one<E, D, 0, true>(g, blocks, st) : p.mt == 0 ? launch_one<E, D, 0>(g, blocks, st) : p.mt == 1 ? launch_one<E, D, 1>(g, blocks, st) : launch_one<E, D, D == 256 && Shape<E, D>::kCodes ? 1 : 2>(g, blocks, st);
     if (rc == AWEQ_OK && g.parts > 1) {
         const int64_t rows = g.T * g.Hq;
         // (up to 64 parts a wavefront is as fast as four or faster: 2048 rows of 18 parts 35.1 us with the attention, four each 44.7)
@@ -935,7 +948,11 @@ extern "C" size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, in
 {
     if (!attn::shapes_ok(T, Hq, Hk, D, B, max_q, prefix_len, max_len)) return 0;
     max_q = max_q < T ? max_q : T;
-    const int parts = attn::plan(T, Hq, Hk, B, max_q, prefix_len, max_len).parts();
+    int parts = 1;
+    for (const bool codes : {false, true}) {
+        const int n = attn::plan(D, codes, T, Hq, Hk, B, max_q, prefix_len, max_len).parts();
+        if (n > parts) parts = n;
+    }
     return parts > 1 ? (size_t)parts * (size_t)(T * Hq) * (size_t)(D * 4 + 8) : 0;
 }
 
@@ -957,7 +974,7 @@ extern "C" int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, in
     if (!aligned16(q) || !aligned16(out) || (ldq % 8) != 0 || (ldo % 8) != 0 || !aligned16(k_cache) || !aligned16(v_cache) ||
         (cache_dt == AWEQ_I8 && (!aligned16(k_step) || !aligned16(v_step))))
         return AWEQ_ERR_ALIGN;
-    const attn::Plan p = attn::plan(T, Hq, Hk, B, max_q, prefix_len, max_len);
+    const attn::Plan p = attn::plan(D, cache_dt == AWEQ_I8, T, Hq, Hk, B, max_q, prefix_len, max_len);
     const size_t need = aweq_prefix_attention_ws(T, Hq, Hk, D, B, max_q, prefix_len, max_len);
     if (need && (!ws || ws_bytes < need)) return AWEQ_ERR_WORKSPACE;
     if (need && !aligned16(ws)) return AWEQ_ERR_ALIGN;

@@ -103,6 +103,17 @@ def test_some_new_tokens_of_each_sequence(B, G):
             Case("bf16", "i8", 64, 2 * G, 2, 16, lens, new, prefix, seed=m).all(B)
 
 
+@pytest.mark.parametrize("dt,cache", [("f16", "same"), ("bf16", "same"), ("f16", "i8")])
+@pytest.mark.parametrize("G", [1, 4, 9])
+def test_heads_of_256_values(B, G, dt, cache):
+    """Their tiles of keys are shorter, and their row tiles another number where single tokens are behind a prefix: ranges that end in each part of a tile."""
+    for new in ([1, 1, 1, 1, 1], [1, 0, 20, 3, 1], [40, 33, 0, 64, 1]):
+        for prefix in (0, 17, 48, 97, 1100):
+            print(f"[forms] heads of 256, x {G}, new {new}, prefix {prefix}", flush=True)
+            Case(dt, cache, 256, 2 * G, 2, 16 if prefix % 2 else 128, [n + x for n, x in zip(new, (0, 31, 32, 33, 700))], new, prefix, seed=prefix).all(B)
+    Case(dt, cache, 256, 2 * G, 2, 64, [0, 0, 0], [7, 1, 9], 900, seed=G).all(B, max_len=0)
+
+
 def test_steps_next_to_the_smallest_numbers(B):
     """bfloat16 values so small that max / 127 is subnormal: the step stays normal, codes and attention finite."""
     D, page = 64, 16
