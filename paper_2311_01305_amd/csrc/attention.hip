@@ -22,6 +22,13 @@
 //
 // An 8-bit cache is multiplied as binary16 codes.  The step of a key goes to its score.  The step of a value goes into the exponent:
 // p' = exp(s + log step - m') stays in range and is what multiplies the codes; the sum takes p' / step back.
+//
+// What bounds it (heads of 128 values).  Wide: HBM, 4.9 - 5.5 TB/s of keys and values where they are many (24 sequences of 3000 - 15001 tokens and a prefix of
+// 2000, 461 MB of codes, 100 us with the join; a copy of 1 GB reaches 5.2); for one sequence the launches and a round trip each (1900 tokens, 31 MB: 9 us and 3 for
+// the join).  Tall: the clock under load: 970 TFLOP/s in binary16 (1024 new tokens of 2 sequences behind 8192), 80 % of what a product of 8192 x 8192 x 8192
+// reaches here, the matrix cores busy for half of the cycles.  Products of one tile between the exponentials of another, 32 x 32 x 16 instructions, raised
+// priority around the products and a third tile in flight left that as it was.  The prefix of a decode step, whose rows are few, is one round of
+// workgroups that wait for their tiles (64 tokens behind 8192, 25 us, of which half the sequences' own keys; join 5).
 #include "wide_unit.hpp"
 
 #include <cmath>
@@ -410,11 +417,10 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
         const int sub = q * SH::kRowsPerLoad + lane / C, trow = group * 16 + sub;    // row of the 16, of the tile (the swizzle's)
         return (uint32_t)(min(sub, last) * kRow + ((lane % C) ^ (v ? swz_v<C, kCodes>(trow) : swz_k<C>(trow))) * 16);
     };
-    constexpr bool kKept = D < 256;   // (no registers left for them with longer heads)
+    const bool fetches_v = N < kWaves && wave >= 2;   // (short tiles: of V instead of K)
     uint32_t from_k[SH::kLoads], from_v[SH::kLoads];
 #pragma unroll
-    for (int q = 0; q < SH::kLoads; ++q) { from_k[q] = fetch_offset(q, false, 15); from_v[q] = fetch_offset(q, true, 15); }
-    const bool fetches_k = N == kWaves || wave < 2, fetches_v = N == kWaves || wave >= 2;
+    for (int q = 0; q < SH::kLoads; ++q) { from_k[q] = fetch_offset(q, fetches_v, 15); from_v[q] = fetch_offset(q, true, 15); }
     auto fetch = [&](int tile, uint32_t slot) {
         int page = next_page;
         if (tile + 1 < tiles) next_page = page_of(tile + 1);
@@ -422,21 +428,25 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
         // the group's first key, a multiple of 16, so that it lies in one page; past the end the last group that has a key
         const int end = tile < np ? j.pb : j.ob, key0 = min(first_key(tile) + group * 16, (end - 1) & ~15), last = end - 1 - key0;
         const int64_t row0 = (((int64_t)page * g.Hk + j.kvh) << g.page_shift) + (key0 & (g.page_size - 1));   // its row of the cache
+        const uint32_t to = lds0 + slot + (uint32_t)(group * 16 * kRow);
         const char* const kb = reinterpret_cast<const char*>(g.k_cache) + row0 * kRow;
         const char* const vb = reinterpret_cast<const char*>(g.v_cache) + row0 * kRow;
-        const uint32_t to = lds0 + slot + (uint32_t)(group * 16 * kRow);
-        if (kKept && last >= 15) {
+        if constexpr (N < kWaves) {
+            const char* const base = fetches_v ? vb : kb;
+            const uint32_t half = to + (fetches_v ? SH::kHalf : 0);
+            if (last >= 15) {
 #pragma unroll
-            for (int q = 0; q < SH::kLoads; ++q) {
-                if (fetches_k) dma16(kb, from_k[q], to + q * 1024);
-                if (fetches_v) dma16(vb, from_v[q], to + q * 1024 + SH::kHalf);
+                for (int q = 0; q < SH::kLoads; ++q) dma16(base, from_k[q], half + q * 1024);
+            } else {
+#pragma unroll
+                for (int q = 0; q < SH::kLoads; ++q) dma16(base, fetch_offset(q, fetches_v, last), half + q * 1024);
             }
+        } else if (last >= 15) {
+#pragma unroll
+            for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, from_k[q], to + q * 1024); dma16(vb, from_v[q], to + q * 1024 + SH::kHalf); }
         } else {
 #pragma unroll
-            for (int q = 0; q < SH::kLoads; ++q) {
-                if (fetches_k) dma16(kb, fetch_offset(q, false, last), to + q * 1024);
-                if (fetches_v) dma16(vb, fetch_offset(q, true, last), to + q * 1024 + SH::kHalf);
-            }
+            for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, fetch_offset(q, false, last), to + q * 1024); dma16(vb, fetch_offset(q, true, last), to + q * 1024 + SH::kHalf); }
         }
         if constexpr (kCodes) dma4((grp & 1 ? g.v_step : g.k_step) + row0 + min(col, last), lds0 + slot + 2 * SH::kHalf + (uint32_t)wave * 256);
     };
@@ -451,12 +461,19 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) at_v[d] = R::value_offset(d);
     rows.arrived();
-    auto step = [&](int tile, auto slot_c) {
-        constexpr int slot = decltype(slot_c)::value * SH::kSlot;
+    // Own keys that this wavefront's last row sees; tiles past them, and all where it has no rows, are left to the others (6 prompts of up to 1365 tokens behind
+    // 4111: 389 us -> 373; as a branch inside the loop 380, and 4 - 7 % lost at heads of 64 and 256)
+    const int seen = __builtin_amdgcn_readfirstlane(row0 < j.rows ? j.sees0 + (min(row0 + 16 * MT, j.rows) - 1) / g.G : 0);
+    const int work_tiles = row0 >= j.rows ? 0 : np + (min(seen, j.ob) > j.oa ? (min(seen, j.ob) - j.oa + kTile - 1) / kTile : 0);
+    auto landed = [&](int tile, uint32_t slot) {
         wait_vm<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();     // the tile has landed for everyone, and everyone is done with the one before
         if (tile + 1 < tiles) fetch(tile + 1, SH::kSlot - slot);
+    };
+    auto step = [&](int tile, auto slot_c) {
+        constexpr int slot = decltype(slot_c)::value * SH::kSlot;
+        landed(tile, slot);
         const char* const kt = lds + slot;
         const char* const vt = kt + SH::kHalf;
 
@@ -500,10 +517,11 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
             rows.values(vt, u, pu, at_v);
         }
     };
-    for (int tile = 0; tile < tiles; tile += 2) {
+    for (int tile = 0; tile < work_tiles; tile += 2) {
         step(tile, std::integral_constant<int, 0>{});
-        if (tile + 1 < tiles) step(tile + 1, std::integral_constant<int, 1>{});
+        if (tile + 1 < work_tiles) step(tile + 1, std::integral_constant<int, 1>{});
     }
+    for (int tile = work_tiles; tile < tiles; ++tile) landed(tile, (tile & 1) * (uint32_t)SH::kSlot);
     if (est && lane == 0) raise_status(g.status, est);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -867,7 +885,7 @@ static Plan plan(int64_t D, bool codes, int64_t T, int64_t Hq, int64_t Hk, int64
     p.fused = prefix_len > 0 && own_tall && all_rows >= B * 128;
     const bool has_shared = prefix_len > 0 && !p.fused, has_own = max_len > 0 || prefix_len == 0 || p.fused;
     // Row tiles of 16 a wavefront: one of 256 values, so that two workgroups share a compute unit (us, two -> one: 190-token chunks of 4 sequences of 4000 - 8000
-    // keys 288 -> 213, 2048 tokens behind 4096 keys 271 -> 219); but where single tokens' workgroups have the launch in common, which hold 16-bit keys in the
+    // keys 288 -> 209, 2048 tokens behind 4096 keys 271 -> 207); but where single tokens' workgroups have the launch in common, which hold 16-bit keys in the
     // registers of two (decode of 64 behind 8192 62 -> 84), not
     p.mt = has_own && own_tall ? (most_rows > 64 && D < 256 ? 2 : 1) : 0;
     if (has_shared && shared_tall && p.mt < 2) p.mt = D == 256 ? (has_own && !own_tall && !codes ? 2 : 1) : all_rows > 64 || p.mt == 2 ? 2 : 1;

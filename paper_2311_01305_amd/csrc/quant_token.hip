@@ -1,7 +1,9 @@
 // Quantizer of Eq. 1-2 with b = 8 whose slice is a token: Step and Z from the token's own range, widened to contain 0.
 //
-// HBM-bound: 2 bytes in (binary16 / bfloat16), 1 byte out per value, and 7 vector operations a value beside that (11 with scales).  The range has to be known before the first code, so a workgroup keeps the values
-// of its tokens in registers between the two: every value is read once.
+// HBM-bound: 2 bytes in (binary16 / bfloat16), 1 byte out per value, and 7 vector operations a value beside that (11 with scales).  The range
+// has to be known before the first code, so a workgroup keeps the values of its tokens in registers between the two: every value is read once.
+// Measured: 8192 tokens of 22016 bfloat16 values 112 - 122 us, 4.4 - 4.8 TB/s of both; 1777 of 11008 binary16 values with scales 18.8, 3.1 (889 workgroups
+// of two tokens each are one round, which loads, computes and stores at the same time everywhere); 29 of 8192 5, a launch and two exchanges.
 #include "gemm_tokens.hpp"
 #include "token_range.hpp"
 
