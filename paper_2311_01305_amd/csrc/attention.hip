@@ -13,7 +13,9 @@
 //
 // Two forms:
 //  - tall (many rows: the prefix, prompts): four wavefronts with rows of their own share tiles of 64 keys (32 of 512 bytes), filled by LDS-DMA loads of 16 bytes a
-//    lane, two tiles in turn; chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.
+//    lane, two tiles in turn; chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.  Codes go through registers instead, requested two tiles
+//    ahead, and are binary16 in LDS: converted once for the workgroup's rows, with the logarithm and the reciprocal of their steps, not by each wavefront
+//    (us: 2048 tokens behind 8192 keys 462 -> 373, 5 tokens of 16 sequences of up to 6000 48 -> 36, 64 tokens behind 8192 34.5 -> 31).
 //  - wide (up to 16 rows: one token's heads): four wavefronts have the same rows and tiles of 32 keys of their own, whose results meet in
 //    LDS at the end.  K goes from memory to registers in the operand's order, V to registers and through the wavefront's own LDS; the next
 //    tile is requested as soon as this one's registers are free.
@@ -89,14 +91,10 @@ __device__ __forceinline__ void wait_vm()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-// lane i's 16 bytes (4 bytes) land at lds_addr + 16 i (4 i); lds_addr and base wave-uniform
+// lane i's 16 bytes land at lds_addr + 16 i; lds_addr and base wave-uniform
 __device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t lds_addr)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void dma4(const float* at, uint32_t lds_addr)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr), "v"(at) : "memory");
 }
 
 // over the four lanes that hold a row's keys: lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -146,9 +144,10 @@ struct Shape {
     static constexpr int kChunks = kRow / 16;
     static constexpr int kLoads = kRow * 16 / 1024;            // load instructions for 16 rows
     static constexpr int kRowsPerLoad = 1024 / kRow;
-    // tall: K, V, and (codes) for each group of 16 keys 16 steps of K, 16 of V (and 32 unused); tiles that leave room for two workgroups
-    static constexpr int kTile = kRow == 512 ? 32 : kTallKeys, kGroups = kTile / 16;
-    static constexpr int kHalf = kTile * kRow;
+    // tall: K, V, in 16 bits, and (codes) for each group of 16 keys what their steps enter (StepTerms, 64 bytes unused); tiles that leave room for two workgroups
+    static constexpr int kTallRow = 2 * D;
+    static constexpr int kTile = kTallRow == 512 ? 32 : kTallKeys, kGroups = kTile / 16;
+    static constexpr int kHalf = kTile * kTallRow;
     static constexpr int kSlot = 2 * kHalf + (kCodes ? kGroups * 256 : 0);
     static constexpr int kTallLds = 2 * kSlot;
     // wide: V of a tile for each wavefront; at the end their O, maximum and sum
@@ -190,11 +189,21 @@ struct Job {
     int64_t part;
 };
 
-template <class E, int D, int MT>
+// the step of a value as the softmax takes it (both operations take a subnormal number for 0)
+__device__ __forceinline__ void step_terms(float step, float& log2, float& inverse)
+{
+    const float x = fmaxf(step, 1.17549435e-38f);
+    log2 = __builtin_amdgcn_logf(x);
+    inverse = __builtin_amdgcn_rcpf(x);
+}
+
+// PAIRS: K and V are multiplied as they lie in the cache, so that of codes 16 bytes are two operands
+template <class E, int D, int MT, bool PAIRS>
 struct Rows {
     using M = Mfma<E>;
     using V = typename M::V;
     static constexpr bool kCodes = Shape<E, D>::kCodes;
+    static constexpr int kRow = PAIRS ? D : 2 * D, kChunks = kRow / 16;   // of V's tile
 
     V q[MT][D / 32];
     float scale[MT];        // to log2
@@ -202,8 +211,8 @@ struct Rows {
     f32x4 o[MT][D / 16];
     float m[MT], l[MT];     // (l: of this lane's keys)
 
-    // Column lane % 16 of row tile i is row `row0` + 16 i + that; eight values of its head at a time, in the order that K is read in: 32 kk + 8 grp, or for
-    // codes, whose 16-byte chunks are two operands, 64 (kk / 2) + 16 grp + 8 (kk % 2)
+    // Column lane % 16 of row tile i is row `row0` + 16 i + that; eight values of its head at a time, in the order that K is read in: 32 kk + 8 grp, or in
+    // pairs 64 (kk / 2) + 16 grp + 8 (kk % 2)
     __device__ __forceinline__ void load(const Args& g, const Job& j, int row0)
     {
         const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
@@ -212,7 +221,7 @@ struct Rows {
             const int r = min(row0 + 16 * i + col, j.rows - 1);
             sees[i] = j.sees0 + r / g.G;
             const char* src = reinterpret_cast<const char*>(g.q) + ((j.t0 + r / g.G) * g.ldq + (int64_t)(j.kvh * g.G + r % g.G) * D) * 2;
-            auto at = [&](int kk) { return src + (kCodes ? 64 * (kk / 2) + 16 * grp + 8 * (kk % 2) : 32 * kk + 8 * grp) * 2; };
+            auto at = [&](int kk) { return src + (PAIRS ? 64 * (kk / 2) + 16 * grp + 8 * (kk % 2) : 32 * kk + 8 * grp) * 2; };
             scale[i] = g.scale_log2e;
             if (kCodes && g.q_bf16) {
                 // bfloat16 queries as binary16: scaled by a power of two, the largest value below 2^15
@@ -255,22 +264,12 @@ struct Rows {
     }
 
     // Scores s[i][n] of 16 keys each to probabilities for the second product; key0: the tile's first key, end: the range's, own: of the sequence.
-    // ks, vs: (codes) the steps of this lane's keys.
+    // ks, lv, rv: (codes) of this lane's keys the step of K, log2 and reciprocal of the step of V.
     template <int N>
-    __device__ __forceinline__ void softmax(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], int key0, int end, bool own, const float (&ks)[N][4], const float (&vs)[N][4])
+    __device__ __forceinline__ void softmax(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], int key0, int end, bool own, const float (&ks)[N][4], const float (&lv)[N][4],
+                                            const float (&rv)[N][4])
     {
         const int grp = (threadIdx.x & (kWave - 1)) >> 4;
-        float lv[N][4], rv[N][4];
-        if constexpr (kCodes) {
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float x = fmaxf(vs[n][v], 1.17549435e-38f);   // (both operations take a subnormal number for 0)
-                    lv[n][v] = __builtin_amdgcn_logf(x);
-                    rv[n][v] = __builtin_amdgcn_rcpf(x);
-                }
-        }
         float top[MT];
         bool high = false;
 #pragma unroll
@@ -328,9 +327,9 @@ struct Rows {
     // Where a lane's transposing reads of V begin, for 16 values at d: keys 4 grp .. of the first 16 (codes: and of the second) of a tile
     static __device__ __forceinline__ int value_offset(int d)
     {
-        constexpr int C = Shape<E, D>::kChunks, kRow = Shape<E, D>::kRow;
+        constexpr int C = kChunks;
         const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
-        if constexpr (kCodes) {
+        if constexpr (PAIRS) {
             const int r = col >> 1, row = 16 * (r >> 2) + 4 * grp + (r & 3);
             return row * kRow + ((d ^ swz_v<C, true>(row)) * 16) + (col & 1) * 8;
         } else {
@@ -342,12 +341,11 @@ struct Rows {
     // O^T += V^T P^T for keys 32 u .. 32 u + 31 of the tile at vt (the swizzles repeat every 16 rows, the codes' every 32)
     __device__ __forceinline__ void values(const char* vt, int u, const V (&p)[MT], const int (&at)[D / 16])
     {
-        constexpr int kRow = Shape<E, D>::kRow;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
             V vf;
             const char* const from = vt + at[d] + u * 32 * kRow;
-            if constexpr (kCodes) {
+            if constexpr (PAIRS) {
                 const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)from);
                 vf = codes_to_f16(w[0], w[1]);
             } else {
@@ -391,10 +389,10 @@ template <class E, int D, int MT>
 __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* lds)
 {
     using SH = Shape<E, D>;
-    using R = Rows<E, D, MT>;
+    using R = Rows<E, D, MT, false>;
     using V = typename R::V;
-    constexpr int C = SH::kChunks, kRow = SH::kRow, N = SH::kGroups, kTile = SH::kTile;
-    static_assert(N == kWaves || (N == 2 && !SH::kCodes), "a wavefront fetches a group of K and of V, or one of the two");
+    constexpr int C = R::kChunks, kRow = R::kRow, N = SH::kGroups, kTile = SH::kTile;
+    static_assert(N == kWaves || N == 2, "a wavefront fetches a group of K and of V, or one of the two");
     constexpr bool kCodes = SH::kCodes;
     const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
@@ -412,25 +410,32 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
         return scalar_at(tile < np ? g.prefix_table : j.table, key >> g.page_shift);
     };
     int next_page = tiles > 0 ? page_of(0) : 0;
-    // this lane's 16 bytes of the load instructions of K and V, from the first of the 16 rows
-    auto fetch_offset = [&](int q, bool v, int last) {
-        const int sub = q * SH::kRowsPerLoad + lane / C, trow = group * 16 + sub;    // row of the 16, of the tile (the swizzle's)
-        return (uint32_t)(min(sub, last) * kRow + ((lane % C) ^ (v ? swz_v<C, kCodes>(trow) : swz_k<C>(trow))) * 16);
-    };
     const bool fetches_v = N < kWaves && wave >= 2;   // (short tiles: of V instead of K)
-    uint32_t from_k[SH::kLoads], from_v[SH::kLoads];
-#pragma unroll
-    for (int q = 0; q < SH::kLoads; ++q) { from_k[q] = fetch_offset(q, fetches_v, 15); from_v[q] = fetch_offset(q, true, 15); }
-    auto fetch = [&](int tile, uint32_t slot) {
+    // The group's first key of a tile is a multiple of 16, so that it lies in one page; past the end the last group that has a key.  Returns its row of the
+    // cache; `last`: of the 16, the last that the range has.  Tiles are asked for in order: the next one's page is on its way by then.
+    auto place = [&](int tile, int& last) {
         int page = next_page;
         if (tile + 1 < tiles) next_page = page_of(tile + 1);
         if ((unsigned)page >= (unsigned)g.pages) { est |= AWEQ_ST_INDEX; page = 0; }
-        // the group's first key, a multiple of 16, so that it lies in one page; past the end the last group that has a key
-        const int end = tile < np ? j.pb : j.ob, key0 = min(first_key(tile) + group * 16, (end - 1) & ~15), last = end - 1 - key0;
-        const int64_t row0 = (((int64_t)page * g.Hk + j.kvh) << g.page_shift) + (key0 & (g.page_size - 1));   // its row of the cache
-        const uint32_t to = lds0 + slot + (uint32_t)(group * 16 * kRow);
+        const int end = tile < np ? j.pb : j.ob, key0 = min(first_key(tile) + group * 16, (end - 1) & ~15);
+        last = end - 1 - key0;
+        return (((int64_t)page * g.Hk + j.kvh) << g.page_shift) + (key0 & (g.page_size - 1));
+    };
+    // 16 bits: LDS-DMA; this lane's 16 bytes of the load instructions of K and V, from the first of the 16 rows
+    auto fetch_offset = [&](int q, bool v, int last) {
+        const int sub = q * SH::kRowsPerLoad + lane / C, trow = group * 16 + sub;    // row of the 16, of the tile (the swizzle's)
+        return (uint32_t)(min(sub, last) * kRow + ((lane % C) ^ (v ? swz_v<C, false>(trow) : swz_k<C>(trow))) * 16);
+    };
+    uint32_t from_k[SH::kLoads], from_v[SH::kLoads];
+    if constexpr (!kCodes)
+#pragma unroll
+        for (int q = 0; q < SH::kLoads; ++q) { from_k[q] = fetch_offset(q, fetches_v, 15); from_v[q] = fetch_offset(q, true, 15); }
+    auto fetch = [&](int tile, uint32_t slot) {
+        int last;
+        const int64_t row0 = place(tile, last);
         const char* const kb = reinterpret_cast<const char*>(g.k_cache) + row0 * kRow;
         const char* const vb = reinterpret_cast<const char*>(g.v_cache) + row0 * kRow;
+        const uint32_t to = lds0 + slot + (uint32_t)(group * 16 * kRow);
         if constexpr (N < kWaves) {
             const char* const base = fetches_v ? vb : kb;
             const uint32_t half = to + (fetches_v ? SH::kHalf : 0);
@@ -448,13 +453,53 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
 #pragma unroll
             for (int q = 0; q < SH::kLoads; ++q) { dma16(kb, fetch_offset(q, false, last), to + q * 1024); dma16(vb, fetch_offset(q, true, last), to + q * 1024 + SH::kHalf); }
         }
-        if constexpr (kCodes) dma4((grp & 1 ? g.v_step : g.k_step) + row0 + min(col, last), lds0 + slot + 2 * SH::kHalf + (uint32_t)wave * 256);
+    };
+    // Codes: to registers, and from there as binary16 to LDS, with what their steps enter: each is converted once for the workgroup's rows
+    constexpr int kCodeChunks = D / 16;
+    i32x4 code_k[SH::kLoads], code_v[SH::kLoads];
+    float step_kv;
+    auto request = [&](int tile) {
+        int last;
+        const int64_t row0 = place(tile, last);
+        const char* const kb = reinterpret_cast<const char*>(fetches_v ? g.v_cache : g.k_cache) + row0 * D;
+        const char* const vb = reinterpret_cast<const char*>(g.v_cache) + row0 * D;
+#pragma unroll
+        for (int q = 0; q < SH::kLoads; ++q) {
+            const uint32_t from = (uint32_t)(min(q * SH::kRowsPerLoad + lane / kCodeChunks, last) * D + (lane % kCodeChunks) * 16);
+            code_k[q] = *reinterpret_cast<const i32x4*>(kb + from);
+            if constexpr (N == kWaves) code_v[q] = *reinterpret_cast<const i32x4*>(vb + from);
+        }
+        step_kv = ((grp & 1) ? g.v_step : g.k_step)[row0 + min(col, last)];
+    };
+    auto convert = [&](uint32_t slot) {
+        char* const tile = lds + slot;
+        auto put = [&](char* half, int row, int swz, const i32x4& w) {
+            const int c = 2 * (lane % kCodeChunks);
+            *reinterpret_cast<f16x8*>(half + row * kRow + ((c ^ swz) * 16)) = codes_to_f16(w[0], w[1]);
+            *reinterpret_cast<f16x8*>(half + row * kRow + (((c + 1) ^ swz) * 16)) = codes_to_f16(w[2], w[3]);
+        };
+#pragma unroll
+        for (int q = 0; q < SH::kLoads; ++q) {
+            const int row = group * 16 + q * SH::kRowsPerLoad + lane / kCodeChunks;
+            put(tile + (fetches_v ? SH::kHalf : 0), row, fetches_v ? swz_v<C, false>(row) : swz_k<C>(row), code_k[q]);
+            if constexpr (N == kWaves) put(tile + SH::kHalf, row, swz_v<C, false>(row), code_v[q]);
+        }
+        if (!fetches_v && lane < 32) {
+            float* const terms = reinterpret_cast<float*>(tile + 2 * SH::kHalf + group * 256) + col;
+            if (grp == 0) terms[0] = step_kv;
+            else step_terms(step_kv, terms[16], terms[32]);
+        }
     };
 
     R rows;
     rows.load(g, j, row0);
-    if (tiles > 0) fetch(0, 0);
-    constexpr int kSteps = kCodes ? D / 64 : D / 32;
+    if constexpr (kCodes) {
+        if (tiles > 0) { request(0); convert(0); }
+        if (tiles > 1) request(1);
+    } else {
+        if (tiles > 0) fetch(0, 0);
+    }
+    constexpr int kSteps = D / 32;
     int at_k[kSteps], at_v[D / 16];
 #pragma unroll
     for (int kk = 0; kk < kSteps; ++kk) at_k[kk] = col * kRow + (((kk * 4 + grp) ^ swz_k<C>(col)) * 16);   // (repeats every 16 rows)
@@ -466,10 +511,16 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
     const int seen = __builtin_amdgcn_readfirstlane(row0 < j.rows ? j.sees0 + (min(row0 + 16 * MT, j.rows) - 1) / g.G : 0);
     const int work_tiles = row0 >= j.rows ? 0 : np + (min(seen, j.ob) > j.oa ? (min(seen, j.ob) - j.oa + kTile - 1) / kTile : 0);
     auto landed = [&](int tile, uint32_t slot) {
-        wait_vm<0>();
+        if constexpr (!kCodes) wait_vm<0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();     // the tile has landed for everyone, and everyone is done with the one before
-        if (tile + 1 < tiles) fetch(tile + 1, SH::kSlot - slot);
+        asm volatile("" ::: "memory");
+        if constexpr (kCodes) {
+            if (tile + 1 < tiles) convert(SH::kSlot - slot);
+            if (tile + 2 < tiles) request(tile + 2);
+        } else {
+            if (tile + 1 < tiles) fetch(tile + 1, SH::kSlot - slot);
+        }
     };
     auto step = [&](int tile, auto slot_c) {
         constexpr int slot = decltype(slot_c)::value * SH::kSlot;
@@ -485,30 +536,22 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
 #pragma unroll
             for (int kk = 0; kk < kSteps; ++kk) {
                 const i32x4 w = *reinterpret_cast<const i32x4*>(kt + at_k[kk] + n * 16 * kRow);
-                if constexpr (kCodes) {
-                    const V a = codes_to_f16(w[0], w[1]), b = codes_to_f16(w[2], w[3]);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(a, rows.q[i][2 * kk], s[i][n]);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(b, rows.q[i][2 * kk + 1], s[i][n]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(__builtin_bit_cast(V, w), rows.q[i][kk], s[i][n]);
-                }
+                for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(__builtin_bit_cast(V, w), rows.q[i][kk], s[i][n]);
             }
         }
-        float ks[N][4], vs[N][4];
+        float ks[N][4], lv[N][4], rv[N][4];
         if constexpr (kCodes) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const Float4 a = *reinterpret_cast<const Float4*>(kt + 2 * SH::kHalf + n * 256 + grp * 16);
-                const Float4 c = *reinterpret_cast<const Float4*>(kt + 2 * SH::kHalf + n * 256 + 64 + grp * 16);
+                const Float4* const terms = reinterpret_cast<const Float4*>(kt + 2 * SH::kHalf + n * 256 + grp * 16);
+                const Float4 a = terms[0], b = terms[4], c = terms[8];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) { ks[n][v] = a.f[v]; vs[n][v] = c.f[v]; }
+                for (int v = 0; v < 4; ++v) { ks[n][v] = a.f[v]; lv[n][v] = b.f[v]; rv[n][v] = c.f[v]; }
             }
         }
         V p[MT][N / 2];
-        rows.template softmax<N>(s, p, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, ks, vs);
+        rows.template softmax<N>(s, p, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, ks, lv, rv);
 #pragma unroll
         for (int u = 0; u < N / 2; ++u) {
             V pu[MT];
@@ -539,7 +582,7 @@ template <class E, int D, bool STREAM>
 __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* lds)
 {
     using SH = Shape<E, D>;
-    using R = Rows<E, D, 1>;
+    using R = Rows<E, D, 1, SH::kCodes>;
     using V = typename R::V;
     constexpr int C = SH::kChunks, kRow = SH::kRow, N = kWideKeys / 16;
     constexpr bool kCodes = SH::kCodes;
@@ -645,8 +688,15 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
             request(tile + 1);
             if (tile + 2 < tiles) pages_of(tile + 2);
         }
+        float lv[N][4], rv[N][4];
+        if constexpr (kCodes) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) step_terms(vs[n][v], lv[n][v], rv[n][v]);
+        }
         V p[1][N / 2];
-        rows.template softmax<N>(s, p, first + tile * step, end, own, ks, vs);
+        rows.template softmax<N>(s, p, first + tile * step, end, own, ks, lv, rv);
 #pragma unroll
         for (int u = 0; u < N / 2; ++u) {
             const V pu[1] = {p[0][u]};
