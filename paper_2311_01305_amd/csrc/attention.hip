@@ -936,8 +936,12 @@ static Plan plan(int64_t D, bool codes, int64_t T, int64_t Hq, int64_t Hk, int64
     const bool has_shared = prefix_len > 0 && !p.fused, has_own = max_len > 0 || prefix_len == 0 || p.fused;
     // Row tiles of 16 a wavefront: one of 256 values, so that two workgroups share a compute unit (us, two -> one: 190-token chunks of 4 sequences of 4000 - 8000
     // keys 288 -> 209, 2048 tokens behind 4096 keys 271 -> 207); but where single tokens' workgroups have the launch in common, which hold 16-bit keys in the
-    // registers of two (decode of 64 behind 8192 62 -> 84), not
-    p.mt = has_own && own_tall ? (most_rows > 64 && D < 256 ? 2 : 1) : 0;
+    // registers of two (decode of 64 behind 8192 62 -> 84), not.  With shorter heads one where workgroups of two are no more than the compute units (us, two -> one: 300 tokens x 16
+    // heads of codes 19.1 -> 12.9, 500 x 32 17.7 -> 15.3, 1000 x 32 heads of 64 20.1 -> 16.1, of 128 28.4 -> 25.5, two of 700 x 8 23.2 -> 21.7; but 2000 x 8 37.7 ->
+    // 38.4, and where ranges of more keys fill the chip, 200 behind 6000, 44 -> 59)
+    const int64_t own_keys = max_len + (p.fused ? prefix_len : 0), pairs = B * Hk * cdiv(most_rows, 2 * kWaves * 16);
+    const bool fills = pairs * tall_splits(pairs, own_keys) > 256;
+    p.mt = has_own && own_tall ? (most_rows > 64 && D < 256 && fills ? 2 : 1) : 0;
     if (has_shared && shared_tall && p.mt < 2) p.mt = D == 256 ? (has_own && !own_tall && !codes ? 2 : 1) : all_rows > 64 || p.mt == 2 ? 2 : 1;
     if (has_shared) {
         p.shared.tall = shared_tall;

@@ -114,6 +114,15 @@ def test_heads_of_256_values(B, G, dt, cache):
     Case(dt, cache, 256, 2 * G, 2, 64, [0, 0, 0], [7, 1, 9], 900, seed=G).all(B, max_len=0)
 
 
+@pytest.mark.parametrize("cache", ["same", "i8"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_row_tiles_by_the_workgroups_they_leave(B, D, cache):
+    """Prompts in tiles of 64 rows (few heads) and of 128 (many), that end in each part of one, and rows of tiles that see different keys."""
+    for Hq, Hk, new, before, prefix in ((2, 2, [200, 1, 130], 0, 0), (2, 1, [65, 97], 33, 70), (64, 32, [200, 1, 130], 0, 0), (96, 48, [129, 97, 64], 33, 70)):
+        print(f"[forms] row tiles, {Hq}/{Hk} heads of {D} {cache}", flush=True)
+        Case("bf16", cache, D, Hq, Hk, 16, [n + before for n in new], new, prefix, seed=Hq).all(B)
+
+
 def test_steps_next_to_the_smallest_numbers(B):
     """bfloat16 values so small that max / 127 is subnormal: the step stays normal, codes and attention finite."""
     D, page = 64, 16
