@@ -368,7 +368,7 @@ __device__ __forceinline__ void store_row(const Args& g, const Job& j, int r, in
     const int64_t t = j.t0 + r / g.G;
     const int h = j.kvh * g.G + r % g.G;
     if (g.parts == 1) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = l != 0.0f ? 1.0f / l : 0.0f;   // (0: no key; a NaN goes on)
         if (g.q_bf16) {
             typedef __bf16 b4 __attribute__((ext_vector_type(4)));
             *reinterpret_cast<b4*>(reinterpret_cast<__bf16*>(g.out) + t * g.ldo + (int64_t)h * D + d) =
@@ -377,10 +377,10 @@ __device__ __forceinline__ void store_row(const Args& g, const Job& j, int r, in
             *reinterpret_cast<f16x4*>(reinterpret_cast<_Float16*>(g.out) + t * g.ldo + (int64_t)h * D + d) =
                 f16x4{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
         }
-        if (d == 0 && g.lse) g.lse[t * g.Hq + h] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+        if (d == 0 && g.lse) g.lse[t * g.Hq + h] = l != 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     } else {
         const int64_t at = j.part * (g.T * g.Hq) + t * g.Hq + h;
-        if (l > 0.0f) *reinterpret_cast<f32x4*>(g.part_o + at * D + d) = v;   // (a part without keys is not read)
+        if (l != 0.0f) *reinterpret_cast<f32x4*>(g.part_o + at * D + d) = v;   // (a part without keys is not read)
         if (d == 0) g.part_ml[at] = make_float2(m, l);
     }
 }
@@ -827,9 +827,12 @@ __global__ __launch_bounds__(256) void join_kernel(Args g)
     }
     mm = wave_allreduce(mm, Larger());
     float w[kOf], ll = 0.0f;
+    uint64_t there[kOf];             // parts that have keys: of no weight at all, they may still have a NaN or an infinity
 #pragma unroll
     for (int c = 0; c < kOf; ++c) {
-        w[c] = ml[c].y > 0.0f ? __builtin_amdgcn_exp2f(ml[c].x - mm) : 0.0f;
+        const bool keys = ml[c].y != 0.0f;
+        there[c] = __builtin_amdgcn_ballot_w64(keys);
+        w[c] = keys ? __builtin_amdgcn_exp2f(ml[c].x - mm) : 0.0f;
         ll += w[c] * ml[c].y;
     }
     ll = wave_allreduce(ll, OpAdd());
@@ -844,9 +847,8 @@ __global__ __launch_bounds__(256) void join_kernel(Args g)
             for (int f = 0; f < kFlight; ++f) {
                 const int p = p0 + f * W * kAtOnce + sub;
                 a[f] = __shfl(w[c], p & (kWave - 1));
-                if (p >= n) a[f] = 0.0f;
                 x[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                if (a[f] != 0.0f) x[f] = *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)(c * kWave + p) * all_rows + row) * D + at);
+                if (p < n && (there[c] >> p & 1)) x[f] = *reinterpret_cast<const f32x4*>(g.part_o + ((int64_t)(c * kWave + p) * all_rows + row) * D + at);
             }
 #pragma unroll
             for (int f = 0; f < kFlight; ++f) v += a[f] * x[f];
@@ -864,7 +866,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args g)
 #pragma unroll
         for (int o = 1; o < W; ++o) v += s_part[o][at / 4];
     }
-    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+    const float inv = ll != 0.0f ? 1.0f / ll : 0.0f;
     if (sub == 0) {
         const int64_t to = row / g.Hq * g.ldo + row % g.Hq * D + at;
         if (g.q_bf16) {
@@ -874,7 +876,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args g)
             *reinterpret_cast<f16x4*>(reinterpret_cast<_Float16*>(g.out) + to) = f16x4{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
         }
     }
-    if (lane == 0 && g.lse) g.lse[row] = ll > 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
+    if (lane == 0 && g.lse) g.lse[row] = ll != 0.0f ? (mm + __builtin_amdgcn_logf(ll)) * kLn2 : -INFINITY;
 }
 
 // How a call is cut up
