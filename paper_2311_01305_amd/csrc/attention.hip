@@ -47,6 +47,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLazy = 8.0f;       // log2 of what a probability may be over 1
+constexpr float kFar = 1 << 22;     // scores (log2) that binary32 holds to half or better
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kWideRows = 16, kWideKeys = 32, kTallKeys = 64;
 
@@ -210,6 +211,7 @@ struct Rows {
     int sees[MT];           // own keys that the row sees
     f32x4 o[MT][D / 16];
     float m[MT], l[MT];     // (l: of this lane's keys)
+    bool far;               // a maximum is so large that its last place is no small part of 1
 
     // Column lane % 16 of row tile i is row `row0` + 16 i + that; eight values of its head at a time, in the order that K is read in: 32 kk + 8 grp, or in
     // pairs 64 (kk / 2) + 16 grp + 8 (kk % 2)
@@ -245,6 +247,7 @@ struct Rows {
             }
             m[i] = -INFINITY;
             l[i] = 0.0f;
+            far = false;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[i][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -297,6 +300,7 @@ struct Rows {
             high = high || top[i] > m[i] + kLazy;
         }
         if (__builtin_amdgcn_ballot_w64(high) != 0) {
+            bool large = false;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const float m_new = fmaxf(m[i], row_reduce(top[i], Larger()));
@@ -305,17 +309,32 @@ struct Rows {
                 l[i] *= a;
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) o[i][d] *= a;
+                large = large || (fabsf(m_new) > kFar && m_new != -INFINITY);
+            }
+            far = __builtin_amdgcn_ballot_w64(large) != 0;
+        }
+        float use[MT], times[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) { use[i] = m[i] == -INFINITY ? 0.0f : m[i]; times[i] = scale[i]; }
+        if (!kCodes && far) {   // (what a maximum was rounded by would not cancel in the fused form: it may be more than any exponent)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) s[i][n][v] = s[i][n][v] * scale[i] - use[i];
+                use[i] = 0.0f;
+                times[i] = 1.0f;
             }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const float use = m[i] == -INFINITY ? 0.0f : m[i];
             float sum = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const float x = __builtin_amdgcn_exp2f(kCodes ? s[i][n][v] - use : __builtin_fmaf(s[i][n][v], scale[i], -use));
+                    const float x = __builtin_amdgcn_exp2f(kCodes ? s[i][n][v] - use[i] : __builtin_fmaf(s[i][n][v], times[i], -use[i]));
                     if constexpr (kCodes) sum = __builtin_fmaf(x, rv[n][v], sum);
                     else sum += x;
                     p[i][n / 2][(n & 1) * 4 + v] = (typename M::S)x;

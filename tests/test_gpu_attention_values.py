@@ -186,3 +186,28 @@ def test_a_score_of_minus_infinity_leaves_its_key_out(B, form, D):
         b.check(out, lse)
         if every:
             assert (out[:, 0] == 0).all() and (lse[:, 0] == -math.inf).all()
+
+
+def large_scores(B, form, dt, codes):
+    """Scores of 2^30 and more that are whole numbers of a power of two, so that their sums are exact and the largest ones often equal."""
+    lens, new, prefix, Hq, Hk, joined = FORMS[form]
+    for D in (64, 128):
+        b = Batch(dt, codes, D, lens, new, prefix, Hq, Hk, seed=D)
+        g = torch.Generator()
+        g.manual_seed(D)
+        whole = lambda x: torch.randint(-3, 4, x.shape, generator=g)
+        b.q = (whole(b.q) * 2.0 ** (13 if dt == "f16" else 50)).to(TYPES[dt])
+        for r, x in enumerate(b.k):
+            b.k[r] = whole(x).to(torch.int8) if codes else (whole(x) * 2.0 ** (13 if dt == "f16" else 50)).to(TYPES[dt])
+            if codes:
+                b.ks[r].fill_(2.0 ** 20)
+        b.scale = 0.25
+        print(f"[values] {form} D={D} {dt} codes={codes} large scores", flush=True)
+        out, lse = b.run(B, joined)
+        b.check(out, lse, exact_scores=True)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_scores_of_any_size(B, form, dt):
+    large_scores(B, form, dt, False)
