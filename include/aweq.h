@@ -418,8 +418,9 @@ int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, i
  * raise AWEQ_ST_INDEX and are clamped (results unspecified, no access out of range).  Rows of out and lse past q_start[B] are unspecified.
  * The prefix is read once for all the batch's queries, which multiply its keys together; long key ranges are split between
  * workgroups whose partial results (fp32, in ws) a second launch joins.  Scores and softmax in fp32, with products of the stored
- * type exact in fp32; the probabilities are rounded to F16 / BF16 for the product with v (BF16 queries over an 8-bit cache: both
- * products in F16, the queries scaled by a power of two).  D 64, 128 or 256; Hq a multiple of Hk; scale > 0;
+ * type exact in fp32; the probabilities are rounded to F16 / BF16 for the product with v (an 8-bit cache: both products in F16, BF16 queries scaled by a power
+ * of two, and probabilities times their value's step by one for each token and head, which follows the largest step that it sees: a step says nothing of its
+ * key's weight; a step of a value that is not finite makes the out of what sees it NaN).  D 64, 128 or 256; Hq a multiple of Hk; scale > 0;
  * cache as above.
  * ws: aweq_prefix_attention_ws(...) bytes, 16-byte aligned (host function). */
 size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len);

@@ -14,7 +14,7 @@
 // Two forms:
 //  - tall (many rows: the prefix, prompts): four wavefronts with rows of their own share tiles of 64 keys (32 of 512 bytes), filled by LDS-DMA loads of 16 bytes a
 //    lane, two tiles in turn; chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.  Codes go through registers instead, requested two tiles
-//    ahead, and are binary16 in LDS: converted once for the workgroup's rows, with the logarithm and the reciprocal of their steps, not by each wavefront
+//    ahead, and are binary16 in LDS: converted once for the workgroup's rows, not by each wavefront
 //    (us: 2048 tokens behind 8192 keys 462 -> 373, 5 tokens of 16 sequences of up to 6000 48 -> 36, 64 tokens behind 8192 34.5 -> 31).
 //  - wide (up to 16 rows: one token's heads): four wavefronts have the same rows and tiles of 32 keys of their own, whose results meet in
 //    LDS at the end.  K goes from memory to registers in the operand's order, V to registers and through the wavefront's own LDS; the next
@@ -22,8 +22,11 @@
 // 16 neighbouring tokens lie in one page (its size is a multiple of 16), so a group of 16 rows has one base address.  A tile's rows past the range
 // repeat its last token: what a page holds past the range is never read.
 //
-// An 8-bit cache is multiplied as binary16 codes.  The step of a key goes to its score.  The step of a value goes into the exponent:
-// p' = exp(s + log step - m') stays in range and is what multiplies the codes; the sum takes p' / step back.
+// An 8-bit cache is multiplied as binary16 codes.  The step of a key goes to its score.  The step of a value goes to the probability that multiplies
+// its codes, p' = p step 2^e, with a power of two for each row that keeps p' in binary16's range and follows the largest step which the row has seen, as the
+// maximum follows the scores; O is rescaled when it changes.  The exponential brings 2^e along, and the sum has it too: no operation more for a key.  (What
+// is below 2^-60 or beyond 2^90, a power of two for the wavefront's rows together, goes to the steps first.)  Maximum and sum are of the scores alone: a value's
+// step says nothing of its weight.
 //
 // What bounds it (heads of 128 values).  Wide: HBM, 4.9 - 5.5 TB/s of keys and values where they are many (24 sequences of 3000 - 15001 tokens and a prefix of
 // 2000, 461 MB of codes, 100 us with the join; a copy of 1 GB reaches 5.2); for one sequence the launches and a round trip each (1900 tokens, 31 MB: 9 us and 3 for
@@ -47,6 +50,8 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLazy = 8.0f;       // log2 of what a probability may be over 1
+constexpr int kStepBits = 7;        // (codes) log2 of what a step 2^e may be, which multiplies that: together below binary16's 2^16
+constexpr int kLeast = -60, kMost = 90;   // (codes) e that the exponential brings along: sums of 2^30 keys stay in range, and so do keys of 2^-60 of the largest
 constexpr float kFar = 1 << 22;     // scores (log2) that binary32 holds to half or better
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kWideRows = 16, kWideKeys = 32, kTallKeys = 64;
@@ -107,6 +112,7 @@ __device__ __forceinline__ float row_reduce(float v, Op op)
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+struct OpMaximum { __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); } };   // (of IEEE: a NaN stays one)
 struct Larger { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
 // E: type of the cache (int8_t: codes)
@@ -145,11 +151,11 @@ struct Shape {
     static constexpr int kChunks = kRow / 16;
     static constexpr int kLoads = kRow * 16 / 1024;            // load instructions for 16 rows
     static constexpr int kRowsPerLoad = 1024 / kRow;
-    // tall: K, V, in 16 bits, and (codes) for each group of 16 keys what their steps enter (StepTerms, 64 bytes unused); tiles that leave room for two workgroups
+    // tall: K, V, in 16 bits, and (codes) for each group of 16 keys the steps of K and of V; tiles that leave room for two workgroups
     static constexpr int kTallRow = 2 * D;
     static constexpr int kTile = kTallRow == 512 ? 32 : kTallKeys, kGroups = kTile / 16;
     static constexpr int kHalf = kTile * kTallRow;
-    static constexpr int kSlot = 2 * kHalf + (kCodes ? kGroups * 256 : 0);
+    static constexpr int kSlot = 2 * kHalf + (kCodes ? kGroups * 128 : 0);
     static constexpr int kTallLds = 2 * kSlot;
     // wide: V of a tile for each wavefront; at the end their O, maximum and sum
     static constexpr int kWideV = kWideKeys * kRow;
@@ -190,14 +196,6 @@ struct Job {
     int64_t part;
 };
 
-// the step of a value as the softmax takes it (both operations take a subnormal number for 0)
-__device__ __forceinline__ void step_terms(float step, float& log2, float& inverse)
-{
-    const float x = fmaxf(step, 1.17549435e-38f);
-    log2 = __builtin_amdgcn_logf(x);
-    inverse = __builtin_amdgcn_rcpf(x);
-}
-
 // PAIRS: K and V are multiplied as they lie in the cache, so that of codes 16 bytes are two operands
 template <class E, int D, int MT, bool PAIRS>
 struct Rows {
@@ -207,11 +205,14 @@ struct Rows {
     static constexpr int kRow = PAIRS ? D : 2 * D, kChunks = kRow / 16;   // of V's tile
 
     V q[MT][D / 32];
-    float scale[MT];        // to log2
+    float scale[MT];        // to log2 (codes: the keys' steps bring that; the power of two that the queries have to lose)
     int sees[MT];           // own keys that the row sees
     f32x4 o[MT][D / 16];
     float m[MT], l[MT];     // (l: of this lane's keys)
     bool far;               // a maximum is so large that its last place is no small part of 1
+    float most[MT];         // (codes) no value's step that the row has seen is larger; a power of two, or 0
+    float use[MT];          // (codes) what the exponential takes off a score: the maximum less held(i)
+    int base;               // (codes) the sum is 2^held(i) times what it stands for, O 2^(base + held(i)) times
 
     // Column lane % 16 of row tile i is row `row0` + 16 i + that; eight values of its head at a time, in the order that K is read in: 32 kk + 8 grp, or in
     // pairs 64 (kk / 2) + 16 grp + 8 (kk % 2)
@@ -224,7 +225,7 @@ struct Rows {
             sees[i] = j.sees0 + r / g.G;
             const char* src = reinterpret_cast<const char*>(g.q) + ((j.t0 + r / g.G) * g.ldq + (int64_t)(j.kvh * g.G + r % g.G) * D) * 2;
             auto at = [&](int kk) { return src + (PAIRS ? 64 * (kk / 2) + 16 * grp + 8 * (kk % 2) : 32 * kk + 8 * grp) * 2; };
-            scale[i] = g.scale_log2e;
+            scale[i] = kCodes ? 1.0f : g.scale_log2e;
             if (kCodes && g.q_bf16) {
                 // bfloat16 queries as binary16: scaled by a power of two, the largest value below 2^15
                 float x[D / 32][8], big = 0.0f;
@@ -240,7 +241,7 @@ struct Rows {
                 for (int kk = 0; kk < D / 32; ++kk)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) q[i][kk][e] = (typename M::S)ldexpf(x[kk][e], e2);
-                scale[i] = ldexpf(g.scale_log2e, -e2);
+                scale[i] = ldexpf(1.0f, -e2);
             } else {
 #pragma unroll
                 for (int kk = 0; kk < D / 32; ++kk) q[i][kk] = *reinterpret_cast<const V*>(at(kk));
@@ -248,6 +249,9 @@ struct Rows {
             m[i] = -INFINITY;
             l[i] = 0.0f;
             far = false;
+            base = 0;
+            most[i] = 0.0f;
+            use[i] = 0.0f;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) o[i][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -266,65 +270,113 @@ struct Rows {
             }
     }
 
+    __device__ __forceinline__ int shift(int i) const { return kStepBits + 127 - (int)(__float_as_uint(most[i]) >> 23); }
+    __device__ __forceinline__ int held(int i) const { return min(max(shift(i) - base, kLeast), kMost); }
+
     // Scores s[i][n] of 16 keys each to probabilities for the second product; key0: the tile's first key, end: the range's, own: of the sequence.
-    // ks, lv, rv: (codes) of this lane's keys the step of K, log2 and reciprocal of the step of V.
-    template <int N>
-    __device__ __forceinline__ void softmax(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], int key0, int end, bool own, const float (&ks)[N][4], const float (&lv)[N][4],
-                                            const float (&rv)[N][4])
+    // (codes) The steps of K are in the scores, scaled and to log2; v_steps(n): those of V of this lane's four keys, asked for twice, since they are not kept
+    // across the branches between (of keys past the range: anything).
+    template <int N, class VSteps>
+    __device__ __forceinline__ void softmax(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], int key0, int end, bool own, VSteps v_steps)
     {
         const int grp = (threadIdx.x & (kWave - 1)) >> 4;
-        float top[MT];
-        bool high = false;
+        float top[MT], step[MT];   // (step: codes)
+        bool high = false, loud = false, odd = false;
+        float widest = 0.0f;
+        if constexpr (kCodes) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const Float4 vs = v_steps(n);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) widest = __builtin_elementwise_maximum(widest, vs.f[v]);   // (a NaN stays one)
+            }
+        }
+        auto mine = [&](int i) { return (own ? min(end, sees[i]) : end) - key0 - grp * 4; };   // of this lane's keys, how far the row sees
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const int lim = own ? min(end, sees[i]) : end;
-            if constexpr (kCodes) {
+            step[i] = widest;
+            if (__builtin_amdgcn_ballot_w64(key0 + 16 * N > (own ? min(end, sees[i]) : end)) != 0) {
+                const int in = mine(i);
+                if constexpr (kCodes) odd = __builtin_amdgcn_ballot_w64(!(widest < INFINITY)) != 0;
+                step[i] = 0.0f;
 #pragma unroll
-                for (int n = 0; n < N; ++n)
+                for (int n = 0; n < N; ++n) {
+                    Float4 vs;
+                    if constexpr (kCodes) vs = v_steps(n);
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) s[i][n][v] = __builtin_fmaf(s[i][n][v], ks[n][v] * scale[i], lv[n][v]);
-            }
-            if (__builtin_amdgcn_ballot_w64(key0 + 16 * N > lim) != 0) {
-                const int mine = lim - key0 - grp * 4;
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) s[i][n][v] = n * 16 + v < mine ? s[i][n][v] : -INFINITY;
+                    for (int v = 0; v < 4; ++v) {
+                        s[i][n][v] = n * 16 + v < in ? s[i][n][v] : -INFINITY;
+                        if constexpr (kCodes) step[i] = n * 16 + v < in ? __builtin_elementwise_maximum(step[i], vs.f[v]) : step[i];
+                    }
+                }
             }
             float t = -INFINITY;
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) t = fmaxf(t, s[i][n][v]);
-            top[i] = kCodes ? t : t * scale[i];    // (scale > 0)
+            top[i] = t * scale[i];    // (scale > 0)
             high = high || top[i] > m[i] + kLazy;
+            if constexpr (kCodes) loud = loud || !(step[i] <= most[i]);
         }
-        if (__builtin_amdgcn_ballot_w64(high) != 0) {
-            bool large = false;
+        if (__builtin_amdgcn_ballot_w64(high || loud) != 0) {
+            float times[MT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const float m_new = fmaxf(m[i], row_reduce(top[i], Larger()));
-                const float a = __builtin_amdgcn_exp2f(m[i] - (m_new == -INFINITY ? 0.0f : m_new));
-                m[i] = m_new;
-                l[i] *= a;
+            for (int i = 0; i < MT; ++i) times[i] = 1.0f;
+            if (!kCodes || __builtin_amdgcn_ballot_w64(high) != 0) {
+                bool large = false;
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) o[i][d] *= a;
-                large = large || (fabsf(m_new) > kFar && m_new != -INFINITY);
+                for (int i = 0; i < MT; ++i) {
+                    const float m_new = fmaxf(m[i], row_reduce(top[i], Larger()));
+                    times[i] = __builtin_amdgcn_exp2f(m[i] - (m_new == -INFINITY ? 0.0f : m_new));
+                    m[i] = m_new;
+                    l[i] *= times[i];
+                    large = large || (fabsf(m_new) > kFar && m_new != -INFINITY);
+                }
+                far = __builtin_amdgcn_ballot_w64(large) != 0;
             }
-            far = __builtin_amdgcn_ballot_w64(large) != 0;
-        }
-        float use[MT], times[MT];
+            if constexpr (kCodes) {
+                if (__builtin_amdgcn_ballot_w64(loud) != 0) odd = rescale(step, times) || odd;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) { use[i] = m[i] == -INFINITY ? 0.0f : m[i]; times[i] = scale[i]; }
-        if (!kCodes && far) {   // (what a maximum was rounded by would not cancel in the fused form: it may be more than any exponent)
+                for (int i = 0; i < MT; ++i) use[i] = (m[i] == -INFINITY || far ? 0.0f : m[i]) - (float)held(i);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) o[i][d] *= times[i];
+        }
+        float less[MT], times[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            less[i] = kCodes ? use[i] : m[i] == -INFINITY ? 0.0f : m[i];
+            times[i] = scale[i];
+        }
+        if (far) {   // (what a maximum was rounded by would not cancel in the fused form: it may be more than any exponent)
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
 #pragma unroll
                 for (int n = 0; n < N; ++n)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) s[i][n][v] = s[i][n][v] * scale[i] - use[i];
-                use[i] = 0.0f;
+                    for (int v = 0; v < 4; ++v) s[i][n][v] = s[i][n][v] * scale[i] - (m[i] == -INFINITY ? 0.0f : m[i]);
+                if constexpr (!kCodes) less[i] = 0.0f;
                 times[i] = 1.0f;
+            }
+        }
+        float vs[N][4];
+        if constexpr (kCodes) {
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const Float4 x = v_steps(n);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) vs[n][v] = x.f[v];
+            }
+            if (base != 0 || odd) {   // (what is not finite is not for rows that do not see it)
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) vs[n][v] = vs[n][v] < INFINITY ? ldexpf(vs[n][v], base) : 0.0f;
+                asm volatile("" ::: "memory");
             }
         }
 #pragma unroll
@@ -334,12 +386,74 @@ struct Rows {
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const float x = __builtin_amdgcn_exp2f(kCodes ? s[i][n][v] - use[i] : __builtin_fmaf(s[i][n][v], times[i], -use[i]));
-                    if constexpr (kCodes) sum = __builtin_fmaf(x, rv[n][v], sum);
-                    else sum += x;
-                    p[i][n / 2][(n & 1) * 4 + v] = (typename M::S)x;
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][n][v], times[i], -less[i]));
+                    sum += x;
+                    p[i][n / 2][(n & 1) * 4 + v] = (typename M::S)(kCodes ? x * vs[n][v] : x);
                 }
             l[i] += sum;
+        }
+    }
+
+    // (codes) The powers of two after a step that is larger than those before; whether one is not finite.  step: of this lane's keys that a row sees; times: what
+    // O is to be multiplied by
+    __device__ __forceinline__ bool rescale(const float (&step)[MT], float (&times)[MT])
+    {
+        int before[MT];
+        bool odd = false, outside = base != 0;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            before[i] = held(i);
+            const float largest = row_reduce(step[i], OpMaximum());
+            if (!(largest < INFINITY)) {
+                odd = true;
+                times[i] = NAN;
+            } else if (largest > most[i]) {
+                most[i] = __uint_as_float(((__float_as_uint(largest) >> 23) + 1) << 23);   // (the next power of two)
+            }
+            outside = outside || (most[i] > 0.0f && (shift(i) < kLeast || shift(i) > kMost));
+        }
+        const int old = base;
+        if (__builtin_amdgcn_ballot_w64(outside) != 0) {
+            int least = 1024, greatest = -1024;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                if (most[i] > 0.0f) {
+                    least = min(least, shift(i));
+                    greatest = max(greatest, shift(i));
+                }
+            least = __builtin_amdgcn_readfirstlane(wave_allreduce(least, OpMin()));
+            greatest = __builtin_amdgcn_readfirstlane(wave_allreduce(greatest, OpMax()));
+            base = min(max(greatest - kMost, 0), least - kLeast);   // (rows whose steps are less than 2^-150 of another's of these have fewer digits)
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int up = held(i) - before[i];
+            l[i] = ldexpf(l[i], up);
+            times[i] = ldexpf(times[i], up + base - old);
+        }
+        return __builtin_amdgcn_ballot_w64(odd) != 0;
+    }
+
+    // After the last key.  (codes) The sum's power of two goes to the maximum, which it is as good as, and O's is the same; where it is a large one both lose it
+    __device__ __forceinline__ void finish()
+    {
+        if constexpr (kCodes) {
+            bool large = far || base != 0;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) large = large || (m[i] != -INFINITY && (held(i) < -32 || held(i) > 32));
+            if (__builtin_amdgcn_ballot_w64(large) == 0) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) m[i] = m[i] == -INFINITY ? m[i] : use[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    l[i] = ldexpf(l[i], -held(i));
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) o[i][d][v] = ldexpf(o[i][d][v], -base - held(i));
+                }
+            }
         }
     }
 
@@ -504,9 +618,9 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
             if constexpr (N == kWaves) put(tile + SH::kHalf, row, swz_v<C, false>(row), code_v[q]);
         }
         if (!fetches_v && lane < 32) {
-            float* const terms = reinterpret_cast<float*>(tile + 2 * SH::kHalf + group * 256) + col;
-            if (grp == 0) terms[0] = step_kv;
-            else step_terms(step_kv, terms[16], terms[32]);
+            float* const steps = reinterpret_cast<float*>(tile + 2 * SH::kHalf + group * 128) + col;
+            if (grp == 0) steps[0] = step_kv * g.scale_log2e;
+            else steps[16] = step_kv;
         }
     };
 
@@ -559,18 +673,17 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
                 for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(__builtin_bit_cast(V, w), rows.q[i][kk], s[i][n]);
             }
         }
-        float ks[N][4], lv[N][4], rv[N][4];
+        V p[MT][N / 2];
+        const char* const steps = kt + 2 * SH::kHalf + grp * 16;
         if constexpr (kCodes) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const Float4* const terms = reinterpret_cast<const Float4*>(kt + 2 * SH::kHalf + n * 256 + grp * 16);
-                const Float4 a = terms[0], b = terms[4], c = terms[8];
+                const Float4 ks = *reinterpret_cast<const Float4*>(steps + n * 128);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) { ks[n][v] = a.f[v]; lv[n][v] = b.f[v]; rv[n][v] = c.f[v]; }
+                for (int i = 0; i < MT; ++i) s[i][n] *= f32x4{ks.f[0], ks.f[1], ks.f[2], ks.f[3]};
             }
         }
-        V p[MT][N / 2];
-        rows.template softmax<N>(s, p, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, ks, lv, rv);
+        rows.template softmax<N>(s, p, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, [&](int n) { return *reinterpret_cast<const Float4*>(steps + n * 128 + 64); });
 #pragma unroll
         for (int u = 0; u < N / 2; ++u) {
             V pu[MT];
@@ -585,6 +698,7 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
     }
     for (int tile = work_tiles; tile < tiles; ++tile) landed(tile, (tile & 1) * (uint32_t)SH::kSlot);
     if (est && lane == 0) raise_status(g.status, est);
+    rows.finish();
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const float l = row_reduce(rows.l[i], OpAdd());
@@ -649,7 +763,7 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
                 const int row = min(key0 + q * SH::kRowsPerLoad + lane / C, end - 1) & in_page;
                 vr[n * SH::kLoads + q] = value_at(vb + (uint32_t)(row * kRow + (lane % C) * 16));
             }
-            if constexpr (kCodes) {   // (those past the end are 1 below: what lies there may be anything)
+            if constexpr (kCodes) {   // (past the end: anything)
                 const int row = ((key0 < end ? key0 : (end - 1) & ~15) & in_page) + grp * 4;
                 kst[n] = *reinterpret_cast<const Float4*>(g.k_step + head_row + row);
                 vst[n] = *reinterpret_cast<const Float4*>(g.v_step + head_row + row);
@@ -692,30 +806,21 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
                 *reinterpret_cast<i32x4*>(vt + row * kRow + (((lane % C) ^ swz_v<C, kCodes>(row)) * 16)) = vr[n * SH::kLoads + q];
             }
         wave_lds_fence();
-        float ks[N][4], vs[N][4];
+        Float4 vs[N];
         if constexpr (kCodes) {
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < N; ++n) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const bool in = first + tile * step + n * 16 + grp * 4 + v < end;
-                    ks[n][v] = in ? kst[n].f[v] : 1.0f;
-                    vs[n][v] = in ? vst[n].f[v] : 1.0f;
-                }
+                for (int v = 0; v < 4; ++v) s[0][n][v] *= kst[n].f[v] * g.scale_log2e;
+                vs[n] = vst[n];
+            }
         }
         if (tile + 1 < tiles) {
             request(tile + 1);
             if (tile + 2 < tiles) pages_of(tile + 2);
         }
-        float lv[N][4], rv[N][4];
-        if constexpr (kCodes) {
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) step_terms(vs[n][v], lv[n][v], rv[n][v]);
-        }
         V p[1][N / 2];
-        rows.template softmax<N>(s, p, first + tile * step, end, own, ks, lv, rv);
+        rows.template softmax<N>(s, p, first + tile * step, end, own, [&](int n) { return vs[n]; });
 #pragma unroll
         for (int u = 0; u < N / 2; ++u) {
             const V pu[1] = {p[0][u]};
@@ -725,6 +830,7 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
     if (est && lane == 0) raise_status(g.status, est);
 
     // the wavefronts' keys of the same 16 rows
+    rows.finish();
     const float l = row_reduce(rows.l[0], OpAdd());
     __syncthreads();   // (every wavefront is done with its tiles)
     float* const so = reinterpret_cast<float*>(lds);                         // [wave][row][D]
@@ -751,12 +857,13 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
     }
 }
 
-// Wavefronts a SIMD that the registers have to allow
+// Wavefronts a SIMD that the registers have to allow, and for which the compiler orders loads and products (with room for one more it waited for each load of a
+// tile by itself: 8-bit codes, row tiles of 64, 5 tokens of 16 sequences of up to 6000 keys 42.0 us -> 36.6; binary16, 711 tokens x 8 heads 21.5 -> 20.0)
 constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : MT == 1 ? 2 : 1; }
 
 // MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it.  STREAM (MT 0): keys and values past the caches (rule and figures at the launch)
 template <class E, int D, int MT, bool STREAM>
-__global__ __launch_bounds__(kThreads, waves_wanted(D, MT)) void attention_kernel(Args g)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_wanted(D, MT), waves_wanted(D, MT)))) void attention_kernel(Args g)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const bool shared = (int)blockIdx.x < g.shared.blocks;

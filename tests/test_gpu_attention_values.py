@@ -211,3 +211,38 @@ def large_scores(B, form, dt, codes):
 @pytest.mark.parametrize("form", list(FORMS))
 def test_scores_of_any_size(B, form, dt):
     large_scores(B, form, dt, False)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_steps_of_any_size(B, form, D, dt):
+    """A value's step says nothing about its key's weight: the smallest normal number in all keys or in a few of them, sizes spread over many orders, and
+    large ones in keys that earlier tokens do not see."""
+    lens, new, prefix, Hq, Hk, joined = FORMS[form]
+    tiny = 2.0 ** -126
+    spread = (-30, 6) if dt == "f16" else (-80, 30)
+    for kind in ("all_tiny", "five_tiny", "every_other_tiny", "spread", "large_last"):
+        print(f"[values] {form} D={D} {dt} steps: {kind}", flush=True)
+        b = Batch(dt, True, D, lens, new, prefix, Hq, Hk, seed=D)
+        g = torch.Generator()
+        g.manual_seed(D)
+        for r, s in enumerate(b.vs):
+            n = s.shape[0]
+            if kind == "all_tiny":
+                s.fill_(tiny)
+            elif kind == "five_tiny":
+                s[torch.randperm(n, generator=g)[:5]] = tiny
+            elif kind == "every_other_tiny":
+                s[::2] = tiny
+            elif kind == "spread":
+                s *= 2.0 ** torch.randint(*spread, s.shape, generator=g)
+            elif r and n > 1:
+                s[-(-n // 2):] *= 2.0 ** spread[1]
+        b.check(*b.run(B, joined))
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_scores_of_any_size_over_codes(B, form, dt):
+    large_scores(B, form, dt, True)
