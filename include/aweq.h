@@ -413,7 +413,8 @@ int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, i
  *   new tokens, appended before this call: new token i of m sees the first lens[b] - m + 1 + i of them.
  *   out[t][h] = sum_j p_j v_j,  p = softmax(scale * q k_j);   lse[t][h] (fp32, nullable) = log sum_j exp(scale * q k_j).
  * A token without any key gets zeros, and lse -inf; so does one whose scores all are -inf, and any key of such a score is left out.  A NaN in a query, in a key
- * that it sees or in that key's step, and a score of +inf, make the token's out and lse for that head NaN, however the keys are split; no status bit tells of it.  max_len and max_q (HOST): no lens[b] and no sequence's count of new tokens is larger; the launch is
+ * that it sees or in that key's step, and a score of +inf, make the token's out and lse for that head NaN, however the keys are split; a
+ * value that is not finite makes the out of the tokens that see it infinite or NaN where it stands, and has no part in any other's.  No status bit tells of it.  max_len and max_q (HOST): no lens[b] and no sequence's count of new tokens is larger; the launch is
  * laid out for them.  A page outside [0, pages), a length over max_len or over what table_ld pages hold, or rows of q_start out of order
  * raise AWEQ_ST_INDEX and are clamped (results unspecified, no access out of range).  Rows of out and lse past q_start[B] are unspecified.
  * The prefix is read once for all the batch's queries, which multiply its keys together; long key ranges are split between

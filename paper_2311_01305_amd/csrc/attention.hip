@@ -22,6 +22,10 @@
 // 16 neighbouring tokens lie in one page (its size is a multiple of 16), so a group of 16 rows has one base address.  A tile's rows past the range
 // repeat its last token: what a page holds past the range is never read.
 //
+// A value that a row does not see has a probability of 0, which times an infinity or a NaN is not 0.  Where the workgroup's rows do not see all keys of its range
+// and an output comes out not finite, the workgroup takes the range once more and counts what is not finite by rows that see it: up to twice the time, for
+// such calls alone (the others: a look at the outputs, us, before -> now: 6 prompts behind 4111 keys 373.3 -> 376.2, 3 of 700 tokens 24.0 -> 25.1).
+//
 // An 8-bit cache is multiplied as binary16 codes.  The step of a key goes to its score.  The step of a value goes to the probability that multiplies
 // its codes, p' = p step 2^e, with a power of two for each row that keeps p' in binary16's range and follows the largest step which the row has seen, as the
 // maximum follows the scores; O is rescaled when it changes.  The exponential brings 2^e along, and the sum has it too: no operation more for a key.  (What
@@ -120,12 +124,14 @@ template <class E> struct Mfma;
 template <> struct Mfma<_Float16> {
     typedef f16x8 V;
     typedef _Float16 S;
+    static constexpr unsigned kExponent = 0x7c00;   // all ones
     static __device__ __forceinline__ f32x4 mul(V a, V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mfma<int8_t> : Mfma<_Float16> {};
 template <> struct Mfma<__bf16> {
     typedef bf16x8 V;
     typedef __bf16 S;
+    static constexpr unsigned kExponent = 0x7f80;
     static __device__ __forceinline__ f32x4 mul(V a, V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
@@ -204,6 +210,7 @@ struct Rows {
     static constexpr bool kCodes = Shape<E, D>::kCodes;
     static constexpr int kRow = PAIRS ? D : 2 * D, kChunks = kRow / 16;   // of V's tile
 
+    int lane;
     V q[MT][D / 32];
     float scale[MT];        // to log2 (codes: the keys' steps bring that; the power of two that the queries have to lose)
     int sees[MT];           // own keys that the row sees
@@ -216,9 +223,10 @@ struct Rows {
 
     // Column lane % 16 of row tile i is row `row0` + 16 i + that; eight values of its head at a time, in the order that K is read in: 32 kk + 8 grp, or in
     // pairs 64 (kk / 2) + 16 grp + 8 (kk % 2)
-    __device__ __forceinline__ void load(const Args& g, const Job& j, int row0)
+    __device__ __forceinline__ void load(const Args& g, const Job& j, int row0, int of)
     {
-        const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+        lane = of;
+        const int col = lane & 15, grp = lane >> 4;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int r = min(row0 + 16 * i + col, j.rows - 1);
@@ -246,10 +254,19 @@ struct Rows {
 #pragma unroll
                 for (int kk = 0; kk < D / 32; ++kk) q[i][kk] = *reinterpret_cast<const V*>(at(kk));
             }
+        }
+        begin();
+    }
+
+    // no key yet
+    __device__ __forceinline__ void begin()
+    {
+        far = false;
+        base = 0;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
             m[i] = -INFINITY;
             l[i] = 0.0f;
-            far = false;
-            base = 0;
             most[i] = 0.0f;
             use[i] = 0.0f;
 #pragma unroll
@@ -273,15 +290,20 @@ struct Rows {
     __device__ __forceinline__ int shift(int i) const { return kStepBits + 127 - (int)(__float_as_uint(most[i]) >> 23); }
     __device__ __forceinline__ int held(int i) const { return min(max(shift(i) - base, kLeast), kMost); }
 
-    // Scores s[i][n] of 16 keys each to probabilities for the second product; key0: the tile's first key, end: the range's, own: of the sequence.
-    // (codes) The steps of K are in the scores, scaled and to log2; v_steps(n): those of V of this lane's four keys, asked for twice, since they are not kept
-    // across the branches between (of keys past the range: anything).
-    template <int N, class VSteps>
-    __device__ __forceinline__ void softmax(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], int key0, int end, bool own, VSteps v_steps)
+    // of this lane's keys in a tile from key0 on, how far row i sees; end: of the range, own: the sequence's
+    __device__ __forceinline__ int mine(int i, int key0, int end, bool own) const
     {
-        const int grp = (threadIdx.x & (kWave - 1)) >> 4;
+        return (own ? min(end, sees[i]) : end) - key0 - (lane >> 4) * 4;
+    }
+
+    // Scores s[i][n] of 16 keys each from key0 on: those that a row does not see to -inf, maxima and what hangs on them.  (codes) The steps of K are in the
+    // scores, scaled and to log2; v_steps(n): those of V of this lane's four keys, asked for twice, since they are not kept across the branches between
+    // (of keys past the range: anything); odd: one is not finite.
+    template <int N, class VSteps>
+    __device__ __forceinline__ void maxima(f32x4 (&s)[MT][N], int key0, int end, bool own, VSteps v_steps, bool& odd)
+    {
         float top[MT], step[MT];   // (step: codes)
-        bool high = false, loud = false, odd = false;
+        bool high = false, loud = false;
         float widest = 0.0f;
         if constexpr (kCodes) {
 #pragma unroll
@@ -291,12 +313,11 @@ struct Rows {
                 for (int v = 0; v < 4; ++v) widest = __builtin_elementwise_maximum(widest, vs.f[v]);   // (a NaN stays one)
             }
         }
-        auto mine = [&](int i) { return (own ? min(end, sees[i]) : end) - key0 - grp * 4; };   // of this lane's keys, how far the row sees
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             step[i] = widest;
             if (__builtin_amdgcn_ballot_w64(key0 + 16 * N > (own ? min(end, sees[i]) : end)) != 0) {
-                const int in = mine(i);
+                const int in = mine(i, key0, end, own);
                 if constexpr (kCodes) odd = __builtin_amdgcn_ballot_w64(!(widest < INFINITY)) != 0;
                 step[i] = 0.0f;
 #pragma unroll
@@ -345,6 +366,12 @@ struct Rows {
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) o[i][d] *= times[i];
         }
+    }
+
+    // Scores to probabilities for the second product
+    template <int N, class VSteps>
+    __device__ __forceinline__ void weights(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], VSteps v_steps, bool odd)
+    {
         float less[MT], times[MT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -458,10 +485,10 @@ struct Rows {
     }
 
     // Where a lane's transposing reads of V begin, for 16 values at d: keys 4 grp .. of the first 16 (codes: and of the second) of a tile
-    static __device__ __forceinline__ int value_offset(int d)
+    __device__ __forceinline__ int value_offset(int d) const
     {
         constexpr int C = kChunks;
-        const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+        const int col = lane & 15, grp = lane >> 4;
         if constexpr (PAIRS) {
             const int r = col >> 1, row = 16 * (r >> 2) + 4 * grp + (r & 3);
             return row * kRow + ((d ^ swz_v<C, true>(row)) * 16) + (col & 1) * 8;
@@ -471,26 +498,93 @@ struct Rows {
         }
     }
 
-    // O^T += V^T P^T for keys 32 u .. 32 u + 31 of the tile at vt (the swizzles repeat every 16 rows, the codes' every 32)
-    __device__ __forceinline__ void values(const char* vt, int u, const V (&p)[MT], const int (&at)[D / 16])
+    // V^T of 16 values for keys 32 u .. 32 u + 31 of the tile at vt (the swizzles repeat every 16 rows, the codes' every 32)
+    static __device__ __forceinline__ V value_operand(const char* vt, int u, int at)
+    {
+        const char* const from = vt + at + u * 32 * kRow;
+        if constexpr (PAIRS) {
+            const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)from);
+            return codes_to_f16(w[0], w[1]);
+        } else {
+            union { s16x4 h[2]; V v; } f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                f.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from + half * 16 * kRow));
+            return f.v;
+        }
+    }
+
+    // O^T += V^T P^T for the tile at vt
+    template <int N>
+    __device__ __forceinline__ void values(const char* vt, const V (&p)[MT][N / 2], const int (&at)[D / 16])
     {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-            V vf;
-            const char* const from = vt + at[d] + u * 32 * kRow;
-            if constexpr (PAIRS) {
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)from);
-                vf = codes_to_f16(w[0], w[1]);
-            } else {
-                union { s16x4 h[2]; V v; } f;
+        for (int u = 0; u < N / 2; ++u)
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    f.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from + half * 16 * kRow));
-                vf = f.v;
+            for (int d = 0; d < D / 16; ++d) {
+                const V vf = value_operand(vt, u, at[d]);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) o[i][d] = M::mul(vf, p[i][u], o[i][d]);
             }
+    }
+
+    // The same where some are not finite and rows do not see all keys: what is not finite is counted, with 1 in the place of what a row sees, and makes the outputs of
+    // rows that see some NaN
+    template <int N>
+    __device__ __forceinline__ void values_seen(const char* vt, const V (&p)[MT][N / 2], const int (&at)[D / 16], int key0, int end, bool own)
+    {
+        typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+        constexpr unsigned short kBelow = M::kExponent - 1;
+        const unsigned short one = __builtin_bit_cast(unsigned short, (typename M::S)1.0f);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) o[i][d] = M::mul(vf, p[i], o[i][d]);
+        for (int u = 0; u < N / 2; ++u) {
+            u16x8 sees_it[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sees_it[i][e] = (2 * u + e / 4) * 16 + e % 4 < mine(i, key0, end, own) ? one : 0;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+                const u16x8 bits = __builtin_bit_cast(u16x8, value_operand(vt, u, at[d]));
+                const u16x8 over = __builtin_elementwise_max((u16x8)(bits & (unsigned short)0x7fff), (u16x8)kBelow) - kBelow;
+                const u16x8 mask = (u16x8)0 - __builtin_elementwise_min(over, (u16x8)1);    // all ones where it is not finite
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+                    const f32x4 bad = M::mul(__builtin_bit_cast(V, (u16x8)(mask & one)), __builtin_bit_cast(V, sees_it[i]), none);
+                    o[i][d] = M::mul(__builtin_bit_cast(V, (u16x8)(bits & ~mask)), p[i][u], o[i][d]);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[i][d][v] = bad[v] > 0.0f ? NAN : o[i][d][v];
+                }
+                __builtin_amdgcn_sched_barrier(0);   // (few registers rather than few waits)
+            }
         }
+    }
+
+    // All of it for a tile whose scores are s
+    template <int N, bool SEEN, class VSteps>
+    __device__ __forceinline__ void attend(f32x4 (&s)[MT][N], const char* vt, const int (&at)[D / 16], int key0, int end, bool own, VSteps v_steps)
+    {
+        bool odd = false;
+        maxima<N>(s, key0, end, own, v_steps, odd);
+        V p[MT][N / 2];
+        weights<N>(s, p, v_steps, odd);
+        if constexpr (SEEN) values_seen<N>(vt, p, at, key0, end, own);
+        else values<N>(vt, p, at);
+    }
+
+    // Whether an output is not finite.  Where rows do not see all keys that may be another's doing: a probability of 0 times an infinity or a NaN is not 0.  Then
+    // the workgroup does it all again with SEEN, which minds what a row sees.
+    __device__ __forceinline__ bool not_finite() const
+    {
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) z = __builtin_elementwise_maximum(z, fabsf(o[i][d][v]));
+        return __builtin_amdgcn_ballot_w64(!(z < INFINITY)) != 0;
     }
 };
 
@@ -518,8 +612,18 @@ __device__ __forceinline__ void store_row(const Args& g, const Job& j, int r, in
     }
 }
 
-template <class E, int D, int MT>
-__device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* lds)
+// AGAIN: one that the compiler does not know to be the same, so that the second time keeps no registers through the first
+template <bool AGAIN>
+__device__ __forceinline__ int thread_index()
+{
+    int t = (int)threadIdx.x;
+    if constexpr (AGAIN) asm volatile("" : "+v"(t));
+    return t;
+}
+
+// SEEN: some value is not finite (both forms); true: it has to be done again with SEEN
+template <class E, int D, int MT, bool SEEN>
+__device__ __forceinline__ bool tall_block(const Args& g, const Job& j, char* lds)
 {
     using SH = Shape<E, D>;
     using R = Rows<E, D, MT, false>;
@@ -527,8 +631,8 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
     constexpr int C = R::kChunks, kRow = R::kRow, N = SH::kGroups, kTile = SH::kTile;
     static_assert(N == kWaves || N == 2, "a wavefront fetches a group of K and of V, or one of the two");
     constexpr bool kCodes = SH::kCodes;
-    const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const int thread = thread_index<SEEN>(), lane = thread & (kWave - 1), col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(thread / kWave);
     const int row0 = j.row0 + wave * 16 * MT;
     const int group = N == kWaves ? wave : wave & 1;   // of 16 keys of a tile, which this wavefront fetches
 
@@ -624,8 +728,11 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
         }
     };
 
+    __shared__ int s_again;
+    const bool unseen = !kCodes && !SEEN && j.ob > max(j.oa, j.sees0 + j.row0 / g.G);   // (the workgroup's first row does not see all)
+    if (unseen && threadIdx.x == 0) s_again = 0;   // (a barrier a tile before it is used)
     R rows;
-    rows.load(g, j, row0);
+    rows.load(g, j, row0, lane);
     if constexpr (kCodes) {
         if (tiles > 0) { request(0); convert(0); }
         if (tiles > 1) request(1);
@@ -637,7 +744,7 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
 #pragma unroll
     for (int kk = 0; kk < kSteps; ++kk) at_k[kk] = col * kRow + (((kk * 4 + grp) ^ swz_k<C>(col)) * 16);   // (repeats every 16 rows)
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) at_v[d] = R::value_offset(d);
+    for (int d = 0; d < D / 16; ++d) at_v[d] = rows.value_offset(d);
     rows.arrived();
     // Own keys that this wavefront's last row sees; tiles past them, and all where it has no rows, are left to the others (6 prompts of up to 1365 tokens behind
     // 4111: 389 us -> 373; as a branch inside the loop 380, and 4 - 7 % lost at heads of 64 and 256)
@@ -673,7 +780,6 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
                 for (int i = 0; i < MT; ++i) s[i][n] = R::M::mul(__builtin_bit_cast(V, w), rows.q[i][kk], s[i][n]);
             }
         }
-        V p[MT][N / 2];
         const char* const steps = kt + 2 * SH::kHalf + grp * 16;
         if constexpr (kCodes) {
 #pragma unroll
@@ -683,14 +789,7 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
                 for (int i = 0; i < MT; ++i) s[i][n] *= f32x4{ks.f[0], ks.f[1], ks.f[2], ks.f[3]};
             }
         }
-        rows.template softmax<N>(s, p, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, [&](int n) { return *reinterpret_cast<const Float4*>(steps + n * 128 + 64); });
-#pragma unroll
-        for (int u = 0; u < N / 2; ++u) {
-            V pu[MT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) pu[i] = p[i][u];
-            rows.values(vt, u, pu, at_v);
-        }
+        rows.template attend<N, SEEN>(s, vt, at_v, first_key(tile), tile < np ? j.pb : j.ob, tile >= np, [&](int n) { return *reinterpret_cast<const Float4*>(steps + n * 128 + 64); });
     };
     for (int tile = 0; tile < work_tiles; tile += 2) {
         step(tile, std::integral_constant<int, 0>{});
@@ -698,6 +797,11 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
     }
     for (int tile = work_tiles; tile < tiles; ++tile) landed(tile, (tile & 1) * (uint32_t)SH::kSlot);
     if (est && lane == 0) raise_status(g.status, est);
+    if (unseen) {
+        if (rows.not_finite() && lane == 0) s_again = 1;
+        __syncthreads();
+        if (__builtin_amdgcn_readfirstlane(s_again) != 0) return true;
+    }
     rows.finish();
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -708,19 +812,20 @@ __device__ __forceinline__ void tall_block(const Args& g, const Job& j, char* ld
             for (int d = 0; d < D / 16; ++d) store_row<D>(g, j, r, d * 16 + grp * 4, rows.o[i][d], rows.m[i], l);
         }
     }
+    return false;
 }
 
 // STREAM: past the caches
-template <class E, int D, bool STREAM>
-__device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* lds)
+template <class E, int D, bool STREAM, bool SEEN>
+__device__ __forceinline__ bool wide_block(const Args& g, const Job& j, char* lds)
 {
     using SH = Shape<E, D>;
     using R = Rows<E, D, 1, SH::kCodes>;
     using V = typename R::V;
     constexpr int C = SH::kChunks, kRow = SH::kRow, N = kWideKeys / 16;
     constexpr bool kCodes = SH::kCodes;
-    const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const int thread = thread_index<SEEN>(), lane = thread & (kWave - 1), col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(thread / kWave);
 
     // one range: the prefix's or the sequence's
     const bool own = j.ob > j.oa;
@@ -770,16 +875,22 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
             }
         }
     };
+    __shared__ int s_again;
+    const bool unseen = !kCodes && !SEEN && own && end > j.sees0 + j.row0 / g.G;
+    if (unseen) {
+        if (threadIdx.x == 0) s_again = 0;
+        __syncthreads();
+    }
     R rows;
     if (tiles > 0) pages_of(0);
-    rows.load(g, j, j.row0);
+    rows.load(g, j, j.row0, lane);
     if (tiles > 0) {
         request(0);
         if (tiles > 1) pages_of(1);
     }
     int at_v[D / 16];
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) at_v[d] = R::value_offset(d);
+    for (int d = 0; d < D / 16; ++d) at_v[d] = rows.value_offset(d);
     rows.arrived();
     for (int tile = 0; tile < tiles; ++tile) {
         f32x4 s[1][N];
@@ -819,27 +930,23 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
             request(tile + 1);
             if (tile + 2 < tiles) pages_of(tile + 2);
         }
-        V p[1][N / 2];
-        rows.template softmax<N>(s, p, first + tile * step, end, own, [&](int n) { return vs[n]; });
-#pragma unroll
-        for (int u = 0; u < N / 2; ++u) {
-            const V pu[1] = {p[0][u]};
-            rows.values(vt, u, pu, at_v);
-        }
+        rows.template attend<N, SEEN>(s, vt, at_v, first + tile * step, end, own, [&](int n) { return vs[n]; });
     }
     if (est && lane == 0) raise_status(g.status, est);
 
     // the wavefronts' keys of the same 16 rows
+    if (unseen && rows.not_finite() && lane == 0) s_again = 1;
     rows.finish();
     const float l = row_reduce(rows.l[0], OpAdd());
     __syncthreads();   // (every wavefront is done with its tiles)
+    if (unseen && __builtin_amdgcn_readfirstlane(s_again) != 0) return true;
     float* const so = reinterpret_cast<float*>(lds);                         // [wave][row][D]
     float* const sm = so + kWaves * kWideRows * D;                           // [wave][row][2]
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4*>(so + (wave * 16 + col) * D + ((d * 4 + grp) ^ col) * 4) = rows.o[0][d];
     if (grp == 0) { sm[(wave * 16 + col) * 2] = rows.m[0]; sm[(wave * 16 + col) * 2 + 1] = l; }
     __syncthreads();
-    for (int e = threadIdx.x; e < kWideRows * D / 4; e += kThreads) {
+    for (int e = thread; e < kWideRows * D / 4; e += kThreads) {
         const int r = e / (D / 4), d = e % (D / 4);
         if (j.row0 + r >= j.rows) continue;
         float mm = -INFINITY, ll = 0.0f;
@@ -855,6 +962,7 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
         }
         store_row<D>(g, j, j.row0 + r, d * 4, v, mm, ll);
     }
+    return false;
 }
 
 // Wavefronts a SIMD that the registers have to allow, and for which the compiler orders loads and products (with room for one more it waited for each load of a
@@ -862,16 +970,15 @@ __device__ __forceinline__ void wide_block(const Args& g, const Job& j, char* ld
 constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : MT == 1 ? 2 : 1; }
 
 // MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it.  STREAM (MT 0): keys and values past the caches (rule and figures at the launch)
-template <class E, int D, int MT, bool STREAM>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_wanted(D, MT), waves_wanted(D, MT)))) void attention_kernel(Args g)
+template <class E, int D, int MT, bool STREAM, bool SEEN>
+__device__ __forceinline__ bool attention_block(const Args& g, int block, char* lds)
 {
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const bool shared = (int)blockIdx.x < g.shared.blocks;
+    const bool shared = block < g.shared.blocks;
     const Work& w = shared ? g.shared : g.own;
-    const int id = (int)blockIdx.x - (shared ? 0 : g.shared.blocks);
+    const int id = block - (shared ? 0 : g.shared.blocks);
     // Workgroup ids go round-robin over the XCDs: all row tiles of one range of a key head to the same one, whose L2 then has the range's K and V
     const int seq = id / kXcdCount, combo = seq / w.row_tiles * kXcdCount + id % kXcdCount;
-    if (combo >= w.combos) return;
+    if (combo >= w.combos) return false;
     const int split = combo / g.Hk % w.splits, b = combo / g.Hk / w.splits;
     const int tile_rows = w.tall ? kWaves * 16 * MT : kWideRows;
     Job j;
@@ -904,7 +1011,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
         if (est && threadIdx.x == 0) raise_status(g.status, est);
         j.t0 = t0;
         j.rows = tokens * g.G;
-        if (j.row0 >= j.rows) return;
+        if (j.row0 >= j.rows) return false;
         j.sees0 = len - tokens + 1;
         j.table = g.table + (int64_t)b * g.table_ld;
         const int seen = max(0, min(len, j.sees0 + min((j.row0 + tile_rows - 1) / g.G, tokens - 1)));   // by the workgroup's last row
@@ -921,12 +1028,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
             j.ob = min((max(hi, np) - np) * kTallKeys, seen);
         }
     }
-    if constexpr (MT > 0) {
-        if (w.tall) tall_block<E, D, MT>(g, j, lds);
-        else wide_block<E, D, false>(g, j, lds);
-    } else {
-        wide_block<E, D, STREAM>(g, j, lds);
-    }
+    if constexpr (MT > 0) return w.tall ? tall_block<E, D, MT, SEEN>(g, j, lds) : wide_block<E, D, false, SEEN>(g, j, lds);
+    else return wide_block<E, D, STREAM, SEEN>(g, j, lds);
+}
+
+template <class E, int D, int MT, bool STREAM>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_wanted(D, MT), waves_wanted(D, MT)))) void attention_kernel(Args g)
+{
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    int block = (int)blockIdx.x;
+    if (!attention_block<E, D, MT, STREAM, false>(g, block, lds) || Shape<E, D>::kCodes) return;
+    // Once more, from the arguments on: nothing is kept in registers for it
+    typedef const __attribute__((address_space(4))) Args* ConstArgs;
+    ConstArgs from = (ConstArgs)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(from), "+s"(block)::"memory");
+    __syncthreads();   // (of the tiles and the flag)
+    const Args again = *(const Args*)from;
+    attention_block<E, D, MT, STREAM, true>(again, block, lds);
 }
 
 constexpr int kJoinParts = 256;

@@ -246,3 +246,21 @@ def test_steps_of_any_size(B, form, D, dt):
 @pytest.mark.parametrize("form", list(FORMS))
 def test_scores_of_any_size_over_codes(B, form, dt):
     large_scores(B, form, dt, True)
+
+
+@pytest.mark.parametrize("dt,codes", KINDS)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_values_that_are_not_finite(B, form, D, dt, codes):
+    """They reach the tokens that see their key; the same sequence's earlier tokens, whose probability of it is 0, have none of it."""
+    lens, new, prefix, Hq, Hk, joined = FORMS[form]
+    for plant in ("nan",) if codes else ("nan", "inf", "-inf"):
+        print(f"[values] {form} D={D} {dt} codes={codes} {plant} in a value", flush=True)
+        base = Batch(dt, codes, D, lens, new, prefix, Hq, Hk, seed=D)
+        for r, j in somewhere(base) + [(1, lens[0] - 1)]:
+            b = Batch(dt, codes, D, lens, new, prefix, Hq, Hk, seed=D)
+            if codes:
+                b.vs[r][j, 0] = float(plant)
+            else:
+                b.v[r][j, 0, 7] = float(plant)
+            b.check(*b.run(B, joined))
