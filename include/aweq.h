@@ -392,12 +392,13 @@ int aweq_qk_rope(const void* q, const void* k, aweq_dtype dt, int64_t T, int64_t
 /* ---- A paged cache of keys and values.  k_cache and v_cache hold `pages` pages of Hk heads of page_size tokens of D values each,
  * [pages][Hk][page_size][D], in the queries' type (F16 or BF16), or as 8-bit codes (cache_dt = AWEQ_I8) with k_step and v_step
  * [pages][Hk][page_size] fp32: the value is code * step, step = max |x| / 127 of the token's head (the smallest normal number at least; 1 for a head of
- * zeros; always positive), code = round(x / step).
+ * zeros; always positive, or NaN), code = round(x / step).
  * (Symmetric, unlike the quantizers above: a zero point would cost a correction of every score.)  page_size: a power of two from 16 to 256.
  *
  * aweq_kv_append: aweq_qk_rope, with the keys, and the values v[T][Hk][D] (pitch ldv) as they are, going to the cache: token t to row slot[t] %
  * page_size of page slot[t] / page_size (int64; negative: the token is left out of the cache, a padded batch; past the last page: the
- * same, and AWEQ_ST_INDEX).  Tokens of one call must not share a slot.  An 8-bit code is made of the rotated value before any other rounding.  q
+ * same, and AWEQ_ST_INDEX).  Tokens of one call must not share a slot.  An 8-bit code is made of the rotated value before any other rounding; a
+ * head with a NaN or an infinity gets a step of NaN and raises AWEQ_ST_NONFINITE (a cache of the values' type holds them as they are). q
  * nullable (with q_out).  D % 8 == 0 and D <= 256; dt F16 or BF16. */
 int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, int64_t T, int64_t Hq, int64_t Hk, int64_t D,
                    int64_t ldq, int64_t ldk, int64_t ldv, const int32_t* pos, const double* freq, int64_t rot, int interleaved, float gain,

@@ -116,7 +116,6 @@ __device__ __forceinline__ float row_reduce(float v, Op op)
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-struct OpMaximum { __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); } };   // (of IEEE: a NaN stays one)
 struct Larger { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
 // E: type of the cache (int8_t: codes)

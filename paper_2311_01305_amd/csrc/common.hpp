@@ -146,6 +146,9 @@ __device__ __forceinline__ void wave_lds_fence()
 
 struct OpMin { template <class T> __device__ T operator()(T a, T b) const { return a < b ? a : b; } };
 struct OpMax { template <class T> __device__ T operator()(T a, T b) const { return a > b ? a : b; } };
+// (of IEEE: a NaN stays one)
+struct OpMinimum { __device__ float operator()(float a, float b) const { return __builtin_elementwise_minimum(a, b); } };
+struct OpMaximum { __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); } };
 struct OpAdd { template <class T> __device__ T operator()(T a, T b) const { return a + b; } };
 
 // All-reduce over aligned groups of 2^LEVELS lanes (LEVELS = 6: the whole wavefront).

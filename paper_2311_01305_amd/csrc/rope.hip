@@ -44,16 +44,19 @@ struct Args {
 
 enum { kRows, kCache, kCodes };   // where keys go: rows as queries do, a cache of the same type, a cache of 8-bit codes
 
-// largest |x| of a head's values to a step, its codes and the step itself to the cache
+// largest |x| of a head's values to a step, its codes and the step itself to the cache.  False where one is not finite: the step is NaN then, and what reads
+// the head finds nothing but NaN, whatever the codes
 template <int G>
-__device__ __forceinline__ void store_codes(int8_t* dst, float* step_at, const float a[8], const float b[8], int ua, int ub, int units, bool writes_step)
+__device__ __forceinline__ bool store_codes(int8_t* dst, float* step_at, const float a[8], const float b[8], int ua, int ub, int units, bool writes_step)
 {
     float big = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) big = fmaxf(big, fmaxf(fabsf(a[i]), fabsf(b[i])));
-    big = group_allreduce<G>(big, OpMax());
-    float step = fmaxf(big / 127.0f, 1.17549435e-38f);   // (not subnormal: what reads it takes such a number for 0)
-    if (!(big > 0.0f) || isinf(step)) step = 1.0f;
+    for (int i = 0; i < 8; ++i) big = OpMaximum()(big, OpMaximum()(fabsf(a[i]), fabsf(b[i])));
+    big = group_allreduce<G>(big, OpMaximum());
+    const bool finite = big < INFINITY;
+    float step = fmaxf(big / 127.0f, 1.17549435e-38f);   // (not subnormal: the quotients keep their digits)
+    if (big == 0.0f) step = 1.0f;
+    if (!finite) step = NAN;
     if (writes_step) *step_at = step;
     auto pack = [&](const float x[8]) {
         uint32_t w[2] = {0u, 0u};
@@ -66,6 +69,7 @@ __device__ __forceinline__ void store_codes(int8_t* dst, float* step_at, const f
     };
     if (ua < units) *reinterpret_cast<uint2*>(dst + ua * 8) = pack(a);
     if (ub < units) *reinterpret_cast<uint2*>(dst + ub * 8) = pack(b);
+    return finite;
 }
 
 // STREAM: past the caches (the rule and figures at the launch)
@@ -221,8 +225,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Args g)
                 put(dst, has_a && keep, has_b && keep);
             } else {
                 const bool kept = (has_a || has_b) && keep;
-                store_codes<G>(reinterpret_cast<int8_t*>(is_v ? g.v_cache : g.k_cache) + at * g.D, (is_v ? g.v_step : g.k_step) + at, a, b,
-                               has_a && keep ? ua : units, has_b && keep ? ub : units, units, kept && lane == 0);
+                const bool finite = store_codes<G>(reinterpret_cast<int8_t*>(is_v ? g.v_cache : g.k_cache) + at * g.D, (is_v ? g.v_step : g.k_step) + at, a, b,
+                                                   has_a && keep ? ua : units, has_b && keep ? ub : units, units, kept && lane == 0);
+                if (!finite && kept && lane == 0) raise_status(g.status, AWEQ_ST_NONFINITE);
             }
         }
     }

@@ -35,8 +35,6 @@ __device__ __forceinline__ void token_extremes(const Unit<E>& u, const float is[
         hi = __builtin_elementwise_maximum(__builtin_elementwise_maximum(hi, a), b);
     }
 }
-struct OpMinimum { __device__ float operator()(float a, float b) const { return __builtin_elementwise_minimum(a, b); } };
-struct OpMaximum { __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); } };
 
 // Eq. 2 for a range that contains 0.  A range so small that its 255th part is subnormal would leave steps of too few digits for a zero point in
 // [0, 255]: clamped (its values are below 1e-36)
