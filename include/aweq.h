@@ -358,8 +358,8 @@ int aweq_quant_tokens(const void* X, aweq_dtype dt, int64_t T, int64_t K, int64_
  * are inputs (zero_x in [0, 255], as aweq_quant_tokens writes them).  wq, step_w, zero_w, w_group, rowsum_w, bias (nullable): the
  * weight as in aweq_w8a8_gemm.
  *   out[t,n] = step_x[t] step_w[n] (acc - Z'x[t] rowsum_w[n] - Z'w[n] rowsum_x[t] + K Z'x[t] Z'w[n]) + bias[n],  Z' = Z - 128,
- * the integer exact in 32 bits (zero_w outside [0, 255]: AWEQ_ST_ZEROPOINT, as there), scaled in fp64 and rounded once to out_dt (F32, F16,
- * BF16; pitch ldo).  K % 8 == 0, K <= 32768, N % 4 == 0, ldo % 4 == 0, 16-byte aligned pointers. */
+ * the integer exact in 32 bits (zero_w outside [0, 255]: AWEQ_ST_ZEROPOINT, as there), scaled in fp64, rounded to fp32 and from there to out_dt
+ * (F32, F16, BF16; pitch ldo).  K % 8 == 0, K <= 32768, N % 4 == 0, ldo % 4 == 0, 16-byte aligned pointers. */
 int aweq_w8a8_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, int64_t K, int64_t ldx, const float* inv_s,
                           int8_t* xq, float* step_x, int32_t* zero_x, int32_t* rowsum_x,
                           const int8_t* wq, int64_t N, const float* step_w, const int32_t* zero_w, int w_group,

@@ -702,7 +702,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
             for (int c = 0; c < 4; ++c) {
                 if constexpr (TOK) {   // (|Z'x| and |A| fit 24 bits as well)
                     const int iv = (int)((unsigned)o[c] + (unsigned)__mul24(nzw[c], rs >> 8) - (unsigned)__mul24((int)cn[c], (int)(int8_t)rs));
-                    y[c] = DEQ == 1 ? token_scaled_f32(iv, sx, sw.f[c], bs.f[c]) : token_scaled(iv, sx, sw.f[c], bs.f[c]);
+                    y[c] = token_scaled(iv, sx, sw.f[c], bs.f[c]);
                     continue;
                 }
                 const double div = (double)(int)((unsigned)o[c] + cn[c] + (unsigned)__mul24(nzw[c], rs));
@@ -903,7 +903,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
                             for (int c = 0; c < 4; ++c) {
                                 if constexpr (TOK) {
                                     const int iv = token_integer(o[c], (int)(int8_t)rs, cn[c], nzw[c], (int)rs >> 8);
-                                    y[c] = DEQ == 1 ? token_scaled_f32(iv, sx, sw.f[c], bs.f[c]) : token_scaled(iv, sx, sw.f[c], bs.f[c]);
+                                    y[c] = token_scaled(iv, sx, sw.f[c], bs.f[c]);
                                     continue;
                                 }
                                 // |row sum| <= 128 K < 2^23 and |Z'w| < 2^23 for any zero point binary16 weights can

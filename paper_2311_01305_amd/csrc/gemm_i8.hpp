@@ -91,17 +91,13 @@ MidPlan plan_mid(int64_t T, int64_t N);
 int launch_gemm_i8_mid(const GemmArgs& g, const MidPlan& p, hipStream_t st, bool tokens = false);
 
 // The output of a product whose tokens have scales of their own: acc - Z'x A - Z'w rowsum_x, A = rowsum_w - K Z'w, in wrap-around 32 bits (nzw
-// = -Z'w), and its scaling, the same in every form: binary16 and bfloat16 in fp32 (its roundings, 2^-23 together, are far inside the
-// output's), binary32 in fp64
+// = -Z'w), and its scaling, the same in every form: in fp64 (the steps' product is exact there, and a bias may cancel what it is added to), rounded to fp32 and
+// from there to a 16-bit output
 __device__ __forceinline__ int token_integer(int acc, int zx, unsigned a, int nzw, int rowsum_x)
 {
     return (int)((unsigned)acc - (unsigned)zx * a + (unsigned)nzw * (unsigned)rowsum_x);
 }
-__device__ __forceinline__ float token_scaled(int i, float sx, float sw, float bias) { return __builtin_fmaf((float)i, sx * sw, bias); }
-__device__ __forceinline__ float token_scaled_f32(int i, float sx, float sw, float bias)
-{
-    return (float)((double)i * ((double)sx * (double)sw) + (double)bias);
-}
+__device__ __forceinline__ float token_scaled(int i, float sx, float sw, float bias) { return (float)__builtin_fma((double)i, (double)sx * (double)sw, (double)bias); }
 
 // Time of one round of workgroups at K = 8192 (us; every kernel's time is close to proportional to K): 256 tiles of 256 x 256
 constexpr double kTiledRoundCost = 100.0;

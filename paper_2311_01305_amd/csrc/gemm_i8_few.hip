@@ -337,8 +337,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
             for (int c = 0; c < 4; ++c) {
                 if constexpr (TOK) {
                     const int iv = token_integer(o[c], s_zx[tl], s_cn[nl + c], -(int)s_zw[nl + c], (int)rs);
-                    y[c] = g.out_f16 == kOutF32 ? token_scaled_f32(iv, s_sx[tl], s_sw[nl + c], (float)s_bias[nl + c])
-                                                : token_scaled(iv, s_sx[tl], s_sw[nl + c], (float)s_bias[nl + c]);
+                    y[c] = token_scaled(iv, s_sx[tl], s_sw[nl + c], (float)s_bias[nl + c]);
                     continue;
                 }
                 const double div = (double)(int)((unsigned)o[c] + s_cn[nl + c] - s_zw[nl + c] * rs);

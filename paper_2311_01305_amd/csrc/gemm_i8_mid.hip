@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
             for (int c = 0; c < 4; ++c) {
                 if constexpr (TOK) {
                     const int iv = token_integer(o[c], zxx[i], cn[c], -zw[c], rsx[i]);
-                    y[c] = g.out_f16 == kOutF32 ? token_scaled_f32(iv, sxx[i], sw[c], bs[c]) : token_scaled(iv, sxx[i], sw[c], bs[c]);
+                    y[c] = token_scaled(iv, sxx[i], sw[c], bs[c]);
                     continue;
                 }
                 const double div = (double)(int)((unsigned)o[c] + cn[c] - (unsigned)zw[c] * (unsigned)rsx[i]);
