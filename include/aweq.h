@@ -355,7 +355,7 @@ int aweq_quant_tokens(const void* X, aweq_dtype dt, int64_t T, int64_t K, int64_
 
 /* ---- Product in 8-bit integers with a (Step, Z) for each token and each output channel.  X F32 / F16 / BF16 is quantised by
  * aweq_quant_tokens first (xq, step_x, zero_x, rowsum_x are written); X I8 (ldx = K) already is xq, and step_x, zero_x, rowsum_x
- * are inputs (zero_x in [0, 255], as aweq_quant_tokens writes them).  wq, step_w, zero_w, w_group, rowsum_w, bias (nullable): the
+ * are inputs (zero_x in [0, 255], as aweq_quant_tokens writes them; outside: clamped, and AWEQ_ST_ZEROPOINT).  wq, step_w, zero_w, w_group, rowsum_w, bias (nullable): the
  * weight as in aweq_w8a8_gemm.
  *   out[t,n] = step_x[t] step_w[n] (acc - Z'x[t] rowsum_w[n] - Z'w[n] rowsum_x[t] + K Z'x[t] Z'w[n]) + bias[n],  Z' = Z - 128,
  * the integer exact in 32 bits (zero_w outside [0, 255]: AWEQ_ST_ZEROPOINT, as there), scaled in fp64, rounded to fp32 and from there to out_dt

@@ -562,7 +562,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_fast(Args g)
                 const int64_t t = cm0 + wm * (32 * MI) + hh * 64 + lane;
                 rsx[hh] = t < g.T ? g.rowsum_x[t] : 0;
                 if constexpr (TOK) {
-                    rsx[hh] = (int)((unsigned)rsx[hh] << 8) | ((t < g.T ? g.act_zero[t] - 128 : 0) & 255);   // (|row sum| <= 2^22)
+                    rsx[hh] = (int)((unsigned)rsx[hh] << 8) | ((t < g.T ? token_zero(g.act_zero[t], est) : 0) & 255);   // (|row sum| <= 2^22)
                     sxx[hh] = t < g.T ? g.act_step[t] : 0.0f;
                 }
             }

@@ -97,6 +97,13 @@ __device__ __forceinline__ int token_integer(int acc, int zx, unsigned a, int nz
 {
     return (int)((unsigned)acc - (unsigned)zx * a + (unsigned)nzw * (unsigned)rowsum_x);
 }
+// a token's Z' = Z - 128; Z outside [0, 255] is reported and clamped
+__device__ __forceinline__ int token_zero(int zero, uint32_t& est)
+{
+    const int z = min(max(zero, 0), 255);
+    if (z != zero) est |= AWEQ_ST_ZEROPOINT;
+    return z - 128;
+}
 __device__ __forceinline__ float token_scaled(int i, float sx, float sw, float bias) { return (float)__builtin_fma((double)i, (double)sx * (double)sw, (double)bias); }
 
 // Time of one round of workgroups at K = 8192 (us; every kernel's time is close to proportional to K): 256 tiles of 256 x 256

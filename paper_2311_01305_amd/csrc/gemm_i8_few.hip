@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_few(GemmArgs g, typename std
             s_zw[threadIdx.x] = (unsigned)zw;
         } else if (QX == 0 && e_tok >= 0 && e_tok < kTokens) {
             s_rx[e_tok] = (unsigned)e_rw;
-            if constexpr (TOK) { s_sx[e_tok] = e_sx; s_zx[e_tok] = zx; }
+            if constexpr (TOK) { s_sx[e_tok] = e_sx; s_zx[e_tok] = token_zero(e_zx, est); }
         }
     }
     __syncthreads();

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
         for (int i = 0; i < kRows; ++i) {
             const int64_t t = min(m0 + er + i * kRowStep, g.T - 1);
             rsx[i] = g.rowsum_x[t];
-            if constexpr (TOK) { zxx[i] = g.act_zero[t] - 128; sxx[i] = g.act_step[t]; }
+            if constexpr (TOK) { zxx[i] = g.act_zero[t]; sxx[i] = g.act_step[t]; }
         }
     }
 
@@ -196,6 +196,9 @@ __global__ __launch_bounds__(kThreads) void gemm_i8_mid(GemmArgs g)
     if (deq) {
         // the tiled kernel's arithmetic: the integer part in wrap-around 32 bits, scaled and shifted in fp64
         if (zx < -128 || zx > 127) est |= AWEQ_ST_ZEROPOINT;
+        if constexpr (TOK)
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) zxx[i] = token_zero(zxx[i], est);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             if (zw[c] < -128 || zw[c] > 127) est |= AWEQ_ST_ZEROPOINT;

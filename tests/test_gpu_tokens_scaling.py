@@ -94,3 +94,20 @@ def test_steps_whose_product_is_small(B, T, N, K):
         assert float((codes[1].double().max() * layer.d[1].double().max())) < 2.0 ** -126 < float(want.abs().max())
         allowed = (UNIT[out] * 1.001 + 2.0 ** -24) * want.abs() + TINY[out] + 2.0 ** -149
         assert bool(((y - want).abs() <= allowed).all()), (out, float(((y - want).abs() / allowed).max()))
+
+
+@pytest.mark.parametrize("T,N,K", SHAPES)
+def test_zero_points_that_no_token_can_have(B, T, N, K):
+    """Given codes whose zero point is outside [0, 255] are reported and taken as if it were the nearest inside, whatever form the sizes lead to."""
+    layer = Layer(N, K, T + N)
+    x = torch.randn(T, K, device=DEV).half()
+    _, codes, status = layer.call(B, x, "f16", "f16", None)
+    assert status == 0
+    for zero in (-1, 256, 300, -20000):
+        print(f"[scaling] zero T={T} N={N} K={K} {zero}", flush=True)
+        outside, inside = codes[2].clone(), codes[2].clone()
+        outside[T // 2], inside[T // 2] = zero, min(max(zero, 0), 255)
+        y, _, status = layer.call(B, x, "f16", "f32", None, [codes[0], codes[1], outside, codes[3]])
+        want, _, none = layer.call(B, x, "f16", "f32", None, [codes[0], codes[1], inside, codes[3]])
+        assert status == B.ST_ZEROPOINT and none == 0
+        assert torch.equal(y, want)
