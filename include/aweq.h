@@ -424,8 +424,10 @@ int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, i
  * of two, and probabilities times their value's step by one for each token and head, which follows the largest step that it sees: a step says nothing of its
  * key's weight; a step of a value that is not finite makes the out of what sees it NaN).  D 64, 128 or 256; Hq a multiple of Hk; scale > 0;
  * cache as above.
- * ws: aweq_prefix_attention_ws(...) bytes, 16-byte aligned (host function). */
+ * ws: aweq_prefix_attention_ws(...) bytes, 16-byte aligned (host function; 0: none is needed).  A smaller call may need more, since fewer rows are split into
+ * more ranges: aweq_prefix_attention_ws_most is enough for every call with no more of T, B, max_q, prefix_len and max_len whose T is at most its B max_q. */
 size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len);
+size_t aweq_prefix_attention_ws_most(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len);
 int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int64_t D, int64_t ldq,
                           const void* k_cache, const void* v_cache, const float* k_step, const float* v_step, aweq_dtype cache_dt,
                           int64_t pages, int64_t page_size, int64_t Hk, const int32_t* prefix_table, int64_t prefix_len,

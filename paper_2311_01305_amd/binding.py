@@ -28,7 +28,7 @@ EXPORTS = ("aweq_workspace_size", "aweq_status_string", "aweq_calib_stats", "awe
            "aweq_quant_weight", "aweq_quant_act", "aweq_w8a8_gemm", "aweq_bias_correct",
            "aweq_panel_bytes", "aweq_pack_panels_i8", "aweq_unpack_panels_i8", "aweq_wonly_gemm", "aweq_fold_quant_weight", "aweq_w8a8_gemm_fused",
            "aweq_calib_stats_static", "aweq_calibrate", "aweq_quant_tokens", "aweq_w8a8_gemm_tokens", "aweq_rope_frequencies", "aweq_qk_rope",
-           "aweq_kv_append", "aweq_prefix_attention_ws", "aweq_prefix_attention")
+           "aweq_kv_append", "aweq_prefix_attention_ws", "aweq_prefix_attention_ws_most", "aweq_prefix_attention")
 STATIC_SCRATCH_BYTES = 16 << 20
 
 _vp, _i64, _i32, _u64, _f32, _f64, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_uint64, C.c_float, C.c_double, C.c_size_t
@@ -66,8 +66,9 @@ def load_library():
     lib.aweq_unpack_panels_i8.argtypes = [_vp, _i64, _i64, _vp, _i64, _vp]
     lib.aweq_rope_frequencies.restype = _i32
     lib.aweq_rope_frequencies.argtypes = [_i64, _f64, _i32, _f64, _f64, _f64, _f64, _vp]
-    lib.aweq_prefix_attention_ws.restype = _sz
-    lib.aweq_prefix_attention_ws.argtypes = [_i64] * 8
+    for name in ("aweq_prefix_attention_ws", "aweq_prefix_attention_ws_most"):
+        getattr(lib, name).restype = _sz
+        getattr(lib, name).argtypes = [_i64] * 8
     spec = importlib.util.spec_from_loader("_native", importlib.machinery.ExtensionFileLoader("_native", _NATIVE_PATH))
     calls = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(calls)
@@ -252,6 +253,10 @@ def aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, ldq, ldk, ldv, pos, freq, rot, int
 
 def aweq_prefix_attention_ws(T, Hq, Hk, D, B, max_q, prefix_len, max_len):
     return int(load_library().aweq_prefix_attention_ws(int(T), int(Hq), int(Hk), int(D), int(B), int(max_q), int(prefix_len), int(max_len)))
+
+
+def aweq_prefix_attention_ws_most(T, Hq, Hk, D, B, max_q, prefix_len, max_len):
+    return int(load_library().aweq_prefix_attention_ws_most(int(T), int(Hq), int(Hk), int(D), int(B), int(max_q), int(prefix_len), int(max_len)))
 
 
 def aweq_prefix_attention(q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, prefix_table, prefix_len, table,

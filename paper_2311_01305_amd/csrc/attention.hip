@@ -1143,10 +1143,11 @@ static int64_t split_count(int64_t items, int64_t len, int64_t want, int64_t lea
 // Tall workgroups: one for each compute unit, of 512 keys or more, or two, which overlap one's products with the other's exponentials, where that leaves
 // 1024 keys: a range's rows are written and read once more to be joined (us, one -> two: 1024 rows a key head against 16384 keys 95 -> 82, but 256 rows
 // against 8192 23.1 -> 25.1, and with the batch's own keys in the same launch 38.2 -> 47.1).  Ranges of 256 keys where most compute units had none.
+constexpr int64_t kTallWant = 512, kTallLeast = 256, kWideWant = 2048, kWideLeast = 128;
 static int64_t tall_splits(int64_t items, int64_t len)
 {
-    const int64_t one = split_count(items, len, 256, 512), two = split_count(items, len, 512, 1024);
-    if (items * one < 64) return split_count(items, len, 256, 256);
+    const int64_t one = split_count(items, len, kTallWant / 2, 2 * kTallLeast), two = split_count(items, len, kTallWant, 4 * kTallLeast);
+    if (items * one < 64) return split_count(items, len, kTallWant / 2, kTallLeast);
     return one > two ? one : two;
 }
 // Wide workgroups: eight for each compute unit (sequences differ in length; two for a single range), of 512 keys or more, or of less where most compute units had none (us, 256 ->
@@ -1154,8 +1155,8 @@ static int64_t tall_splits(int64_t items, int64_t len)
 static int64_t wide_splits(int64_t items, int64_t len, bool one)
 {
     int64_t n = 1;
-    for (int64_t least = 512; least >= 128; least /= 2) {
-        n = split_count(items, len, one ? 512 : 2048, least);
+    for (int64_t least = 4 * kWideLeast; least >= kWideLeast; least /= 2) {
+        n = split_count(items, len, one ? kWideWant / 4 : kWideWant, least);
         if (items * n >= 256) break;
     }
     return n;
@@ -1249,6 +1250,15 @@ static int launch_head(Args& g, const Plan& p, int64_t D, hipStream_t st)
     return launch<E, 256>(g, p, st);
 }
 
+// Rows (a token's query head) times ranges of one kind, at most, for up to `rows` of them and `len` keys.  The work items' tiles hold all rows, so that `want`
+// workgroups of at most `tile` rows each, and one range more (rounding up), have no more; nor has a row more ranges than the keys allow.
+static int64_t most_parts(int64_t rows, int64_t len)
+{
+    static_assert(kTallWant * kWaves * 32 >= kWideWant * kWideRows && kTallLeast >= kWideLeast, "the tall form has the larger product, the wide one the shorter ranges");
+    const int64_t ranges = cdiv(len, kWideLeast), by_keys = rows * (ranges < kMostSplits ? ranges : kMostSplits), by_work = kTallWant * kWaves * 32 + rows;
+    return by_keys < by_work ? by_keys : by_work;
+}
+
 static bool shapes_ok(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len)
 {
     if (T <= 0 || Hq <= 0 || Hk <= 0 || Hq % Hk != 0 || (D != 64 && D != 128 && D != 256) || B <= 0 || max_q <= 0) return false;
@@ -1271,6 +1281,14 @@ extern "C" size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, in
         if (n > parts) parts = n;
     }
     return parts > 1 ? (size_t)parts * (size_t)(T * Hq) * (size_t)(D * 4 + 8) : 0;
+}
+
+extern "C" size_t aweq_prefix_attention_ws_most(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len)
+{
+    if (!attn::shapes_ok(T, Hq, Hk, D, B, max_q, prefix_len, max_len)) return 0;
+    if (prefix_len == 0 && max_len <= attn::kWideLeast) return 0;
+    const int64_t rows = T * Hq, own = attn::most_parts(rows, max_len + prefix_len);   // (a sequence's rows may take the prefix along)
+    return (size_t)(attn::most_parts(rows, prefix_len) + (own > rows ? own : rows)) * (size_t)(D * 4 + 8);
 }
 
 extern "C" int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int64_t D, int64_t ldq,

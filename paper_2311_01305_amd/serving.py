@@ -86,14 +86,18 @@ class AttentionBlock:
         self.q = new(max_tokens, q_heads * D, dtype=cache.dtype)
         self.attended = new(max_tokens, q_heads * D, dtype=cache.dtype)
         self.y = new(max_tokens, out.N, dtype=cache.dtype)
-        self.ws = new(16, dtype=torch.uint8)
+        self.ws, self.kept = new(16, dtype=torch.uint8), []
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
     def reserve(self, tokens, batch, max_q, prefix_len, max_len):
-        """Scratch memory for steps of these bounds, so that none is allocated later (a captured graph keeps its address)."""
-        need = B.aweq_prefix_attention_ws(tokens, self.q_heads, self.cache.heads, self.cache.head_dim, batch, max_q, prefix_len, max_len)
+        """Scratch memory for steps of up to these bounds, so that none is allocated later."""
+        self._scratch(B.aweq_prefix_attention_ws_most(tokens, self.q_heads, self.cache.heads, self.cache.head_dim, batch, max_q, prefix_len, max_len))
+
+    def _scratch(self, need):
+        """What was handed out before stays as it is: a captured graph writes there.  Twice as much each time, so that all of it is no more than the last."""
         if need > self.ws.numel():
-            self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self.kept.append(self.ws)
+            self.ws = torch.empty(max(need, 2 * self.ws.numel()), dtype=torch.uint8, device=self.device)
 
     def _product(self, layer, x, out):
         T, dt = x.shape[0], DTYPES[x.dtype]
@@ -114,7 +118,7 @@ class AttentionBlock:
         B.aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, width, width, width, pos, self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm,
                          self.eps, self.q, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, slot, self.status)
         batch = lens.shape[0]
-        self.reserve(T, batch, max_q, prefix_len, max_len)
+        self._scratch(B.aweq_prefix_attention_ws(T, Hq, Hk, D, batch, max_q, prefix_len, max_len))
         B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
                                 table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
         self._product(self.out_layer, self.attended[:T], self.y)
