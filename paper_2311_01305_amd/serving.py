@@ -68,6 +68,12 @@ class PagedCache:
         return [pages[i // s] * s + i % s for i in range(first, first + count)]
 
 
+def _check(name, t, dtype, shape, longer=False):
+    """What the library reads by its address alone."""
+    if t is None or t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or (tuple(t.shape) < shape if longer else tuple(t.shape) != shape):
+        raise ValueError(f"{name}: {dtype} {list(shape)}{' or longer' if longer else ''}, in one piece")
+
+
 class AttentionBlock:
     """qkv [(Hq + 2 Hk) D x hidden] and out [hidden x Hq D]; buffers for max_tokens tokens of a step, allocated once."""
 
@@ -76,6 +82,11 @@ class AttentionBlock:
         D, Hk = cache.head_dim, cache.heads
         if qkv.N != (q_heads + 2 * Hk) * D or out.K != q_heads * D:
             raise ValueError("the projections' sizes are not those of the heads")
+        if rot:
+            _check("freq", freq, torch.float64, (rot // 2,))
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None:
+                _check(name, w, torch.float32, (D,))
         self.qkv_layer, self.out_layer, self.q_heads, self.cache = qkv, out, q_heads, cache
         self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm, self.eps = freq, rot, interleaved, gain, q_norm, k_norm, eps
         self.max_tokens, self.device = max_tokens, device
@@ -110,6 +121,20 @@ class AttentionBlock:
         T, c = x.shape[0], self.cache
         if T > self.max_tokens or x.dtype != c.dtype:
             raise ValueError("more tokens than max_tokens, or another type than the cache's")
+        batch = lens.shape[0]
+        if T == 0 or x.dim() != 2 or x.shape[1] != self.qkv_layer.K or x.stride(1) != 1:
+            raise ValueError("x: [tokens, hidden], one token at least, each in one piece")
+        if self.rot:
+            _check("pos", pos, torch.int32, (T,))
+        _check("slot", slot, torch.int64, (T,))
+        _check("lens", lens, torch.int32, (batch,))
+        if q_start is not None:
+            _check("q_start", q_start, torch.int32, (batch + 1,))
+        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: int32 [sequences, pages], each row in one piece")
+        if prefix_len:
+            _check("prefix_table", prefix_table, torch.int32, (-(-prefix_len // c.page_size),), longer=True)
+        max_len = min(max_len, table.shape[1] * c.page_size)   # (a view's pitch may be more than its pages)
         dt = DTYPES[x.dtype]
         Hq, Hk, D = self.q_heads, c.heads, c.head_dim
         width = self.qkv_layer.N
@@ -117,7 +142,6 @@ class AttentionBlock:
         q, k, v = self.qkv[:T].split([Hq * D, Hk * D, Hk * D], 1)
         B.aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, width, width, width, pos, self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm,
                          self.eps, self.q, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, slot, self.status)
-        batch = lens.shape[0]
         self._scratch(B.aweq_prefix_attention_ws(T, Hq, Hk, D, batch, max_q, prefix_len, max_len))
         B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
                                 table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
