@@ -192,8 +192,9 @@ def main(argv=None):
     # the prompt once, as one sequence of its own
     pages = cache.take(a.prefix)
     x = torch.randn(a.prefix, a.hidden, device=dev).half()
-    block(x, torch.arange(a.prefix, dtype=torch.int32, device=dev), ints(cache.slots(pages, 0, a.prefix), torch.int64), ints([a.prefix]), ints([pages]),
-          ints([0, a.prefix]), a.prefix, a.prefix)
+    if a.prefix:
+        block(x, torch.arange(a.prefix, dtype=torch.int32, device=dev), ints(cache.slots(pages, 0, a.prefix), torch.int64), ints([a.prefix]), ints([pages]),
+              ints([0, a.prefix]), a.prefix, a.prefix)
     # then the batch behind it, a token each
     own = [cache.take(a.steps) for _ in range(a.batch)]
     table, shared = ints(own), ints(pages)
