@@ -34,11 +34,23 @@ class QuantLinear:
     w_group: int = 0
 
     @classmethod
-    def from_layer(cls, buf: pipeline.LayerBuffers, fold: bool = True):
+    def from_layer(cls, buf: pipeline.LayerBuffers, fold: bool = True, bias: Optional[torch.Tensor] = None, correct: bool = True):
+        """bias: the layer's own, before any correction.  correct: with the mean error that its weights' codes make on the calibration tokens taken off
+        (Eq. 12-15).  (The calibration's bias_out has the mean error of its static activation quantizer in it as well, which is not the tokens' here.)"""
         t = buf.t
         if buf.bits != 8 or buf.group > 0:
             raise ValueError("8-bit weights with a scale for each output channel or the tensor")
-        return cls(buf.N, buf.K, t["codes"], t["step_w"], t["zero_w"], t["rowsum_w"], t["bias_out"], t["inv_s"] if fold else None, buf.group)
+        return cls(buf.N, buf.K, t["codes"], t["step_w"], t["zero_w"], t["rowsum_w"], _bias(t, t, buf.N, buf.K, buf.group, bias) if correct else bias,
+                   t["inv_s"] if fold else None, buf.group)
+
+
+def _bias(t, layer, N, K, group, bias):
+    """A bias less the mean output of what its layer's codes are off the folded weight by."""
+    W = layer["W_hat"]
+    delta, out = torch.empty_like(layer["bias_out"]), torch.empty_like(layer["bias_out"])
+    B.aweq_bias_correct(B.BIAS_WEIGHT_ONLY, W, pipeline._dt(W), N, K, W.stride(0), t["mu_xhat"], 0, None, None, None, None, None, layer["codes"], 8, group,
+                        layer["step_w"], layer["zero_w"], bias, delta, out, True, t["status"])
+    return out
 
 
 class PagedCache:
@@ -159,7 +171,7 @@ def frequencies(rot: int, base: float = 10000.0, kind: int = B.ROPE_PLAIN, devic
 
 
 def calibrated(N, K, seed, tokens=512, dtype=torch.float16, device="cuda:0") -> QuantLinear:
-    """A random layer calibrated on random activations with loud channels."""
+    """A random layer without a bias, calibrated on random activations with loud channels."""
     g = torch.Generator(device=device)
     g.manual_seed(seed)
     x = torch.randn(tokens, K, generator=g, device=device)
@@ -167,9 +179,7 @@ def calibrated(N, K, seed, tokens=512, dtype=torch.float16, device="cuda:0") -> 
     w = torch.randn(N, K, generator=g, device=device) * K ** -0.5
     buf = pipeline.LayerBuffers(tokens, K, N, torch.float16, want_out_i32=False, device=device)
     pipeline.calibrate_layer(x.half(), w.half(), None, buf, forward=False)
-    layer = QuantLinear.from_layer(buf)
-    layer.bias = None
-    return layer
+    return QuantLinear.from_layer(buf, correct=False)
 
 
 def main(argv=None):
