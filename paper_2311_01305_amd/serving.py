@@ -10,7 +10,7 @@ behind it.  No arithmetic of the operators happens here.
 import argparse
 import time
 from dataclasses import dataclass
-from typing import List, Optional
+from typing import List, Optional, Sequence
 
 import torch
 
@@ -22,7 +22,8 @@ DTYPES = {torch.float16: B.AWEQ_F16, torch.bfloat16: B.AWEQ_BF16}
 
 @dataclass
 class QuantLinear:
-    """An 8-bit layer as pipeline.calibrate_layer leaves it.  inv_s: the equalization's 1 / s, or None where what produces the input has it folded in."""
+    """An 8-bit layer as pipeline.calibrate_layer leaves it, or several that read the same input as one.  inv_s: the equalization's 1 / s, or None where what
+    produces the input has it folded in."""
     N: int
     K: int
     codes: torch.Tensor
@@ -42,6 +43,21 @@ class QuantLinear:
             raise ValueError("8-bit weights with a scale for each output channel or the tensor")
         return cls(buf.N, buf.K, t["codes"], t["step_w"], t["zero_w"], t["rowsum_w"], _bias(t, t, buf.N, buf.K, buf.group, bias) if correct else bias,
                    t["inv_s"] if fold else None, buf.group)
+
+    @classmethod
+    def from_group(cls, gb: pipeline.GroupBuffers, fold: bool = True, biases: Optional[Sequence] = None, correct: bool = True):
+        """The layers of pipeline.calibrate_group side by side as one, such as queries, keys and values; biases: of each, as in from_layer."""
+        biases = [None] * len(gb.Ns) if biases is None else list(biases)
+        if len(biases) != len(gb.Ns):
+            raise ValueError("a bias, or None, for each layer")
+        join = lambda name: torch.cat([p[name] for p in gb.per])
+        codes = torch.cat([p["codes"].view(-1, N, 64) for p, N in zip(gb.per, gb.Ns)], 1).flatten()      # (panels of 64 inputs, the channels in each)
+        if correct:
+            biases = [_bias(gb.t, p, N, gb.K, 0, b) for p, N, b in zip(gb.per, gb.Ns, biases)]
+        elif any(b is not None for b in biases):
+            biases = [torch.zeros_like(p["step_w"]) if b is None else b for p, b in zip(gb.per, biases)]
+        bias = None if biases[0] is None else torch.cat(biases)
+        return cls(sum(gb.Ns), gb.K, codes, join("step_w"), join("zero_w"), join("rowsum_w"), bias, gb.t["inv_s"] if fold else None, 0)
 
 
 def _bias(t, layer, N, K, group, bias):

@@ -1,4 +1,4 @@
-"""Calibrated layers on their way into the served block: their biases against the formula in 64 bits."""
+"""Calibrated layers on their way into the served block: their biases against the formula in 64 bits, and those of a group as one layer against each by itself."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -69,7 +69,40 @@ def test_a_layers_bias(S, with_bias, group):
     assert bool(((off.double() - want[None, :]).abs() <= 2.0 ** -22 * product(S, plain, x).abs().amax()).all())
 
 
+@pytest.mark.parametrize("which", ["none", "some", "all", "not corrected"])
+def test_layers_of_a_group_as_one(S, which):
+    from paper_2311_01305_amd import pipeline
+    torch.manual_seed(12)
+    T, K, Ns, D = 200, 264, (256, 128, 128), 64
+    x = activations(T, K)
+    ws = [torch.randn(N, K, device=DEV).half() for N in Ns]
+    biases = [torch.randn(N, device=DEV) if which in ("all", "not corrected") or (which == "some" and i == 1) else None for i, N in enumerate(Ns)]
+    gb = pipeline.GroupBuffers(T, K, Ns, torch.float16, device=DEV)
+    pipeline.calibrate_group(x, ws, biases, gb)
+    whole = S.QuantLinear.from_group(gb, biases=biases, correct=which != "not corrected")
+    parts, first = [], 0
+    for p, N, b in zip(gb.per, Ns, biases):
+        if which == "not corrected":
+            assert torch.equal(whole.bias[first:first + N], b)
+        else:
+            near(whole.bias[first:first + N], expected_bias(gb.t, p, N, K, b))
+        one = S.QuantLinear(N, K, p["codes"], p["step_w"], p["zero_w"], p["rowsum_w"], whole.bias[first:first + N].clone(), gb.t["inv_s"])
+        parts.append(product(S, one, x))
+        first += N
+    assert torch.equal(product(S, whole, x), torch.cat(parts, 1))
+    # four query heads and two key heads of 64: what the block wants in one
+    cache = S.PagedCache(4, 16, 2, D, device=DEV)
+    block = S.AttentionBlock(whole, S.calibrated(K, 4 * D, 2), 4, cache, S.frequencies(D, device=DEV), D, 8, device=DEV)
+    ints = lambda v, dtype=torch.int32: torch.tensor(v, dtype=dtype, device=DEV)
+    pages = cache.take(3)
+    y = block(x[:3], ints([0, 1, 2]), ints(cache.slots(pages, 0, 3), torch.int64), ints([3]), ints([pages]), ints([0, 3]), 3, 3)
+    assert y.shape == (3, K) and bool(torch.isfinite(y).all()) and int(block.status.item()) == 0
+
+
 def test_refusals(S):
     from paper_2311_01305_amd import pipeline
+    gb = pipeline.GroupBuffers(8, 64, (64, 64), torch.float16, device=DEV)
+    with pytest.raises(ValueError):
+        S.QuantLinear.from_group(gb, biases=[None])
     with pytest.raises(ValueError):
         S.QuantLinear.from_layer(pipeline.LayerBuffers(8, 128, 64, torch.float16, bits=4, group=128, w8a8=False, device=DEV))
