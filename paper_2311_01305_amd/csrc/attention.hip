@@ -1304,7 +1304,7 @@ extern "C" int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, in
     if (!attn::shapes_ok(T, Hq, Hk, D, B, max_q, prefix_len, max_len)) return AWEQ_ERR_SHAPE;
     max_q = max_q < T ? max_q : T;
     if (pages <= 0 || pages > 0x7fffffff || page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0) return AWEQ_ERR_SHAPE;
-    if (!(scale > 0.0f) || std::isinf(scale)) return AWEQ_ERR_SHAPE;
+    if (!(scale > 0.0f) || !(scale < 0x1p127f)) return AWEQ_ERR_SHAPE;   // (to base 2 it has to be finite)
     if (ldq < Hq * D || ldo < Hq * D || (!q_start && (T != B || max_q != 1)) || (max_len > 0 && table_ld < 1)) return AWEQ_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(out) || (ldq % 8) != 0 || (ldo % 8) != 0 || !aligned16(k_cache) || !aligned16(v_cache) ||
         (cache_dt == AWEQ_I8 && (!aligned16(k_step) || !aligned16(v_step))))
