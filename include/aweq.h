@@ -422,8 +422,9 @@ int aweq_kv_append(const void* q, const void* k, const void* v, aweq_dtype dt, i
  * workgroups whose partial results (fp32, in ws) a second launch joins.  Scores and softmax in fp32, with products of the stored
  * type exact in fp32; the probabilities are rounded to F16 / BF16 for the product with v (an 8-bit cache: both products in F16, BF16 queries scaled by a power
  * of two, and probabilities times their value's step by one for each token and head, which follows the largest step that it sees: a step says nothing of its
- * key's weight; a step of a value that is not finite makes the out of what sees it NaN).  D 64, 128 or 256; Hq a multiple of Hk; scale > 0, below 2^127;
- * cache as above.
+ * key's weight; a step of a value that is not finite makes the out of what sees it NaN).  D 64, 128 or 256; Hq a multiple of Hk; scale > 0, below 2^127; cache as
+ * above (aweq_kv_append fills heads of other sizes too, which this does not read).  At most: T Hq 2^24 - 1, B Hk 2^24, B 2^20, Hq 2^16, prefix_len and
+ * max_len 2^29, pages 2^31 - 1, workgroups of a launch (sequences or the prefix, key heads, ranges of keys, row tiles) 2^24 - 1; AWEQ_ERR_SHAPE beyond, and 0 from the two functions below.
  * ws: aweq_prefix_attention_ws(...) bytes, 16-byte aligned (host function; 0: none is needed).  A smaller call may need more, since fewer rows are split into
  * more ranges: aweq_prefix_attention_ws_most is enough for every call with no more of T, B, max_q, prefix_len and max_len whose T is at most its B max_q. */
 size_t aweq_prefix_attention_ws(int64_t T, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t max_q, int64_t prefix_len, int64_t max_len);

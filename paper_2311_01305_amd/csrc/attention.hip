@@ -1188,7 +1188,7 @@ static Plan plan(int64_t D, bool codes, int64_t T, int64_t Hq, int64_t Hk, int64
     const int64_t own_keys = max_len + (p.fused ? prefix_len : 0), pairs = B * Hk * cdiv(most_rows, 2 * kWaves * 16);
     const bool fills = pairs * tall_splits(pairs, own_keys) > 256;
     p.mt = has_own && own_tall ? (most_rows > 64 && D < 256 && fills ? 2 : 1) : 0;
-    if (has_shared && shared_tall && p.mt < 2) p.mt = D == 256 ? (has_own && !own_tall && !codes ? 2 : 1) : all_rows > 64 || p.mt == 2 ? 2 : 1;
+    if (has_shared && shared_tall && p.mt < 2) p.mt = D == 256 ? (has_own && !own_tall && !codes ? 2 : 1) : all_rows > 64 ? 2 : 1;
     if (has_shared) {
         p.shared.tall = shared_tall;
         const int64_t tile = shared_tall ? kWaves * 16 * p.mt : kWideRows;

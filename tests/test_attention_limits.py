@@ -23,6 +23,20 @@ def call(lib, **changed):
     return e.value.name, lib.aweq_prefix_attention_ws(*sizes), lib.aweq_prefix_attention_ws_most(*sizes)
 
 
+def test_sizes_up_to_the_limits(B):
+    for inside in (dict(), dict(T=2097151, B=1, max_q=4096, max_len=20000), dict(T=255, Hq=65536, Hk=8192, B=255), dict(B=1 << 20, T=1 << 20, Hk=1),
+                   dict(prefix_len=1 << 29), dict(max_len=1 << 29), dict(pages=0x7fffffff)):
+        name, need, most = call(B, **inside)
+        assert name == "AWEQ_ERR_WORKSPACE" and 0 < need <= most, inside
+
+
+def test_sizes_beyond_them(B):
+    for beyond in (dict(T=2097152, B=1, max_q=4096), dict(T=1 << 24, Hq=1, Hk=1, B=1, max_q=1 << 24), dict(T=256, Hq=65536, Hk=8192), dict(T=2, B=2, Hq=65544, Hk=8),
+                   dict(B=(1 << 20) + 1, T=1 << 20), dict(B=1 << 20, Hk=32, Hq=32, T=1 << 18), dict(prefix_len=(1 << 29) + 1), dict(max_len=(1 << 29) + 1)):
+        assert call(B, **beyond) == ("AWEQ_ERR_SHAPE", 0, 0), beyond
+    assert call(B, pages=0x80000000)[0] == "AWEQ_ERR_SHAPE"
+
+
 def test_scales(B):
     """To base 2 they have to be finite."""
     assert call(B, scale=1.6e38)[0] == "AWEQ_ERR_WORKSPACE"
