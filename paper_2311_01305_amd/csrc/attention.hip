@@ -397,11 +397,14 @@ struct Rows {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) vs[n][v] = x.f[v];
             }
-            if (base != 0 || odd) {   // (what is not finite is not for rows that do not see it)
+            if (base != 0 || odd) {   // (what is not finite, or too large for the power of two that suits what is seen, is for no row here)
 #pragma unroll
                 for (int n = 0; n < N; ++n)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) vs[n][v] = vs[n][v] < INFINITY ? ldexpf(vs[n][v], base) : 0.0f;
+                    for (int v = 0; v < 4; ++v) {
+                        const float scaled = ldexpf(vs[n][v], base);
+                        vs[n][v] = scaled < INFINITY ? scaled : 0.0f;
+                    }
                 asm volatile("" ::: "memory");
             }
         }

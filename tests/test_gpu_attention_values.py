@@ -39,7 +39,7 @@ class Batch:
     also their steps.  A test changes them before put() lays them out."""
 
     def __init__(self, dt, codes, D, lens, new, prefix, Hq, Hk, seed=1):
-        self.__dict__.update(dt=dt, codes=codes, D=D, lens=lens, new=new, prefix=prefix, Hq=Hq, Hk=Hk, scale=D ** -0.5)
+        self.__dict__.update(dt=dt, codes=codes, D=D, lens=lens, new=new, prefix=prefix, Hq=Hq, Hk=Hk, scale=D ** -0.5, past=1.0)
         g = torch.Generator()
         g.manual_seed(seed)
         normal = lambda *s: torch.randn(s, generator=g)
@@ -71,7 +71,7 @@ class Batch:
             at += n
         cache, steps = [], []
         for c, s in ((self.k, self.ks), (self.v, self.vs)):
-            whole, whole_s = torch.zeros(pages, Hk, PAGE, D, dtype=store), torch.ones(pages, Hk, PAGE)
+            whole, whole_s = torch.zeros(pages, Hk, PAGE, D, dtype=store), torch.full((pages, Hk, PAGE), self.past)
             for x, xs, p in zip(c, s, places):
                 r = torch.arange(x.shape[0])
                 whole[p[r // PAGE], :, r % PAGE] = x
@@ -263,4 +263,18 @@ def test_values_that_are_not_finite(B, form, D, dt, codes):
                 b.vs[r][j, 0] = float(plant)
             else:
                 b.v[r][j, 0, 7] = float(plant)
+            b.check(*b.run(B, joined))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_small_steps_before_any_others(B, form):
+    """The smallest steps, and behind the last key of each page whatever a page may hold."""
+    lens, new, prefix, Hq, Hk, joined = FORMS[form]
+    for D in (64, 128, 256):
+        for past in (2.0 ** 100, float("inf"), float("nan"), 0.0):
+            print(f"[values] {form} D={D} small steps before {past}", flush=True)
+            b = Batch("bf16", True, D, lens, new, prefix, Hq, Hk, seed=D)
+            b.past = past
+            for s in b.vs:
+                s.fill_(2.0 ** -126)
             b.check(*b.run(B, joined))
