@@ -15,7 +15,7 @@
 //  - tall (many rows: the prefix, prompts): four wavefronts with rows of their own share tiles of 64 keys (32 of 512 bytes), filled by LDS-DMA loads of 16 bytes a
 //    lane, two tiles in turn; chunks of 16 bytes are XOR swizzled by choosing which one a lane fetches.  Codes go through registers instead, requested two tiles
 //    ahead, and are binary16 in LDS: converted once for the workgroup's rows, not by each wavefront
-//    (us: 2048 tokens behind 8192 keys 462 -> 373, 5 tokens of 16 sequences of up to 6000 48 -> 36, 64 tokens behind 8192 34.5 -> 31).
+//    (us: 2048 tokens behind 8192 keys 462 -> 373, 5 tokens of 16 sequences of up to 6000 48 -> 36, 64 tokens behind 8192 34.5 -> 31; with the steps as below 368, 37, 31).
 //  - wide (up to 16 rows: one token's heads): four wavefronts have the same rows and tiles of 32 keys of their own, whose results meet in
 //    LDS at the end.  K goes from memory to registers in the operand's order, V to registers and through the wavefront's own LDS; the next
 //    tile is requested as soon as this one's registers are free.
@@ -34,10 +34,10 @@
 //
 // What bounds it (heads of 128 values).  Wide: HBM, 4.9 - 5.5 TB/s of keys and values where they are many (24 sequences of 3000 - 15001 tokens and a prefix of
 // 2000, 461 MB of codes, 100 us with the join; a copy of 1 GB reaches 5.2); for one sequence the launches and a round trip each (1900 tokens, 31 MB: 9 us and 3 for
-// the join).  Tall: the clock under load: 970 TFLOP/s in binary16 (1024 new tokens of 2 sequences behind 8192), 80 % of what a product of 8192 x 8192 x 8192
+// the join).  Tall: the clock under load: 950 - 980 TFLOP/s in binary16 (1024 new tokens of 2 sequences behind 8192), 80 % of what a product of 8192 x 8192 x 8192
 // reaches here, the matrix cores busy for half of the cycles.  Products of one tile between the exponentials of another, 32 x 32 x 16 instructions, raised
 // priority around the products and a third tile in flight left that as it was.  The prefix of a decode step, whose rows are few, is one round of
-// workgroups that wait for their tiles (64 tokens behind 8192, 25 us, of which half the sequences' own keys; join 5).
+// workgroups that wait for their tiles (64 tokens behind 8192, 26 us, of which half the sequences' own keys; join 5).
 #include "wide_unit.hpp"
 
 #include <cmath>

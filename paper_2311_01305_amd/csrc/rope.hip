@@ -2,7 +2,7 @@
 // over a token's heads.
 //
 // HBM-bound: every value is read and written once.  Measured (us, TB/s of both): 4099 tokens x 128 heads of 128 binary16 values 48.4, 5.5; append of 7001
-// tokens x 80 heads, normed, 55.5, 5.2; a copy of 1 GB reaches 5.2.  A decode step's call (48 tokens x 96 heads) is its launch, 4.8.
+// tokens x 80 heads, normed, 55.5, 5.2, into 8-bit codes 61, 4.5; a copy of 1 GB reaches 5.2.  A decode step's call (48 tokens x 96 heads) is its launch, 4.8.
 //
 //   y = x w / sqrt(mean x^2 + eps);   the pair (a, b) of a head turns into (a cos - b sin, b cos + a sin), angle = pos freq[i]
 //
