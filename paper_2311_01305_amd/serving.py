@@ -96,10 +96,11 @@ class PagedCache:
         return [pages[i // s] * s + i % s for i in range(first, first + count)]
 
 
-def _check(name, t, dtype, shape, longer=False):
+def _check(name, t, dtype, shape, device, longer=False):
     """What the library reads by its address alone."""
-    if t is None or t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or (tuple(t.shape) < shape if longer else tuple(t.shape) != shape):
-        raise ValueError(f"{name}: {dtype} {list(shape)}{' or longer' if longer else ''}, in one piece")
+    if t is None or t.device != device or t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or \
+            (tuple(t.shape) < shape if longer else tuple(t.shape) != shape):
+        raise ValueError(f"{name}: {dtype} {list(shape)}{' or longer' if longer else ''}, in one piece, on {device}")
 
 
 class AttentionBlock:
@@ -107,14 +108,14 @@ class AttentionBlock:
 
     def __init__(self, qkv: QuantLinear, out: QuantLinear, q_heads: int, cache: PagedCache, freq: Optional[torch.Tensor], rot: int, max_tokens: int,
                  interleaved: bool = False, gain: float = 1.0, q_norm=None, k_norm=None, eps: float = 1e-6, device="cuda:0"):
-        D, Hk = cache.head_dim, cache.heads
+        D, Hk, where = cache.head_dim, cache.heads, cache.k.device
         if qkv.N != (q_heads + 2 * Hk) * D or out.K != q_heads * D:
             raise ValueError("the projections' sizes are not those of the heads")
         if rot:
-            _check("freq", freq, torch.float64, (rot // 2,))
+            _check("freq", freq, torch.float64, (rot // 2,), where)
         for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
             if w is not None:
-                _check(name, w, torch.float32, (D,))
+                _check(name, w, torch.float32, (D,), where)
         self.qkv_layer, self.out_layer, self.q_heads, self.cache = qkv, out, q_heads, cache
         self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm, self.eps = freq, rot, interleaved, gain, q_norm, k_norm, eps
         self.max_tokens, self.device = max_tokens, device
@@ -149,19 +150,19 @@ class AttentionBlock:
         T, c = x.shape[0], self.cache
         if T > self.max_tokens or x.dtype != c.dtype:
             raise ValueError("more tokens than max_tokens, or another type than the cache's")
-        batch = lens.shape[0]
-        if T == 0 or x.dim() != 2 or x.shape[1] != self.qkv_layer.K or x.stride(1) != 1:
-            raise ValueError("x: [tokens, hidden], one token at least, each in one piece")
+        batch, where = lens.shape[0], c.k.device
+        if T == 0 or x.device != where or x.dim() != 2 or x.shape[1] != self.qkv_layer.K or x.stride(1) != 1:
+            raise ValueError(f"x: [tokens, hidden], one token at least, each in one piece, on {where}")
         if self.rot:
-            _check("pos", pos, torch.int32, (T,))
-        _check("slot", slot, torch.int64, (T,))
-        _check("lens", lens, torch.int32, (batch,))
+            _check("pos", pos, torch.int32, (T,), where)
+        _check("slot", slot, torch.int64, (T,), where)
+        _check("lens", lens, torch.int32, (batch,), where)
         if q_start is not None:
-            _check("q_start", q_start, torch.int32, (batch + 1,))
-        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError("table: int32 [sequences, pages], each row in one piece")
+            _check("q_start", q_start, torch.int32, (batch + 1,), where)
+        if table.device != where or table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != batch or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError(f"table: int32 [sequences, pages], each row in one piece, on {where}")
         if prefix_len:
-            _check("prefix_table", prefix_table, torch.int32, (-(-prefix_len // c.page_size),), longer=True)
+            _check("prefix_table", prefix_table, torch.int32, (-(-prefix_len // c.page_size),), where, longer=True)
         max_len = min(max_len, table.shape[1] * c.page_size)   # (a view's pitch may be more than its pages)
         dt = DTYPES[x.dtype]
         Hq, Hk, D = self.q_heads, c.heads, c.head_dim

@@ -72,3 +72,17 @@ def test_lengths_are_bounded_by_the_pages_of_the_table(S, calls):
     block(S)(**arguments(table=torch.zeros(BATCH, 50, dtype=torch.int32)[:, :2], max_len=700))
     numbers = [v for v in next(a for n, a in calls if n == "aweq_prefix_attention") if isinstance(v, int)]
     assert 2 * PAGE in numbers and 700 not in numbers
+
+
+@pytest.mark.parametrize("which", ["x", "pos", "slot", "lens", "table", "q_start", "prefix_table"])
+def test_tensors_elsewhere_are_refused(S, calls, which):
+    """Their addresses mean nothing to the GPU that the cache is on (here: tensors without memory beside those of the CPU)."""
+    with pytest.raises(ValueError):
+        block(S)(**arguments(**{which: arguments()[which].to("meta")}))
+    assert not calls
+
+
+def test_a_block_refuses_tensors_elsewhere(S):
+    for wrong in (dict(freq=torch.ones(16, dtype=torch.float64, device="meta")), dict(q_norm=torch.ones(D, device="meta")), dict(k_norm=torch.ones(D, device="meta"))):
+        with pytest.raises(ValueError):
+            block(S, **wrong)
