@@ -111,6 +111,8 @@ class AttentionBlock:
         D, Hk, where = cache.head_dim, cache.heads, cache.k.device
         if qkv.N != (q_heads + 2 * Hk) * D or out.K != q_heads * D:
             raise ValueError("the projections' sizes are not those of the heads")
+        if D not in (64, 128, 256) or q_heads % Hk:
+            raise ValueError("heads of 64, 128 or 256 values, and a whole number of query heads to a key head: the attention reads no others")
         if rot:
             _check("freq", freq, torch.float64, (rot // 2,), where)
         for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):

@@ -86,3 +86,12 @@ def test_a_block_refuses_tensors_elsewhere(S):
     for wrong in (dict(freq=torch.ones(16, dtype=torch.float64, device="meta")), dict(q_norm=torch.ones(D, device="meta")), dict(k_norm=torch.ones(D, device="meta"))):
         with pytest.raises(ValueError):
             block(S, **wrong)
+
+
+@pytest.mark.parametrize("heads,key_heads,size", [(4, 2, 96), (4, 2, 80), (4, 2, 32), (4, 3, 64)])
+def test_heads_that_the_attention_does_not_read(S, heads, key_heads, size):
+    """Refused when the block is made, not after a step has filled its cache."""
+    layer = lambda N, K: S.QuantLinear(N, K, *[None] * 4)
+    with pytest.raises(ValueError):
+        S.AttentionBlock(layer((heads + 2 * key_heads) * size, HIDDEN), layer(HIDDEN, heads * size), heads, S.PagedCache(8, PAGE, key_heads, size, device="cpu"), None, 0, 8,
+                         device="cpu")
