@@ -174,7 +174,8 @@ struct Shape {
 template <int C>
 __device__ __forceinline__ int swz_k(int row)
 {
-    return C >= 16 ? (row & 15) : (row / (16 / C)) & (C - 1);
+    if constexpr (C >= 16) return row & 15;
+    else return (row / (16 / C)) & (C - 1);
 }
 template <int C, bool CODES>
 __device__ __forceinline__ int swz_v(int row)
