@@ -55,7 +55,8 @@ enum {
     AWEQ_ST_SCALEGUARD = 8u, /* Eq. 10: a channel range was < 1e-5 (s := 1) or s was clamped to [1e-4, 1e4] */
     AWEQ_ST_ZEROPOINT = 16u, /* stage 4 de-quantisation met a zero point outside [0, 255] (a slice whose range does not
                                 contain 0): its 32-bit integer part is exact only while it fits in 32 bits */
-    AWEQ_ST_INDEX = 32u      /* a page, slot or length on the device lies outside what the call was given: clamped or left out */
+    AWEQ_ST_INDEX = 32u,     /* a page, slot or length on the device lies outside what the call was given: clamped or left out */
+    AWEQ_ST_PAGES = 64u      /* aweq_step_plan: fewer pages are free than the step takes; nothing was changed */
 };
 
 typedef enum {
@@ -435,6 +436,82 @@ int aweq_prefix_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, i
                           const int32_t* table, int64_t table_ld, const int32_t* lens, const int32_t* q_start, int64_t B,
                           int64_t max_len, int64_t max_q, float scale, void* out, int64_t ldo, float* lse,
                           void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
+/* ======== Projections in 4-bit floating point ========
+ *
+ * ---- Microscaled 4-bit format.  Each block of 32 values along K has a power of two 2^e, and a value's code stands for one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * times that, with a sign (bit 3).  x[r,k] = X[r,k] * factor[k] (one fp32 multiply; factor nullable).  For a block with the largest magnitude m:
+ *   e = floor(log2 m) - 2, at least -127 (a block of zeros: -127);  code = the nearest to x / 2^e, ties to the even code, 6 where that is larger.
+ * A block with a NaN or an infinity gets the scale NaN, which every value of it then is, and raises AWEQ_ST_NONFINITE.
+ * K % 32 == 0.  Codes: panels of 128 values, two a byte (even k low), rows back to back, zero fill past K:
+ *     byte of M[r][k] = ((k / 128) * rows + r) * 64 + (k % 128) / 2;
+ * scales e + 127 (255: NaN): 16 bytes for each row and four panels (512 values), block b = k % 128 / 32 of panel p = k / 128 at
+ *     ((p / 4) * rows + r) * 16 + ((b % 2) * 2 + b / 2) * 4 + p % 4
+ * (a matrix unit's lane then has the scales of four panels in one register), those of blocks past K in the last panel 127, of panels past it unspecified.
+ * aweq_mx4_code_bytes, aweq_mx4_scale_bytes: sizes of the two buffers (host functions; 0 where the shape is none).
+ * aweq_quant_mx4: X[rows x K] F32, F16 or BF16, pitch ldx.  aweq_mx4_values: the values that the codes stand for, to F32, F16 or BF16 (rounded; BF16 and
+ * F32 hold them as they are), pitch ldo.  K <= 2^20, rows < 2^31; 16-byte aligned pointers and rows. */
+size_t aweq_mx4_code_bytes(int64_t rows, int64_t K);
+size_t aweq_mx4_scale_bytes(int64_t rows, int64_t K);
+int aweq_quant_mx4(const void* X, aweq_dtype dt, int64_t rows, int64_t K, int64_t ldx, const float* factor, uint8_t* codes, uint8_t* scales,
+                   uint32_t* status, void* stream);
+int aweq_mx4_values(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t K, void* out, aweq_dtype out_dt, int64_t ldo, void* stream);
+
+/* ---- Product of two such matrices: out[t,n] = sum_k x[t,k] w[n,k] + bias[n] (bias fp32, nullable).  X[T x K] (F32, F16, BF16; pitch ldx) is quantised as by
+ * aweq_quant_mx4 first, and xq and x_scale are written; X NULL: they are inputs.  wq, w_scale: the weight's.  Products are exact, sums fp32 in an order that
+ * depends on the shape alone, rounded once to out_dt (F32, F16, BF16; pitch ldo).  K % 32 == 0, K <= 2^20, N % 4 == 0, ldo % 4 == 0, T and N < 2^31;
+ * 16-byte aligned pointers. */
+int aweq_mx4_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, int64_t K, int64_t ldx, const float* factor, uint8_t* xq, uint8_t* x_scale,
+                         const uint8_t* wq, const uint8_t* w_scale, int64_t N, const float* bias, void* out, aweq_dtype out_dt, int64_t ldo,
+                         uint32_t* status, void* stream);
+
+/* ======== Drafted tokens: several of a sequence in one step, of which a part is kept ========
+ *
+ * ---- A step's plan, from what each of B sequences has and what it gets.  lens[b]: tokens in its pages; change[b] > 0: that many more, < 0: the last -change
+ * of them go, 0: neither.  With page_size tokens to a page (as above) a sequence has ceil(lens / page_size) pages, the first entries of its row of `table`
+ * ([B][table_pages], pitch table_ld).  free_pages[pages] is a stack of the pages that nobody has, *free_count of them.
+ *   Pages that no longer hold a token are given back, in the order of the sequences and of their rows; they are the first that are taken, then the stack's
+ *   from its top.  Sequences take theirs in order, into the entries behind those that they have.  What is left of those given back goes on the stack.
+ *   lens_out[b] = lens + change, *count_out: pages on the stack;  q_start[B + 1]: the new tokens of each sequence, one sequence after the other;
+ *   pos[t] = prefix_len + place in its sequence, slot[t] = where the token goes (aweq_kv_append), T of each; past q_start[B]: 0 and -1.
+ * Where the pages do not suffice nothing is changed (lens_out = lens, *count_out = *free_count, q_start all 0, pos 0, slot -1) and AWEQ_ST_PAGES is raised; the same,
+ * with AWEQ_ST_INDEX, for a length below 0, more taken away than there is, more tokens than T, a sequence longer than table_pages pages, or a count
+ * outside [0, pages].  lens_out must not be lens, nor count_out free_count (AWEQ_ERR_ALIGN for an output that overlaps an input): a step has the next one's inputs
+ * beside its own.  B <= 8192, T <= 2^24,
+ * pages < 2^31, table_pages <= 2^24, prefix_len <= 2^29, table_pages * page_size <= 2^29. */
+int aweq_step_plan(const int32_t* lens, const int32_t* change, int64_t B, int64_t page_size, int64_t pages, int32_t* table, int64_t table_ld,
+                   int64_t table_pages, int32_t* free_pages, const int32_t* free_count, int64_t prefix_len, int64_t T,
+                   int32_t* lens_out, int32_t* count_out, int32_t* q_start, int32_t* pos, int64_t* slot, uint32_t* status, void* stream);
+
+/* ---- Which of its sequence's new tokens a drafted token sees.  The new tokens of sequence b are the rows q_start[b] .. q_start[b + 1] - 1; parent[t] (int32) is
+ * the place among them of the token that t goes on from, an earlier one, or -1: what the sequence has already (anything else: taken as -1, and
+ * AWEQ_ST_INDEX).  mask[t] (words of 64 bits, pitch mask_ld words >= ceil(max_q / 64)): bit j says that t is new token j or goes on from it, however
+ * far; bits of all ceil(max_q / 64) words are written.  pos[t] (nullable, with lens) = prefix_len + lens[b] - m + depth, m its sequence's new tokens, depth how
+ * many of them come before t on its path.  max_q (HOST): no sequence has more; <= 4096.  Rows past q_start[B] are left as they are.  q_start out of
+ * order, past T, or with more than max_q rows: AWEQ_ST_INDEX and clamped.  B <= 2^20, T <= 2^24. */
+int aweq_tree_mask(const int32_t* parent, int64_t T, const int32_t* q_start, int64_t B, int64_t max_q, const int32_t* lens, int64_t prefix_len,
+                   uint64_t* mask, int64_t mask_ld, int32_t* pos, uint32_t* status, void* stream);
+
+/* ---- aweq_prefix_attention for new tokens that do not all see one another: of its sequence's lens[b] keys a token sees the first lens[b] - m, and of the m
+ * new ones (the last m) those whose bit is set in mask[t] (pitch mask_ld words >= ceil(max_q / 64); any bits, its own or not).  All else, limits and scratch
+ * memory (aweq_prefix_attention_ws, aweq_prefix_attention_ws_most) as there; a row without any key gets zeros and lse -inf, and what a token does not
+ * see has no part in its out, whatever it holds.  q_start is required, and table if max_len > 0; lens[b] < m: AWEQ_ST_INDEX (results of that sequence unspecified). */
+int aweq_tree_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int64_t D, int64_t ldq,
+                        const void* k_cache, const void* v_cache, const float* k_step, const float* v_step, aweq_dtype cache_dt,
+                        int64_t pages, int64_t page_size, int64_t Hk, const int32_t* prefix_table, int64_t prefix_len,
+                        const int32_t* table, int64_t table_ld, const int32_t* lens, const int32_t* q_start, int64_t B,
+                        int64_t max_len, int64_t max_q, const uint64_t* mask, int64_t mask_ld, float scale, void* out, int64_t ldo, float* lse,
+                        void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
+/* ---- After a step some of whose new tokens are kept: kept[b][j], j < count[b] (int32, pitch kept_ld >= every count), are their places among sequence
+ * b's m new tokens, in strictly increasing order.  Their keys and values (and steps) move to the places 0 .. count - 1 of those, and change[b] = count - m is what
+ * aweq_step_plan takes to drop the rest.  The tokens behind the kept ones are unspecified afterwards.  A count outside [0, min(m, kept_ld)], places out of
+ * order or outside [0, m), lens[b] < m, or pages outside [0, pages): AWEQ_ST_INDEX, and nothing of that sequence is moved (change 0; a page outside: the
+ * rows on it alone); so for a sequence longer than table_ld pages.  No two sequences may have a page of new tokens in common.  Caches as in aweq_kv_append;
+ * T, q_start, lens, table: the step's.  B <= 2^20, Hk <= 2^16, T <= 2^24. */
+int aweq_kv_keep(void* k_cache, void* v_cache, float* k_step, float* v_step, aweq_dtype cache_dt, int64_t pages, int64_t page_size, int64_t Hk, int64_t D,
+                 const int32_t* table, int64_t table_ld, const int32_t* lens, const int32_t* q_start, int64_t B, int64_t T,
+                 const int32_t* kept, int64_t kept_ld, const int32_t* count, int32_t* change, uint32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -11,5 +11,6 @@ from .binding import (  # noqa: F401
     aweq_w8a8_gemm, aweq_workspace_size, load_library, aweq_panel_bytes, aweq_pack_panels_i8,
     aweq_unpack_panels_i8, aweq_wonly_gemm, aweq_fold_quant_weight, aweq_calibrate,
     aweq_quant_tokens, aweq_w8a8_gemm_tokens, aweq_rope_frequencies, aweq_qk_rope, aweq_kv_append, aweq_prefix_attention,
-    aweq_prefix_attention_ws, aweq_prefix_attention_ws_most,
+    aweq_prefix_attention_ws, aweq_prefix_attention_ws_most, aweq_mx4_code_bytes, aweq_mx4_scale_bytes, aweq_quant_mx4, aweq_mx4_values,
+    aweq_mx4_gemm_tokens, aweq_step_plan, aweq_tree_mask, aweq_tree_attention, aweq_kv_keep,
 )

@@ -21,14 +21,16 @@ AWEQ_F32, AWEQ_F16, AWEQ_I8, AWEQ_BF16 = 0, 1, 2, 3
 OP_CALIB_STATS, OP_EQUALIZE, OP_QUANT_WEIGHT, OP_W8A8_GEMM, OP_BIAS_CORRECT, OP_WONLY_GEMM, OP_QUANT_ACT, OP_CALIBRATE = range(8)
 BIAS_W8A8, BIAS_WEIGHT_ONLY = 0, 1
 SCALE_NONE, SCALE_RANGE, SCALE_ABSMAX = 0, 1, 2
-ST_DEGENERATE, ST_NONFINITE, ST_BIGQUOT, ST_SCALEGUARD, ST_ZEROPOINT, ST_INDEX = 1, 2, 4, 8, 16, 32
+ST_DEGENERATE, ST_NONFINITE, ST_BIGQUOT, ST_SCALEGUARD, ST_ZEROPOINT, ST_INDEX, ST_PAGES = 1, 2, 4, 8, 16, 32, 64
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 
 EXPORTS = ("aweq_workspace_size", "aweq_status_string", "aweq_calib_stats", "aweq_equalize",
            "aweq_quant_weight", "aweq_quant_act", "aweq_w8a8_gemm", "aweq_bias_correct",
            "aweq_panel_bytes", "aweq_pack_panels_i8", "aweq_unpack_panels_i8", "aweq_wonly_gemm", "aweq_fold_quant_weight", "aweq_w8a8_gemm_fused",
            "aweq_calib_stats_static", "aweq_calibrate", "aweq_quant_tokens", "aweq_w8a8_gemm_tokens", "aweq_rope_frequencies", "aweq_qk_rope",
-           "aweq_kv_append", "aweq_prefix_attention_ws", "aweq_prefix_attention_ws_most", "aweq_prefix_attention")
+           "aweq_kv_append", "aweq_prefix_attention_ws", "aweq_prefix_attention_ws_most", "aweq_prefix_attention",
+           "aweq_mx4_code_bytes", "aweq_mx4_scale_bytes", "aweq_quant_mx4", "aweq_mx4_values", "aweq_mx4_gemm_tokens", "aweq_step_plan",
+           "aweq_tree_mask", "aweq_tree_attention", "aweq_kv_keep")
 STATIC_SCRATCH_BYTES = 16 << 20
 
 _vp, _i64, _i32, _u64, _f32, _f64, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_uint64, C.c_float, C.c_double, C.c_size_t
@@ -69,6 +71,9 @@ def load_library():
     for name in ("aweq_prefix_attention_ws", "aweq_prefix_attention_ws_most"):
         getattr(lib, name).restype = _sz
         getattr(lib, name).argtypes = [_i64] * 8
+    for name in ("aweq_mx4_code_bytes", "aweq_mx4_scale_bytes"):
+        getattr(lib, name).restype = _sz
+        getattr(lib, name).argtypes = [_i64, _i64]
     spec = importlib.util.spec_from_loader("_native", importlib.machinery.ExtensionFileLoader("_native", _NATIVE_PATH))
     calls = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(calls)
@@ -264,3 +269,47 @@ def aweq_prefix_attention(q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step
     _check((_calls or _native()).aweq_prefix_attention(
         q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, prefix_table, prefix_len, table, table_ld, lens,
         q_start, B, max_len, max_q, scale, out, ldo, lse, ws, _nbytes(ws) if ws_bytes is None else ws_bytes, status, _stream(stream)))
+
+
+def aweq_mx4_code_bytes(rows, K):
+    return int(load_library().aweq_mx4_code_bytes(int(rows), int(K)))
+
+
+def aweq_mx4_scale_bytes(rows, K):
+    return int(load_library().aweq_mx4_scale_bytes(int(rows), int(K)))
+
+
+def aweq_quant_mx4(X, dt, rows, K, ldx, factor, codes, scales, status=None, stream=None):
+    _check((_calls or _native()).aweq_quant_mx4(X, dt, rows, K, ldx, factor, codes, scales, status, _stream(stream)))
+
+
+def aweq_mx4_values(codes, scales, rows, K, out, out_dt, ldo, stream=None):
+    _check((_calls or _native()).aweq_mx4_values(codes, scales, rows, K, out, out_dt, ldo, _stream(stream)))
+
+
+def aweq_mx4_gemm_tokens(X, x_dt, T, K, ldx, factor, xq, x_scale, wq, w_scale, N, bias, out, out_dt, ldo, status=None, stream=None):
+    _check((_calls or _native()).aweq_mx4_gemm_tokens(X, x_dt, T, K, ldx, factor, xq, x_scale, wq, w_scale, N, bias, out, out_dt, ldo, status,
+                                                      _stream(stream)))
+
+
+def aweq_step_plan(lens, change, B, page_size, pages, table, table_ld, table_pages, free_pages, free_count, prefix_len, T, lens_out, count_out, q_start,
+                   pos, slot, status=None, stream=None):
+    _check((_calls or _native()).aweq_step_plan(lens, change, B, page_size, pages, table, table_ld, table_pages, free_pages, free_count, prefix_len, T,
+                                                lens_out, count_out, q_start, pos, slot, status, _stream(stream)))
+
+
+def aweq_tree_mask(parent, T, q_start, B, max_q, lens, prefix_len, mask, mask_ld, pos, status=None, stream=None):
+    _check((_calls or _native()).aweq_tree_mask(parent, T, q_start, B, max_q, lens, prefix_len, mask, mask_ld, pos, status, _stream(stream)))
+
+
+def aweq_tree_attention(q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, prefix_table, prefix_len, table,
+                        table_ld, lens, q_start, B, max_len, max_q, mask, mask_ld, scale, out, ldo, lse, ws, status=None, stream=None, ws_bytes=None):
+    _check((_calls or _native()).aweq_tree_attention(
+        q, dt, T, Hq, D, ldq, k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, prefix_table, prefix_len, table, table_ld, lens,
+        q_start, B, max_len, max_q, mask, mask_ld, scale, out, ldo, lse, ws, _nbytes(ws) if ws_bytes is None else ws_bytes, status, _stream(stream)))
+
+
+def aweq_kv_keep(k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, D, table, table_ld, lens, q_start, B, T, kept, kept_ld, count, change,
+                 status=None, stream=None):
+    _check((_calls or _native()).aweq_kv_keep(k_cache, v_cache, k_step, v_step, cache_dt, pages, page_size, Hk, D, table, table_ld, lens, q_start, B, T,
+                                              kept, kept_ld, count, change, status, _stream(stream)))

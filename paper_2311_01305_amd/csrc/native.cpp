@@ -67,7 +67,9 @@ struct Entry<int (*)(A...)> {
 #define ENTRIES(X)                                                                                                     \
     X(aweq_calib_stats) X(aweq_calib_stats_static) X(aweq_equalize) X(aweq_quant_weight) X(aweq_fold_quant_weight)     \
     X(aweq_quant_act) X(aweq_w8a8_gemm) X(aweq_w8a8_gemm_fused) X(aweq_bias_correct) X(aweq_wonly_gemm)                \
-    X(aweq_quant_tokens) X(aweq_w8a8_gemm_tokens) X(aweq_qk_rope) X(aweq_kv_append) X(aweq_prefix_attention)
+    X(aweq_quant_tokens) X(aweq_w8a8_gemm_tokens) X(aweq_qk_rope) X(aweq_kv_append) X(aweq_prefix_attention)           \
+    X(aweq_quant_mx4) X(aweq_mx4_values) X(aweq_mx4_gemm_tokens) X(aweq_step_plan) X(aweq_tree_mask)                   \
+    X(aweq_tree_attention) X(aweq_kv_keep)
 
 #define X(name)                                                                                                        \
     decltype(&::name) p_##name;                                                                                        \

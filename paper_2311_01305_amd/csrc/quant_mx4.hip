@@ -1,0 +1,162 @@
+// Quantizer to microscaled 4-bit floating point, and the values that its codes stand for.
+//
+// HBM-bound: 2 bytes in and 17/32 out a value (16-bit types), and about five vector operations.  A block's 32 values are four lanes' units of eight; 16 lanes
+// have a row's panel and a wavefront four rows of it, four panels one after the other, so that the four scales that a lane's block has in them are the four bytes
+// which belong together, and the codes of four rows are 256 bytes in one piece.
+#include "mx4.hpp"
+
+namespace aweq {
+namespace mx {
+
+constexpr int kThreads = 256;
+constexpr int kRows = 16;      // of a workgroup
+
+struct QuantArgs {
+    const void* X;
+    int64_t rows, K, ldx;
+    const float* factor;
+    uint8_t *codes, *scales;
+    uint32_t* status;
+    int groups;
+    int64_t first;
+};
+
+template <class E, bool FACTOR>
+__global__ __launch_bounds__(kThreads) void quant_kernel(QuantArgs g)
+{
+    const int64_t block = g.first + blockIdx.x;
+    const int group = (int)(block % g.groups);
+    const int64_t r = block / g.groups * kRows + threadIdx.x / 16;
+    const int c = threadIdx.x & 15;
+    const int64_t row = min(r, g.rows - 1);                                      // (rows past the last one: nothing is written)
+    const int64_t k0 = (int64_t)group * (kMxPanel * kMxGroup) + c * 8;
+    const E* const from = reinterpret_cast<const E*>(g.X) + row * g.ldx;
+    Unit<E> raw[kMxGroup];
+    float factor[kMxGroup][8];
+#pragma unroll
+    for (int p = 0; p < kMxGroup; ++p) {
+        const int64_t k = k0 + p * kMxPanel;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { raw[p][e] = (E)0.0f; factor[p][e] = 1.0f; }
+        if (k < g.K) {
+            raw[p] = load_unit(from + k);
+            if constexpr (FACTOR) {
+                const f32x8 f = load_unit(g.factor + k);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) factor[p][e] = f[e];
+            }
+        }
+    }
+    uint32_t scales = 0, st = 0;
+#pragma unroll
+    for (int p = 0; p < kMxGroup; ++p) {
+        const int64_t k = k0 + p * kMxPanel;
+        uint32_t scale;
+        const uint32_t w = mx_unit<FACTOR, E>(raw[p], factor[p], scale);
+        if (scale == 255u) st = AWEQ_ST_NONFINITE;
+        scales |= (k < g.K ? scale : 127u) << (8 * p);
+        const int64_t panel = (int64_t)group * kMxGroup + p;
+        if (r < g.rows && panel * kMxPanel < g.K) *reinterpret_cast<uint32_t*>(g.codes + (panel * g.rows + r) * 64 + c * 4) = w;
+    }
+    if (r < g.rows && (c & 3) == 0) *reinterpret_cast<uint32_t*>(g.scales + ((int64_t)group * g.rows + r) * 16 + mx_scale_place(c >> 2)) = scales;
+    raise_status(g.status, st);
+}
+
+struct ValueArgs {
+    const uint8_t *codes, *scales;
+    int64_t rows, K, ldo;
+    void* out;
+    int groups;
+    int64_t first;
+};
+
+// the value of a code: two bits of exponent and one of mantissa below the sign, under the block's power of two
+__device__ __forceinline__ float mx_value(uint32_t code, float step)
+{
+    const uint32_t m = code & 7u;
+    const float v = m < 2u ? 0.5f * (float)m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
+    return (code & 8u ? -v : v) * step;
+}
+
+template <class E>
+__global__ __launch_bounds__(kThreads) void value_kernel(ValueArgs g)
+{
+    const int64_t block = g.first + blockIdx.x;
+    const int group = (int)(block % g.groups);
+    const int64_t r = block / g.groups * kRows + threadIdx.x / 16;
+    const int c = threadIdx.x & 15;
+    if (r >= g.rows) return;
+    const uint32_t scales = *reinterpret_cast<const uint32_t*>(g.scales + ((int64_t)group * g.rows + r) * 16 + mx_scale_place(c >> 2));
+#pragma unroll
+    for (int p = 0; p < kMxGroup; ++p) {
+        const int64_t panel = (int64_t)group * kMxGroup + p, k = panel * kMxPanel + c * 8;
+        if (k >= g.K) continue;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(g.codes + (panel * g.rows + r) * 64 + c * 4);
+        const uint32_t s = scales >> (8 * p) & 255u;
+        const float step = s == 255u ? NAN : s == 0u ? 0x1p-127f : __uint_as_float(s << 23);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = mx_value(w >> (4 * e) & 15u, step);
+        store_unit(reinterpret_cast<E*>(g.out) + r * g.ldo + k, x);
+    }
+}
+
+// blocks of 16 rows and 512 values; fewer than 2^32 threads to a launch
+template <class A, class F>
+static int launch_blocks(A g, F kernel, hipStream_t st)
+{
+    g.groups = (int)mx_groups(g.K);
+    const int64_t blocks = cdiv(g.rows, kRows) * g.groups, most = (1ll << 32) / kThreads - 1;
+    for (int64_t b = 0; b < blocks; b += most) {
+        g.first = b;
+        kernel<<<(unsigned)(blocks - b < most ? blocks - b : most), kThreads, 0, st>>>(g);
+    }
+    return launch_status();
+}
+
+}  // namespace mx
+
+int check_quant_mx4(const void* X, aweq_dtype dt, int64_t rows, int64_t K, int64_t ldx, const float* factor, const uint8_t* codes, const uint8_t* scales)
+{
+    if (!X || !codes || !scales) return AWEQ_ERR_NULL;
+    if (dt != AWEQ_F32 && dt != AWEQ_F16 && dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    if (!mx_shape_ok(rows, K) || ldx < K) return AWEQ_ERR_SHAPE;
+    if (!aligned16(X) || (ldx * (int64_t)dtype_size(dt)) % 16 != 0 || (factor && !aligned16(factor)) || !aligned16(codes) || !aligned16(scales)) return AWEQ_ERR_ALIGN;
+    return AWEQ_OK;
+}
+
+int launch_quant_mx4(const void* X, aweq_dtype dt, int64_t rows, int64_t K, int64_t ldx, const float* factor, uint8_t* codes, uint8_t* scales,
+                     uint32_t* status, hipStream_t st)
+{
+    const mx::QuantArgs g = {X, rows, K, ldx, factor, codes, scales, status, 0, 0};
+    if (dt == AWEQ_F16) return factor ? mx::launch_blocks(g, mx::quant_kernel<_Float16, true>, st) : mx::launch_blocks(g, mx::quant_kernel<_Float16, false>, st);
+    if (dt == AWEQ_BF16) return factor ? mx::launch_blocks(g, mx::quant_kernel<__bf16, true>, st) : mx::launch_blocks(g, mx::quant_kernel<__bf16, false>, st);
+    return factor ? mx::launch_blocks(g, mx::quant_kernel<float, true>, st) : mx::launch_blocks(g, mx::quant_kernel<float, false>, st);
+}
+
+}  // namespace aweq
+
+using namespace aweq;
+
+extern "C" size_t aweq_mx4_code_bytes(int64_t rows, int64_t K) { return mx_shape_ok(rows, K) ? (size_t)(mx_panels(K) * rows * 64) : 0; }
+
+extern "C" size_t aweq_mx4_scale_bytes(int64_t rows, int64_t K) { return mx_shape_ok(rows, K) ? (size_t)(mx_groups(K) * rows * 16) : 0; }
+
+extern "C" int aweq_quant_mx4(const void* X, aweq_dtype dt, int64_t rows, int64_t K, int64_t ldx, const float* factor, uint8_t* codes, uint8_t* scales,
+                              uint32_t* status, void* stream)
+{
+    const int rc = check_quant_mx4(X, dt, rows, K, ldx, factor, codes, scales);
+    return rc != AWEQ_OK ? rc : launch_quant_mx4(X, dt, rows, K, ldx, factor, codes, scales, status, as_stream(stream));
+}
+
+extern "C" int aweq_mx4_values(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t K, void* out, aweq_dtype out_dt, int64_t ldo, void* stream)
+{
+    if (!codes || !scales || !out) return AWEQ_ERR_NULL;
+    if (out_dt != AWEQ_F32 && out_dt != AWEQ_F16 && out_dt != AWEQ_BF16) return AWEQ_ERR_DTYPE;
+    if (!mx_shape_ok(rows, K) || ldo < K) return AWEQ_ERR_SHAPE;
+    if (!aligned16(codes) || !aligned16(scales) || !aligned16(out) || (ldo * (int64_t)dtype_size(out_dt)) % 16 != 0) return AWEQ_ERR_ALIGN;
+    const mx::ValueArgs g = {codes, scales, rows, K, ldo, out, 0, 0};
+    if (out_dt == AWEQ_F16) return mx::launch_blocks(g, mx::value_kernel<_Float16>, as_stream(stream));
+    if (out_dt == AWEQ_BF16) return mx::launch_blocks(g, mx::value_kernel<__bf16>, as_stream(stream));
+    return mx::launch_blocks(g, mx::value_kernel<float>, as_stream(stream));
+}

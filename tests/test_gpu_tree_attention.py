@@ -1,0 +1,257 @@
+"""Attention of drafted tokens under masks against softmax in 64 bits, one sequence after the other."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2311_01305_amd import binding
+    binding.load_library()
+    return binding
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+class Case:
+    """A batch: own keys of each sequence (lens) with its new tokens (new), a prefix; sees[t]: a row of truth values over its sequence's new tokens.  Everything in
+    the caches that is no key is NaN, and so is every new token's value that nobody sees where `hide` says so."""
+
+    def __init__(self, dt, codes, D, Hq, Hk, page, lens, new, prefix, kind="tree", seed=1, hide=False, junk=False):
+        self.__dict__.update(dt=dt, codes=codes, D=D, Hq=Hq, Hk=Hk, page=page, lens=lens, new=new, prefix=prefix, junk=junk)
+        g = torch.Generator()
+        g.manual_seed(seed)
+        normal = lambda *s: torch.randn(s, generator=g)
+        self.T = sum(new)
+        self.sees = []
+        for m in new:
+            s = torch.zeros(m, m, dtype=torch.bool)
+            for i in range(m):
+                if kind == "any":
+                    s[i] = torch.rand(m, generator=g) < 0.3
+                elif kind == "none":
+                    pass
+                else:
+                    p = -1 if i == 0 else i - 1 if kind == "chain" else int(torch.randint(-1, i, (1,), generator=g))
+                    if p >= 0:
+                        s[i] = s[p]
+                    s[i, i] = True
+            self.sees.append(s)
+        self.q = (2 * normal(self.T, Hq, D)).to(TYPES[dt])
+        need = [-(-n // page) for n in lens]
+        pp = -(-prefix // page)
+        self.pages = pp + sum(need) + 2
+        order = torch.randperm(self.pages, generator=g)
+        self.prefix_table = order[:pp].to(torch.int32)
+        self.width = max(1, max(need)) + 1
+        self.table = torch.full((len(lens), self.width), -1, dtype=torch.int32)
+        at = pp
+        for b, n in enumerate(need):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        store = torch.int8 if codes else TYPES[dt]
+        self.k, self.v = (torch.full((self.pages, Hk, page, D), 99 if codes else float("nan")).to(store) for _ in range(2))
+        self.ks, self.vs = (torch.full((self.pages, Hk, page), float("nan")) for _ in range(2)) if codes else (None, None)
+        self.keys = []
+        for b, (table, n) in enumerate([(self.prefix_table, prefix)] + [(self.table[b], n) for b, n in enumerate(lens)]):
+            both = []
+            for c, s in ((self.k, self.ks), (self.v, self.vs)):
+                x = normal(n, Hk, D)
+                p, r = table[torch.arange(n) // page].long(), torch.arange(n) % page
+                if codes:
+                    x *= torch.exp(normal(n, Hk, 1))
+                    step = x.abs().amax(2) / 127
+                    x = torch.round(x / step[..., None])
+                    s[p, :, r] = step
+                else:
+                    x, step = x.to(store), None
+                if hide and b > 0 and new[b - 1] > 0:
+                    m = new[b - 1]
+                    unseen = torch.arange(n - m, n)[~self.sees[b - 1].any(0)]
+                    if codes:
+                        s[p[unseen], :, r[unseen]] = float("nan")
+                    elif c is self.v:
+                        x[unseen] = float("inf")
+                        x[unseen, :, ::3] = float("nan")
+                    # (a key that nobody sees may hold anything too)
+                    if not codes and c is self.k:
+                        x[unseen] = float("nan")
+                c[p, :, r] = x.to(store)
+                both.append(x.double() if step is None else x.double() * step.double()[..., None])
+            self.keys.append([x.transpose(0, 1) for x in both])
+        self.scale = 1 / math.sqrt(D)
+
+    def mask(self, ld):
+        g = torch.Generator()
+        g.manual_seed(5)
+        out = torch.zeros(self.T, ld, dtype=torch.int64)
+        if self.junk:       # bits past a sequence's new tokens say nothing
+            out = torch.randint(-2 ** 62, 2 ** 62, (self.T, ld), generator=g)
+        t = 0
+        for s in self.sees:
+            m = s.shape[0]
+            for i in range(m):
+                for w in range(ld):
+                    for j in range(64 * w, min(64 * w + 64, m)):
+                        bit = 1 << (j - 64 * w)
+                        v = int(out[t, w]) & (2 ** 64 - 1)
+                        v = v | bit if s[i, j] else v & ~bit
+                        out[t, w] = v - 2 ** 64 if v >> 63 else v
+                t += 1
+        return out
+
+    def run(self, B, max_len=None, max_q=None, ld_extra=0, stream=None):
+        D, Hq = self.D, self.Hq
+        n, max_len, max_q = len(self.lens), max_len or max(self.lens), max_q or max(self.new)
+        ld = -(-max_q // 64) + ld_extra
+        ldo = Hq * D + 8
+        d = {k: None if getattr(self, k) is None else getattr(self, k).to(DEV) for k in ("q", "k", "v", "ks", "vs", "table", "prefix_table")}
+        out = torch.full((self.T, ldo), 4.0, dtype=TYPES[self.dt], device=DEV)
+        lse = torch.full((self.T, Hq), 7.0, device=DEV)
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        size = B.aweq_prefix_attention_ws(self.T, Hq, self.Hk, D, n, max_q, self.prefix, max_len)
+        ws = torch.full((size // 4 + 4,), float("nan"), device=DEV)
+        dt = B.AWEQ_F16 if self.dt == "f16" else B.AWEQ_BF16
+        starts = ints([sum(self.new[:b]) for b in range(n + 1)])
+        B.aweq_tree_attention(d["q"], dt, self.T, Hq, D, Hq * D, d["k"], d["v"], d["ks"], d["vs"], B.AWEQ_I8 if self.codes else dt, self.pages, self.page, self.Hk,
+                              d["prefix_table"], self.prefix, d["table"], self.width, ints(self.lens), starts, n, max_len, max_q, self.mask(ld).to(DEV), ld,
+                              self.scale, out, ldo, lse, ws if size else None, status, stream, ws_bytes=size)
+        assert (out[:, Hq * D:] == 4.0).all()
+        return out[:, :Hq * D].double().cpu(), lse.double().cpu(), int(status.item())
+
+    def check(self, out, lse):
+        """Within: the probabilities' rounding for the product with v (relative 2^-11 or 2^-8 each; binary16 ones are no finer than 2^-25 of the largest), the
+        output's own, and 2e-5 for scores (sums of D products in fp32 of |scores| up to some ten), exponentials and sums."""
+        G, D = self.Hq // self.Hk, self.D
+        q = self.q.double().view(self.T, self.Hk, G, D)
+        got, lse = out.view(self.T, self.Hk, G, D), lse.view(self.T, self.Hk, G)
+        unit = 2.0 ** -11 if self.dt == "f16" else 2.0 ** -8
+        p_unit = unit if not self.codes else 2.0 ** -11
+        t = 0
+        for b, (n, m) in enumerate(zip(self.lens, self.new)):
+            for i in range(m):
+                there = torch.cat((torch.ones(self.prefix + n - m, dtype=torch.bool), self.sees[b][i]))
+                k, v = (torch.cat((self.keys[0][x], self.keys[1 + b][x]), 1)[:, there] for x in range(2))
+                o, l = got[t], lse[t]
+                t += 1
+                if not there.any():
+                    assert (o == 0).all() and (l == -math.inf).all()
+                    continue
+                s = torch.matmul(q[t - 1], k.transpose(1, 2)) * self.scale
+                sizes = torch.matmul(q[t - 1].abs(), k.abs().transpose(1, 2)).amax(2) * self.scale
+                top = s.amax(2, keepdim=True)
+                e = torch.exp(s - top)
+                total = e.sum(2, keepdim=True)
+                want, around = torch.matmul(e, v) / total, torch.matmul(e, v.abs()) / total
+                score = 2e-5 + 2.0 ** -21 * sizes[..., None]
+                small = 2.0 ** -25 * int(there.sum()) * v.abs().amax() / total if p_unit == 2.0 ** -11 else 0.0
+                allowed = 1.01 * p_unit * around + 1.01 * unit * want.abs() + score * around + small + 2.0 ** -24
+                off = (o - want).abs()
+                assert (off <= allowed).all(), (b, i, float(off.max()), float((off / allowed).max()))
+                exact = (top + torch.log(total))[..., 0]
+                assert ((l - exact).abs() <= 1e-5 + 2.0 ** -21 * sizes + 2.0 ** -22 * exact.abs()).all(), (b, i, (l - exact).abs().max())
+
+    def all(self, B, **k):
+        out, lse, status = self.run(B, **k)
+        assert status == 0
+        self.check(out, lse)
+
+
+SETS = {
+    "one": ([1], [1]),
+    "some": ([40, 9, 3, 100], [5, 9, 0, 12]),
+    "word": ([64, 70, 200], [64, 63, 65]),
+    "few_behind_many": ([1500, 700], [3, 8]),
+    "wide": ([333, 150], [130, 150]),
+}
+
+
+@pytest.mark.parametrize("cache", ["f16", "bf16", "f16_i8", "bf16_i8"])
+@pytest.mark.parametrize("D,Hq,Hk,page", [(128, 4, 2, 16), (64, 3, 3, 64), (256, 2, 1, 32), (128, 8, 1, 128)])
+@pytest.mark.parametrize("which", list(SETS))
+def test_trees(B, which, D, Hq, Hk, page, cache):
+    lens, new = SETS[which]
+    for prefix in (0, 77, 640):
+        print(f"[tree] {which} D={D} Hq={Hq} Hk={Hk} page={page} {cache} prefix={prefix}", flush=True)
+        Case(cache.split("_")[0], cache.endswith("i8"), D, Hq, Hk, page, lens, new, prefix, seed=prefix + D).all(B)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("kind", ["chain", "any", "none"])
+def test_other_masks(B, kind, codes):
+    """Chains, masks without order (a token may see later ones and not itself), and masks that leave nothing."""
+    for lens, new, prefix in (([30, 8, 70], [30, 8, 66], 0), ([90, 700], [17, 20], 0), ([90, 20], [17, 20], 100)):
+        for D in (64, 128):
+            Case("f16", codes, D, 4, 2, 16, lens, new, prefix, kind=kind, seed=D).all(B, ld_extra=2)
+            Case("bf16", codes, D, 4, 1, 32, lens, new, prefix, kind=kind, seed=D, junk=True).all(B, max_len=3000, max_q=100)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("lens,new,prefix,Hq", [([40, 50], [5, 30], 0, 2), ([1500, 40], [3, 7], 0, 2), ([300, 200], [100, 90], 200, 8), ([20, 15] * 20, [3, 2] * 20, 300, 2)])
+def test_new_tokens_that_nobody_sees_may_hold_anything(B, lens, new, prefix, Hq, codes):
+    for D in (64, 128, 256):
+        Case("bf16", codes, D, Hq, 2, 16, lens, new, prefix, kind="any", seed=D, hide=True).all(B)
+        Case("f16", codes, D, Hq, 2, 16, lens, new, prefix, kind="none", seed=D, hide=True).all(B)
+
+
+@pytest.mark.parametrize("lens,new,prefix,Hq", [([40, 50], [5, 30], 0, 2), ([1500, 40], [3, 7], 0, 2), ([300, 200], [100, 90], 200, 8)])
+def test_values_that_are_not_finite_reach_those_who_see_them(B, lens, new, prefix, Hq):
+    """And nobody else: one new token's value is infinite at one place and NaN at another."""
+    for dt in ("f16", "bf16"):
+        c = Case(dt, False, 64, Hq, 2, 16, lens, new, prefix)
+        plain = c.run(B)[0]
+        at = lens[0] - new[0] + 1
+        page, row = int(c.table[0, at // 16]), at % 16
+        c.v[page, 1, row, 3], c.v[page, 1, row, 40] = float("inf"), float("nan")
+        out = c.run(B)[0].view(c.T, Hq, 64)
+        plain = plain.view(c.T, Hq, 64)
+        hit = torch.zeros(c.T, Hq, 64, dtype=torch.bool)
+        sees = torch.zeros(c.T, dtype=torch.bool)
+        sees[:new[0]] = c.sees[0][:, 1]
+        hit[sees, Hq // 2:, 3] = hit[sees, Hq // 2:, 40] = True
+        assert not torch.isfinite(out[hit]).any() and sees.any()
+        assert torch.isfinite(out[~hit]).all()
+        assert torch.allclose(out[~hit], plain[~hit], rtol=2.0 ** -6, atol=2.0 ** -9)
+
+
+def test_a_chain_is_the_prefix_attention(B):
+    """Masks of chains see what the prefix attention's tokens see."""
+    c = Case("f16", False, 128, 8, 2, 16, [90, 500, 33], [4, 60, 33], 50, kind="chain")
+    out, lse, status = c.run(B)
+    d = {k: getattr(c, k).to(DEV) for k in ("q", "k", "v", "table", "prefix_table")}
+    other, l2 = torch.empty(c.T, 1024, dtype=torch.float16, device=DEV), torch.empty(c.T, 8, device=DEV)
+    size = B.aweq_prefix_attention_ws(c.T, 8, 2, 128, 3, 60, 50, 500)
+    B.aweq_prefix_attention(d["q"], B.AWEQ_F16, c.T, 8, 128, 1024, d["k"], d["v"], None, None, B.AWEQ_F16, c.pages, 16, 2, d["prefix_table"], 50, d["table"], c.width,
+                            ints(c.lens), ints([0, 4, 64, 97]), 3, 500, 60, c.scale, other, 1024, l2, torch.empty(max(16, size), dtype=torch.uint8, device=DEV), ws_bytes=size)
+    assert (out - other.double().cpu()).abs().max() <= 2.0 ** -10 * 8 and (lse - l2.double().cpu()).abs().max() <= 1e-4
+
+
+def test_out_of_range(B):
+    c = Case("f16", False, 128, 4, 2, 16, [40, 70], [8, 9], 20)
+    c.table[1, 2] = c.pages
+    assert c.run(B)[2] == B.ST_INDEX
+    c = Case("f16", False, 128, 4, 2, 16, [40, 70], [8, 9], 20)
+    assert c.run(B, max_len=60)[2] == B.ST_INDEX
+    c.lens = [40, 5]            # fewer than its new tokens
+    assert c.run(B, max_len=70)[2] == B.ST_INDEX
+
+
+def test_repeats_are_the_same_to_the_bit_and_streams(B):
+    c = Case("f16", False, 128, 8, 2, 16, [900, 50, 333], [9, 20, 3], 700, seed=2)
+    a, b = c.run(B), c.run(B)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        d = c.run(B)
+    side.synchronize()
+    for x in (b, d):
+        assert torch.equal(a[0], x[0]) and torch.equal(a[1], x[1])
