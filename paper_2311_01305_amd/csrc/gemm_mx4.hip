@@ -26,5 +26,7 @@ extern "C" int aweq_mx4_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, i
         const int rc = launch_quant_mx4(X, x_dt, T, K, ldx, factor, xq, x_scale, status, st);
         if (rc != AWEQ_OK) return rc;
     }
+    const MxTiledPlan tiled = plan_mx4_tiled(T, N, K);
+    if (T > 64 && tiled.rc == AWEQ_OK) return launch_mx4_tiled(g, tiled, st);
     return launch_mx4_few(g, st);
 }

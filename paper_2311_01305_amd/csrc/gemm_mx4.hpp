@@ -21,6 +21,15 @@ struct MxIn {
 constexpr int kMxQuantTokens = 4;
 constexpr int64_t kMxQuantBytes = 16384;
 
+// Tiles of 256 tokens (half: 128) x 256 channels; rounds of 256 workgroups with the larger ones
+struct MxTiledPlan {
+    bool half;
+    double rounds;
+    int rc;
+};
+MxTiledPlan plan_mx4_tiled(int64_t T, int64_t N, int64_t K);
+int launch_mx4_tiled(const MxArgs& g, const MxTiledPlan& p, hipStream_t st);
+
 int launch_mx4_few(const MxArgs& g, hipStream_t st);
 int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, hipStream_t st);
 

@@ -204,7 +204,8 @@ def check(out, x, w, b, out_dt):
 
 
 SIZES = [(1, 4, 32), (1, 64, 4096), (2, 100, 544), (3, 20, 96), (4, 2052, 1056), (5, 36, 2080), (16, 64, 512), (17, 48, 1024), (31, 132, 640), (33, 260, 1536),
-         (64, 128, 4608), (65, 516, 128), (100, 1028, 2016), (129, 260, 384), (200, 300, 5152), (257, 516, 1120), (300, 260, 160), (511, 8196, 256), (700, 2100, 1088)]
+         (64, 128, 4608), (65, 516, 128), (100, 1028, 2016), (129, 260, 384), (200, 300, 5152), (257, 516, 1120), (300, 260, 160), (511, 8196, 256), (700, 2100, 1088),
+         (130, 1300, 9056), (260, 512, 4160), (1000, 1036, 1440), (2300, 260, 800), (4200, 4100, 1312), (6000, 2052, 928), (900, 9000, 992)]
 
 
 @pytest.mark.parametrize("T,N,K", SIZES)
