@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libaweq.so")
 # the Python side of the calls: for one interpreter version, which the name says, so that another one does not take it for its own
 NATIVE = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.hip", "stats.hip", "equalize.hip", "quant_weight.hip", "quant_act.hip", "gemm_i8.hip", "gemm_i8_few.hip", "gemm_i8_mid.hip", "gemm_wonly.hip", "gemm_wonly_small.hip", "gemm_wonly_mid.hip", "bias.hip", "weight_pass.hip", "calibrate.hip", "quant_token.hip", "rope.hip", "attention.hip", "attention_tree.hip",
-           "quant_mx4.hip", "gemm_mx4.hip", "gemm_mx4_few.hip", "gemm_mx4_tiled.hip", "drafts.hip"]
+           "quant_mx4.hip", "gemm_mx4.hip", "gemm_mx4_few.hip", "gemm_mx4_tiled.hip", "gemm_mx4_mid.hip", "drafts.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-I", INCLUDE, "-I", CSRC]

@@ -1011,6 +1011,21 @@ __device__ __forceinline__ bool wide_block(const Args& g, const Job& j, char* ld
 // tile by itself: 8-bit codes, row tiles of 64, 5 tokens of 16 sequences of up to 6000 keys 42.0 us -> 36.6; binary16, 711 tokens x 8 heads 21.5 -> 20.0)
 constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : MT == 1 ? 2 : 1; }
 
+// (trees) The n-th longest of up to 64 sequences: workgroups are dealt out in order, and the last ones to begin should be short (us, as they come -> longest
+// first: 40 tokens x 8 heads of 24 sequences of 2000 - 9000 keys behind 2000, codes, 520 -> 422; 8 x 4 of 40 of 500 - 4000 84 -> 65, binary16 97 -> 88; 211 x 4 of 5 of up to 3333
+// behind 4111 126 -> 118)
+__device__ __forceinline__ int longest_first(const int32_t* lens, int B, int n)
+{
+    if (B < 2 || B > kWave) return n;
+    const int lane = (int)threadIdx.x & (kWave - 1), mine = lane < B ? lens[lane] : 0;
+    int ahead = 0;
+    for (int i = 0; i < B; ++i) {
+        const int other = __builtin_amdgcn_readlane(mine, i);
+        ahead += other > mine || (other == mine && i < lane) ? 1 : 0;
+    }
+    return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < B && ahead == n));
+}
+
 // MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it.  STREAM (MT 0): keys and values past the caches (rule and figures at the launch)
 template <class E, int D, int MT, bool STREAM, bool SEEN, bool TREE>
 __device__ __forceinline__ bool attention_block(const Args& g, int block, char* lds)
@@ -1021,7 +1036,11 @@ __device__ __forceinline__ bool attention_block(const Args& g, int block, char* 
     // Workgroup ids go round-robin over the XCDs: all row tiles of one range of a key head to the same one, whose L2 then has the range's K and V
     const int seq = id / kXcdCount, combo = seq / w.row_tiles * kXcdCount + id % kXcdCount;
     if (combo >= w.combos) return false;
-    const int split = combo / g.Hk % w.splits, b = combo / g.Hk / w.splits;
+    const int split = combo / g.Hk % w.splits;
+    int b = combo / g.Hk / w.splits;
+    if constexpr (TREE) {
+        if (!shared) b = longest_first(g.lens, w.combos / (g.Hk * w.splits), b);
+    }
     const int tile_rows = w.tall ? kWaves * 16 * MT : kWideRows;
     Job j;
     j.kvh = combo % g.Hk;

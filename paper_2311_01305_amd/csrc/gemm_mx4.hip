@@ -1,6 +1,51 @@
 // Product in microscaled 4-bit floating point  out[t,n] = sum_k x[t,k] w[n,k] + bias[n]: the entry point and its choice among the forms.
 #include "gemm_mx4.hpp"
 
+namespace aweq {
+
+// What each form is modelled to take (us), from its time with a workgroup on few and on all of the 256 compute units; all are near a constant and a share of the
+// panels.  No form is below the read of the weight.  us, codes given, bfloat16 output, weights that change from call to call:
+//   tokens          1     16    32    64     128    256    512    1024   2048   4096
+//   4096 x 4096     3.1   3.5   4.1   5.1    6.7    9.5   11.5    15.2   23.5   38.9
+//   11008 x 4096    6.6   7.1   8.2   9.5   11.2   13.1   18.6    29.8   51.9    102
+//   8192 x 8192     7.7   7.9   8.7  10.2   15.4   18.6   25.1    38.3   64.0    126
+//   22016 x 8192   17.4  18.6  20    21.4   28.4   36.7   60       108    190    353      (90 MB of codes: 5.4 TB/s at one token)
+struct MxPlan {
+    enum { kFew, kMid, kTiled } form;
+    int a, b;          // few: tt, nt; mid: square; tiled: mi
+    double us;
+};
+
+static MxPlan plan_mx4(int64_t T, int64_t N, int64_t K)
+{
+    const double panels = (double)mx_panels(K), read = 2.2 + (double)N * (double)K * (17.0 / 32.0) / 5.2e6;
+    MxPlan best = {MxPlan::kFew, 1, 1, 1e300};
+    auto offer = [&](int form, int a, int b, double us) {
+        if (us < read) us = read;
+        if (us < best.us) best = {static_cast<decltype(best.form)>(form), a, b, us};
+    };
+    auto rounds = [&](int bm, int bn) { return (double)cdiv(cdiv(T, bm) * cdiv(N, bn), 256); };
+    // few tokens: a round of workgroups in us a panel; two or more share a compute unit (one token's, two tokens' tiles)
+    struct { int tt, nt; double us; } const few[] = {{1, 2, 0.085}, {1, 1, 0.045}, {2, 1, 0.066}, {2, 2, 0.1}, {4, 2, 0.14}, {4, 4, 0.22}};
+    for (const auto& f : few)
+        if (T <= 16 * f.tt * 8) offer(MxPlan::kFew, f.tt, f.nt, 2.2 + panels * f.us * rounds(16 * f.tt, 16 * f.nt));
+    // some hundred: rounds after the first take longer, since nothing of one overlaps with the next
+    if (T > 16 && T <= 2048) {
+        offer(MxPlan::kMid, 0, 0, 5.0 + panels * (0.19 + 0.26 * (rounds(64, 128) - 1.0)));
+        offer(MxPlan::kMid, 1, 0, 5.0 + panels * (0.33 + 0.42 * (rounds(128, 128) - 1.0)));
+    }
+    // many: a tile takes 0.11 + 0.105 mi us a panel with most compute units idle, 1.74 times that with none
+    for (int mi = 4; mi >= 1; --mi) {
+        int64_t tiles = 0, turns = 0;
+        if (!plan_mx4_tiled(T, N, K, mi, tiles, turns)) continue;
+        const double last = (double)(tiles - (turns - 1) * 256) / 256.0, busy = last > 0.4 ? 1.0 + 0.74 * (last - 0.4) / 0.6 : 1.0;
+        offer(MxPlan::kTiled, mi, 0, 5.0 + panels * (0.11 + 0.105 * mi) * (1.74 * (double)(turns - 1) + (busy < 1.74 ? busy : 1.74)));
+    }
+    return best;
+}
+
+}  // namespace aweq
+
 using namespace aweq;
 
 extern "C" int aweq_mx4_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, int64_t K, int64_t ldx, const float* factor, uint8_t* xq, uint8_t* x_scale,
@@ -21,12 +66,14 @@ extern "C" int aweq_mx4_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, i
     g.bias = bias; g.out = out; g.ldo = ldo; g.status = status;
     g.out_kind = out_dt == AWEQ_F16 ? kMxF16 : out_dt == AWEQ_BF16 ? kMxBf16 : kMxF32;
     hipStream_t st = as_stream(stream);
-    if (X && T <= kMxQuantTokens && T * mx_panels(K) * 64 <= kMxQuantBytes) return launch_mx4_few_quant(g, MxIn{X, ldx, factor, xq, x_scale}, x_dt, st);
+    const MxPlan p = plan_mx4(T, N, K);
+    if (X && p.form == MxPlan::kFew && p.a == 1 && T <= kMxQuantTokens && T * mx_panels(K) * 64 <= kMxQuantBytes)
+        return launch_mx4_few_quant(g, MxIn{X, ldx, factor, xq, x_scale}, x_dt, p.b, st);
     if (X) {
         const int rc = launch_quant_mx4(X, x_dt, T, K, ldx, factor, xq, x_scale, status, st);
         if (rc != AWEQ_OK) return rc;
     }
-    const MxTiledPlan tiled = plan_mx4_tiled(T, N, K);
-    if (T > 64 && tiled.rc == AWEQ_OK) return launch_mx4_tiled(g, tiled, st);
-    return launch_mx4_few(g, st);
+    if (p.form == MxPlan::kFew) return launch_mx4_few(g, p.a, p.b, st);
+    if (p.form == MxPlan::kMid) return launch_mx4_mid(g, p.a != 0, st);
+    return launch_mx4_tiled(g, p.a, st);
 }

@@ -21,16 +21,14 @@ struct MxIn {
 constexpr int kMxQuantTokens = 4;
 constexpr int64_t kMxQuantBytes = 16384;
 
-// Tiles of 256 tokens (half: 128) x 256 channels; rounds of 256 workgroups with the larger ones
-struct MxTiledPlan {
-    bool half;
-    double rounds;
-    int rc;
-};
-MxTiledPlan plan_mx4_tiled(int64_t T, int64_t N, int64_t K);
-int launch_mx4_tiled(const MxArgs& g, const MxTiledPlan& p, hipStream_t st);
+// Tiles of 64 mi tokens x 256 channels: how many, and in how many rounds of 256 workgroups; false: too many for a launch
+bool plan_mx4_tiled(int64_t T, int64_t N, int64_t K, int mi, int64_t& tiles, int64_t& rounds);
+int launch_mx4_tiled(const MxArgs& g, int mi, hipStream_t st);
+// Some hundred tokens: tiles of 64 x 128, or 128 x 128
+int launch_mx4_mid(const MxArgs& g, bool square, hipStream_t st);
 
-int launch_mx4_few(const MxArgs& g, hipStream_t st);
-int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, hipStream_t st);
+// Few tokens: tiles of 16 tt tokens x 16 nt channels
+int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st);
+int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, int nt, hipStream_t st);
 
 }  // namespace aweq

@@ -215,20 +215,18 @@ static int launch_tile(MxArgs g, hipStream_t st, MxIn in = {})
 }
 }  // namespace mxfew
 
-int launch_mx4_few(const MxArgs& g, hipStream_t st)
+int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st)
 {
-    const bool wide = g.N > 6144;
-    if (g.T <= 16) return wide ? mxfew::launch_tile<1, 2>(g, st) : mxfew::launch_tile<1, 1>(g, st);
-    if (g.T <= 32) return wide ? mxfew::launch_tile<2, 2>(g, st) : mxfew::launch_tile<2, 1>(g, st);
-    return wide ? mxfew::launch_tile<4, 2>(g, st) : mxfew::launch_tile<2, 2>(g, st);
+    if (tt == 1) return nt == 1 ? mxfew::launch_tile<1, 1>(g, st) : mxfew::launch_tile<1, 2>(g, st);
+    if (tt == 2) return nt == 1 ? mxfew::launch_tile<2, 1>(g, st) : mxfew::launch_tile<2, 2>(g, st);
+    return nt == 2 ? mxfew::launch_tile<4, 2>(g, st) : mxfew::launch_tile<4, 4>(g, st);
 }
 
-int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, hipStream_t st)
+int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, int nt, hipStream_t st)
 {
-    const bool wide = g.N > 6144;
-    if (dt == AWEQ_F16) return wide ? mxfew::launch_tile<1, 2, _Float16>(g, st, in) : mxfew::launch_tile<1, 1, _Float16>(g, st, in);
-    if (dt == AWEQ_BF16) return wide ? mxfew::launch_tile<1, 2, __bf16>(g, st, in) : mxfew::launch_tile<1, 1, __bf16>(g, st, in);
-    return wide ? mxfew::launch_tile<1, 2, float>(g, st, in) : mxfew::launch_tile<1, 1, float>(g, st, in);
+    if (dt == AWEQ_F16) return nt == 2 ? mxfew::launch_tile<1, 2, _Float16>(g, st, in) : mxfew::launch_tile<1, 1, _Float16>(g, st, in);
+    if (dt == AWEQ_BF16) return nt == 2 ? mxfew::launch_tile<1, 2, __bf16>(g, st, in) : mxfew::launch_tile<1, 1, __bf16>(g, st, in);
+    return nt == 2 ? mxfew::launch_tile<1, 2, float>(g, st, in) : mxfew::launch_tile<1, 1, float>(g, st, in);
 }
 
 }  // namespace aweq

@@ -17,24 +17,29 @@ namespace mxtiled {
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 
-constexpr int kThreads = 512, BN = 256;
+constexpr int BN = 256;
 
 struct Args : MxArgs, TileWalk {};
 
+constexpr int kThreads = 512, kWaves = 8, kWn = 4;   // wavefronts: 2 x 4
+constexpr int NJ = 2;                                // MI x 2 instruction tiles each (MI x 4, with half as many wavefronts, reads a third less of LDS and is slower:
+                                                     // us, 8192 x 8192 x 22016 615 -> 652, 4096 x 4096 x 4096 37.4 -> 41.1)
 template <int MI>
 struct Tile {
     static constexpr int kRows = 64 * MI;
     static constexpr int kHalfA = kRows * 64;                     // token rows of a slot, then 16 KiB of weight rows
-    static constexpr int kSlot = kHalfA + BN * 64;                // 32 KiB / 24 KiB
-    static constexpr int kSlots = MI == 4 ? 4 : 5;
+    static constexpr int kSlot = kHalfA + BN * 64;                // 16 KiB + 4 MI KiB
+    static constexpr int kSlots = MI >= 3 ? 4 : 5;
     static constexpr int kAhead = kSlots - 1;                     // panels requested ahead of the one being multiplied
-    static constexpr int kLoads = MI / 2 + 2;                     // load instructions per wavefront and panel
+    static constexpr int kLoadsA = (4 * MI + kWaves - 1) / kWaves;   // load instructions per wavefront and panel, 16 rows each (MI odd: some rows twice)
+    static constexpr int kLoadsB = 16 / kWaves, kLoadsS = 8 / kWaves;   // of the weight, and of a group's scales
+    static constexpr int kLoads = kLoadsA + kLoadsB;
     static constexpr int kSlabs = kAhead * kSlot;                 // 4 KiB per wavefront for the outputs: the last slot and what is behind it
     static constexpr int kScales = 128 * 1024;                    // two slots of (kRows + 256) * 16 bytes
     static constexpr int kScaleSlot = (kRows + BN) * 16;
     static constexpr int kBias = kScales + 2 * kScaleSlot;        // 1 KiB
     static constexpr int kLds = kBias + 1024;
-    static_assert(kSlabs + 8 * 4096 <= kScales && kSlots * kSlot <= kScales, "");
+    static_assert(kSlabs + 8 * 4096 <= kScales && kSlots * kSlot <= kScales, "the ring, then the scales");
 };
 
 // chunk swizzle for 64-byte slot rows: 16 consecutive rows read at one chunk index land on distinct banks
@@ -60,10 +65,11 @@ template <int MI, int OUT>
 __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
 {
     using TL = Tile<MI>;
+    constexpr int kFirstRow = 32 * MI, kFirstCol = 32 * NJ;
     constexpr int kSlot = TL::kSlot, kHalfA = TL::kHalfA, kAhead = TL::kAhead, kLoads = TL::kLoads;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 2, wn = wave & 3;
+    const int wm = wave / kWn, wn = wave % kWn;
     const int stride = gridDim.x;
 
     int vb = blockIdx.x, tile_m = 0, tile_n = 0;
@@ -74,25 +80,27 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
     const int nh = (int)mx_panels(g.K);
     const int pre = nh < kAhead ? nh : kAhead;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    const uint32_t wave_offA = wave * (512 * MI), wave_offB = kHalfA + wave * 2048;
-
-    uint32_t oa[MI / 2], ob[2], os;   // byte offsets from the tile's first row inside a panel, of scales
+    // load q of this wavefront: rows of group (16 of them) wave + kWaves q, of the tokens around again where their groups are not a multiple
+    uint32_t oa[TL::kLoadsA], ob[TL::kLoadsB], os[TL::kLoadsS];   // byte offsets from the tile's first row inside a panel, of scales
+    auto groupA = [&](int q) { return (wave + kWaves * q) % (4 * MI); };
     const uint8_t *srcA, *srcB;       // the tile's rows in the panel being fetched
-    const uint8_t* srcS;              // this wavefront's rows' scales in the group being fetched
-    int64_t stepS;
+    int64_t panel_group;              // the group of scales being fetched
     int64_t m0, n0;
-    // scales: wavefronts bring 64 rows each of the tokens, then of the weight (MI == 2: two of them the first rows once more, so that every one has as many loads)
-    constexpr int kScaleA = TL::kRows / 64;
-    const bool scale_b = wave >= kScaleA && wave < kScaleA + 4;
-    const int scale_row = scale_b ? (wave - kScaleA) * 64 : (wave < kScaleA ? wave : wave - kScaleA - 4) * 64;
-    const uint32_t scale_at = lds0 + TL::kScales + (uint32_t)((scale_b ? TL::kRows + scale_row : scale_row) * 16);
+    // scales: a load is 64 rows of the tokens, then of the weight (with fewer tokens some of them once more, so that every wavefront has as many)
+    auto scale_of_b = [&](int q) { return (wave + kWaves * q) % (MI + 4) >= MI; };
+    auto scale_row = [&](int q) { const int u = (wave + kWaves * q) % (MI + 4); return (u >= MI ? u - MI : u) * 64; };
 
-#define DMA_A(q) dma16(srcA, oa[q], dst_slot + wave_offA + (q) * 1024)
-#define DMA_B(q) dma16(srcB, ob[q], dst_slot + wave_offB + (q) * 1024)
+#define DMA_A(q) dma16(srcA, oa[q], dst_slot + (uint32_t)groupA(q) * 1024)
+#define DMA_B(q) dma16(srcB, ob[q], dst_slot + kHalfA + (uint32_t)(wave + kWaves * (q)) * 1024)
     uint32_t scale_slot = 0;         // where the next group's scales go
     auto fetch_scales = [&]() {
-        dma16(srcS, os, scale_at + scale_slot);
-        srcS += stepS;
+#pragma unroll
+        for (int q = 0; q < TL::kLoadsS; ++q) {
+            const bool of_b = scale_of_b(q);
+            const uint8_t* const from = of_b ? g.b_scale + (panel_group * g.N + n0) * 16 : g.a_scale + (panel_group * g.T + m0) * 16;
+            dma16(from, os[q], lds0 + TL::kScales + scale_slot + (uint32_t)((of_b ? TL::kRows : 0) + scale_row(q)) * 16);
+        }
+        ++panel_group;
         scale_slot = TL::kScaleSlot - scale_slot;
     };
     // addresses of tile (tm, tn) and its bias, first scales and first `pre` panels on their way
@@ -103,25 +111,25 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
         int lane_ = lane;
         asm volatile("" : "+v"(lane_));   // (hidden: formed again for every tile instead of living through the multiplications)
         const int last_m = (int)min((int64_t)TL::kRows, g.T - m0) - 1, last_n = (int)min((int64_t)BN, g.N - n0) - 1;
+        const int sub = lane_ >> 2, chunk = (lane_ & 3) ^ f4(sub);   // (loads start at multiples of 16 rows)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int sub = q * 16 + (lane_ >> 2), chunk = (lane_ & 3) ^ f4(sub);   // (wavefronts start at multiples of 16 rows)
-            if (q < MI / 2) oa[q] = (uint32_t)(min(wave * (8 * MI) + sub, last_m) * 64 + chunk * 16);
-            ob[q] = (uint32_t)(min(wave * 32 + sub, last_n) * 64 + chunk * 16);
-        }
-        os = (uint32_t)(min(scale_row + lane_, scale_b ? last_n : last_m) * 16);
+        for (int q = 0; q < TL::kLoadsA; ++q) oa[q] = (uint32_t)(min(groupA(q) * 16 + sub, last_m) * 64 + chunk * 16);
+#pragma unroll
+        for (int q = 0; q < TL::kLoadsB; ++q) ob[q] = (uint32_t)(min((wave + kWaves * q) * 16 + sub, last_n) * 64 + chunk * 16);
+#pragma unroll
+        for (int q = 0; q < TL::kLoadsS; ++q) os[q] = (uint32_t)(min(scale_row(q) + lane_, scale_of_b(q) ? last_n : last_m) * 16);
         srcA = g.a + m0 * 64;
         srcB = g.b + n0 * 64;
-        srcS = scale_b ? g.b_scale + n0 * 16 : g.a_scale + m0 * 16;
-        stepS = (scale_b ? g.N : g.T) * 16;
+        panel_group = 0;
         scale_slot = 0;
         if (g.bias && wave == 0) dma16(reinterpret_cast<const uint8_t*>(g.bias + n0), (uint32_t)(min(lane_ * 4, last_n - 3) * 4), lds0 + TL::kBias);
         fetch_scales();
         for (int p = 0; p < pre; ++p) {
             const uint32_t dst_slot = lds0 + p * kSlot;
-            DMA_A(0); DMA_B(0);
-            if constexpr (MI == 4) DMA_A(1);
-            DMA_B(1);
+#pragma unroll
+            for (int q = 0; q < TL::kLoadsA; ++q) DMA_A(q);
+#pragma unroll
+            for (int q = 0; q < TL::kLoadsB; ++q) DMA_B(q);
             srcA += panelA; srcB += panelB;
         }
     };
@@ -144,14 +152,14 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
         int offA[2], offB[2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            offA[ks] = (wm * (32 * MI) + fr_row) * 64 + ((ks * 2 + fr_half) ^ f4(fr_row)) * 16;
-            offB[ks] = kHalfA + (wn * 64 + fr_row) * 64 + ((ks * 2 + fr_half) ^ f4(fr_row)) * 16;
+            offA[ks] = (wm * kFirstRow + fr_row) * 64 + ((ks * 2 + fr_half) ^ f4(fr_row)) * 16;
+            offB[ks] = kHalfA + (wn * kFirstCol + fr_row) * 64 + ((ks * 2 + fr_half) ^ f4(fr_row)) * 16;
         }
-        const int offSA = TL::kScales + (wm * (32 * MI) + fr_row) * 16 + fr_half * 8;
-        const int offSB = TL::kScales + (TL::kRows + wn * 64 + fr_row) * 16 + fr_half * 8;
-        v4i a0[MI], b0[2], a1[MI], b1[2];
-        v2i sa[MI], sb[2];
-        v16f acc[MI][2];
+        const int offSA = TL::kScales + (wm * kFirstRow + fr_row) * 16 + fr_half * 8;
+        const int offSB = TL::kScales + (TL::kRows + wn * kFirstCol + fr_row) * 16 + fr_half * 8;
+        v4i a0[MI], b0[NJ], a1[MI], b1[NJ];
+        v2i sa[MI], sb[NJ];
+        v16f acc[MI][NJ];
 
 #define RDA(dst, ks, i) dst[i] = *reinterpret_cast<const v4i*>(st + offA[ks] + (i) * 32 * 64)
 #define RDB(dst, ks, j) dst[j] = *reinterpret_cast<const v4i*>(st + offB[ks] + (j) * 32 * 64)
@@ -163,13 +171,14 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
             const char* st = lds;
 #pragma unroll
             for (int i = 0; i < MI; ++i) { RDA(a0, 0, i); RDSA(sa, i); }
-            RDB(b0, 0, 0); RDB(b0, 0, 1); RDSB(sb, 0); RDSB(sb, 1);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < NJ; ++j) { RDB(b0, 0, j); RDSB(sb, j); }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     Float4 b = {{0.0f, 0.0f, 0.0f, 0.0f}};
-                    if (g.bias) b = *reinterpret_cast<const Float4*>(lds + TL::kBias + (wn * 64 + 32 * j + 8 * q + 4 * fr_half) * 4);
+                    if (g.bias) b = *reinterpret_cast<const Float4*>(lds + TL::kBias + (wn * kFirstCol + 32 * j + 8 * q + 4 * fr_half) * 4);
 #pragma unroll
                     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -181,6 +190,8 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
         // other.  ISSUE: panel h + kAhead is fetched into the slot panel h - 1 occupied (every wave finished reading it before the
         // barrier of panel h - 1), before a group's first one the group's scales.  wait: until panel h + 1 is complete.  J: which byte the scales are in; GROUP: whether
         // h is a group's last panel (1), or not (0), or may be (2).
+        constexpr int kReads = (MI + NJ + MI * NJ / 2 - 1) / (MI * NJ / 2);        // fragments an instruction, so that half of them are enough
+        constexpr int kIssues = (kLoads + MI * NJ - 2) / (MI * NJ - 1);
         uint32_t slot = 0;   // byte offset of panel h's slot
         int h = 0;
         auto half = [&](auto j_c, auto group_c, auto issue_c, auto next_c, auto scales_c, auto wait) {
@@ -189,38 +200,28 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
             const uint32_t next_slot = slot == kAhead * kSlot ? 0 : slot + kSlot;
             const uint32_t dst_slot = lds0 + (slot == 0 ? kAhead * kSlot : slot - kSlot);
             const char* st = lds + slot;
-            SB();
-            if constexpr (MI == 4) {
-                RDA(a1, 1, 0); RDB(b1, 1, 0); RDB(b1, 1, 1); MF(a0, b0, 0, 0, 0);
+            // the second K-step's fragments and the loads one by one between the instructions
+#pragma unroll
+            for (int u = 0; u < MI * NJ; ++u) {
+                const int i = u / NJ, j = u % NJ;
                 SB();
-                if constexpr (ISSUE) {
-                    if (SCALES == 1 || (SCALES == 2 && ((h + kAhead) & 3) == 0)) fetch_scales();
-                    DMA_A(0);
+#pragma unroll
+                for (int r = 0; r < kReads; ++r) {
+                    const int f = u * kReads + r;
+                    if (f == 0) RDA(a1, 1, 0);
+                    else if (f <= NJ) RDB(b1, 1, f - 1);
+                    else if (f < MI + NJ) RDA(a1, 1, f - NJ);
                 }
-                RDA(a1, 1, 1); RDA(a1, 1, 2); MF(a0, b0, 0, 0, 1);
-                SB();
-                if constexpr (ISSUE) DMA_B(0);
-                RDA(a1, 1, 3); MF(a0, b0, 0, 1, 0);
-                SB();
-                if constexpr (ISSUE) DMA_A(1);
-                MF(a0, b0, 0, 1, 1);
-                SB();
-                if constexpr (ISSUE) DMA_B(1);
-                MF(a0, b0, 0, 2, 0); MF(a0, b0, 0, 2, 1); MF(a0, b0, 0, 3, 0); MF(a0, b0, 0, 3, 1);
-            } else {
-                RDA(a1, 1, 0); RDB(b1, 1, 0); MF(a0, b0, 0, 0, 0);
-                SB();
                 if constexpr (ISSUE) {
-                    if (SCALES == 1 || (SCALES == 2 && ((h + kAhead) & 3) == 0)) fetch_scales();
-                    DMA_A(0);
+                    if (u == 0 && (SCALES == 1 || (SCALES == 2 && ((h + kAhead) & 3) == 0))) fetch_scales();
+#pragma unroll
+                    for (int r = 0; r < kIssues; ++r) {
+                        const int f = u * kIssues + r;
+                        if (f < TL::kLoadsA) DMA_A(f);
+                        else if (f < kLoads) DMA_B(f - TL::kLoadsA);
+                    }
                 }
-                RDB(b1, 1, 1); RDA(a1, 1, 1); MF(a0, b0, 0, 0, 1);
-                SB();
-                if constexpr (ISSUE) DMA_B(0);
-                MF(a0, b0, 0, 1, 0);
-                SB();
-                if constexpr (ISSUE) DMA_B(1);
-                MF(a0, b0, 0, 1, 1);
+                MF(a0, b0, 0, i, j);
             }
             SB();
             if constexpr (ISSUE) { srcA += panelA; srcB += panelB; }
@@ -231,47 +232,50 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
                 __builtin_amdgcn_s_barrier();
                 SB();
                 st = lds + next_slot;
-                v2i na[MI], nb[2];
+                v2i na[MI], nb[NJ];
                 if constexpr (GROUP == 1) {
                     read_scale = TL::kScaleSlot - read_scale;
 #pragma unroll
                     for (int i = 0; i < MI; ++i) RDSA(na, i);
-                    RDSB(nb, 0); RDSB(nb, 1);
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) RDSB(nb, j);
                 }
-                RDA(a0, 0, 0); RDB(b0, 0, 0); RDB(b0, 0, 1); MF(a1, b1, 1, 0, 0);
-                SB();
-                if constexpr (MI == 4) {
-                    RDA(a0, 0, 1); RDA(a0, 0, 2); MF(a1, b1, 1, 0, 1);
+#pragma unroll
+                for (int u = 0; u < MI * NJ; ++u) {
+                    const int i = u / NJ, j = u % NJ;
                     SB();
-                    RDA(a0, 0, 3); MF(a1, b1, 1, 1, 0);
-                    SB();
-                    MF(a1, b1, 1, 1, 1); MF(a1, b1, 1, 2, 0); MF(a1, b1, 1, 2, 1); MF(a1, b1, 1, 3, 0); MF(a1, b1, 1, 3, 1);
-                } else {
-                    RDA(a0, 0, 1); MF(a1, b1, 1, 0, 1);
-                    SB();
-                    MF(a1, b1, 1, 1, 0); MF(a1, b1, 1, 1, 1);
+#pragma unroll
+                    for (int r = 0; r < kReads; ++r) {
+                        const int f = u * kReads + r;
+                        if (f == 0) RDA(a0, 0, 0);
+                        else if (f <= NJ) RDB(b0, 0, f - 1);
+                        else if (f < MI + NJ) RDA(a0, 0, f - NJ);
+                    }
+                    MF(a1, b1, 1, i, j);
                 }
                 SB();
                 if constexpr (GROUP == 1) {
 #pragma unroll
                     for (int i = 0; i < MI; ++i) sa[i] = na[i];
-                    sb[0] = nb[0]; sb[1] = nb[1];
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) sb[j] = nb[j];
                 } else if constexpr (GROUP == 2) {
                     if ((h & 3) == 3) {
                         read_scale = TL::kScaleSlot - read_scale;
 #pragma unroll
                         for (int i = 0; i < MI; ++i) RDSA(sa, i);
-                        RDSB(sb, 0); RDSB(sb, 1);
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) RDSB(sb, j);
                     } else {
 #pragma unroll
                         for (int i = 0; i < MI; ++i) sa[i] = v2i{(int)((uint32_t)sa[i][0] >> 8), (int)((uint32_t)sa[i][1] >> 8)};
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) sb[j] = v2i{(int)((uint32_t)sb[j][0] >> 8), (int)((uint32_t)sb[j][1] >> 8)};
+                        for (int j = 0; j < NJ; ++j) sb[j] = v2i{(int)((uint32_t)sb[j][0] >> 8), (int)((uint32_t)sb[j][1] >> 8)};
                     }
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < MI; ++i) { MF(a1, b1, 1, i, 0); MF(a1, b1, 1, i, 1); }
+                for (int u = 0; u < MI * NJ; ++u) MF(a1, b1, 1, u / NJ, u % NJ);
             }
             slot = next_slot;
             ++h;
@@ -286,7 +290,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
             constexpr int J = decltype(j_c)::value;
             constexpr bool scales = (J + 2) % 4 == 0 || (J + 3) % 4 == 0 || (kAhead > 3 && (J + 4) % 4 == 0);
             half(j_c, integral_constant<int, J == 3 ? 1 : 0>{}, true_type{}, true_type{}, integral_constant<int, (J + kAhead) % 4 == 0 ? 1 : 0>{}, [&]() {
-                if (J >= kAhead - 1 || !relaxed || h >= 4) wait_vm<(kAhead - 1) * kLoads + (scales ? 1 : 0)>();
+                if (J >= kAhead - 1 || !relaxed || h >= 4) wait_vm<(kAhead - 1) * kLoads + (scales ? TL::kLoadsS : 0)>();
             });
         };
         while (h + kAhead + 3 < nh) {
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
         asm volatile("" : "+v"(lane_));
         char* const slab = lds + TL::kSlabs + wave * 4096;
         const int tok = lane_ & 31, part = lane_ >> 5;
-        const int64_t wave_t = cm0 + wm * (32 * MI), wave_n = cn0 + wn * 64;
+        const int64_t wave_t = cm0 + wm * kFirstRow, wave_n = cn0 + wn * kFirstCol;
         const bool inside = cm0 + TL::kRows <= g.T && cn0 + BN <= g.N;
         if constexpr (OUT == kMxF32) {
             // 32 channels at a time: rows of 128 bytes, 8 lanes each
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int j = 0; j < NJ; ++j) {
                     wave_lds_fence();
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -354,11 +358,13 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
             for (int i = 0; i < MI; ++i) {
                 wave_lds_fence();
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 4; ++q) {
+                        const v16f& a = acc[i][j];
                         *reinterpret_cast<e4*>(slab + tok * 128 + ((8 * j + 2 * q + part) ^ (tok & 15)) * 8) =
-                            e4{(E)acc[i][j][4 * q], (E)acc[i][j][4 * q + 1], (E)acc[i][j][4 * q + 2], (E)acc[i][j][4 * q + 3]};
+                            e4{(E)a[4 * q], (E)a[4 * q + 1], (E)a[4 * q + 2], (E)a[4 * q + 3]};
+                    }
                 wave_lds_fence();
 #pragma unroll
                 for (int p = 0; p < 8; ++p) {
@@ -383,37 +389,33 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
 
 }  // namespace mxtiled
 
-// Rounds of 256 workgroups; the half as tall tiles are taken where theirs, at a little over half the time, are fewer
-MxTiledPlan plan_mx4_tiled(int64_t T, int64_t N, int64_t K)
+bool plan_mx4_tiled(int64_t T, int64_t N, int64_t K, int mi, int64_t& tiles, int64_t& rounds)
 {
-    constexpr double kHalfTile = 0.57;
-    mxtiled::Args g = {}, h = {};
+    mxtiled::Args g = {};
     int64_t blocks = 0;
-    MxTiledPlan p = {false, 1e30, AWEQ_OK};
-    p.rc = plan_walk(g, T, N, K / 2, 256, blocks);
-    if (p.rc != AWEQ_OK) return p;
-    p.rounds = (double)rounds_of(g);
-    if (plan_walk(h, T, N, K / 2, 128, blocks) == AWEQ_OK && kHalfTile * (double)rounds_of(h) < p.rounds && cdiv(T, 256) * cdiv(N, 256) <= 6 * 256) {
-        p.half = true;
-        p.rounds = kHalfTile * (double)rounds_of(h);
-    }
-    return p;
+    if (plan_walk(g, T, N, K / 2, 64 * mi, blocks) != AWEQ_OK) return false;
+    tiles = (int64_t)g.tiles_m * g.tiles_n;
+    rounds = rounds_of(g);
+    return true;
 }
 
-int launch_mx4_tiled(const MxArgs& m, const MxTiledPlan& p, hipStream_t st)
+template <int MI>
+static int launch_tile(mxtiled::Args& g, hipStream_t st)
+{
+    const void* fn = g.out_kind == kMxF32   ? reinterpret_cast<const void*>(mxtiled::gemm_mx4_tiled<MI, kMxF32>)
+                     : g.out_kind == kMxF16 ? reinterpret_cast<const void*>(mxtiled::gemm_mx4_tiled<MI, kMxF16>)
+                                            : reinterpret_cast<const void*>(mxtiled::gemm_mx4_tiled<MI, kMxBf16>);
+    return launch_persistent(fn, mxtiled::kThreads, mxtiled::Tile<MI>::kLds, &g, g.n_ids, st);
+}
+
+int launch_mx4_tiled(const MxArgs& m, int mi, hipStream_t st)
 {
     mxtiled::Args g = {};
     static_cast<MxArgs&>(g) = m;
     int64_t blocks = 0;
-    const int rc = plan_walk(g, g.T, g.N, g.K / 2, p.half ? 128 : 256, blocks);
+    const int rc = plan_walk(g, g.T, g.N, g.K / 2, 64 * mi, blocks);
     if (rc != AWEQ_OK) return rc;
-    const void* fn = nullptr;
-#define AWEQ_PICK(O)                                                                                                   \
-    if (g.out_kind == O)                                                                                               \
-        fn = p.half ? reinterpret_cast<const void*>(mxtiled::gemm_mx4_tiled<2, O>) : reinterpret_cast<const void*>(mxtiled::gemm_mx4_tiled<4, O>);
-    AWEQ_PICK(kMxF32) AWEQ_PICK(kMxF16) AWEQ_PICK(kMxBf16)
-#undef AWEQ_PICK
-    return launch_persistent(fn, mxtiled::kThreads, p.half ? mxtiled::Tile<2>::kLds : mxtiled::Tile<4>::kLds, &g, g.n_ids, st);
+    return mi == 4 ? launch_tile<4>(g, st) : mi == 3 ? launch_tile<3>(g, st) : mi == 2 ? launch_tile<2>(g, st) : launch_tile<1>(g, st);
 }
 
 }  // namespace aweq
