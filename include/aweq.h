@@ -494,8 +494,8 @@ int aweq_tree_mask(const int32_t* parent, int64_t T, const int32_t* q_start, int
 
 /* ---- aweq_prefix_attention for new tokens that do not all see one another: of its sequence's lens[b] keys a token sees the first lens[b] - m, and of the m
  * new ones (the last m) those whose bit is set in mask[t] (pitch mask_ld words >= ceil(max_q / 64); any bits, its own or not).  All else, limits and scratch
- * memory (aweq_prefix_attention_ws, aweq_prefix_attention_ws_most) as there; a row without any key gets zeros and lse -inf, and what a token does not
- * see has no part in its out, whatever it holds.  q_start is required, and table if max_len > 0; lens[b] < m: AWEQ_ST_INDEX (results of that sequence unspecified). */
+ * memory (aweq_prefix_attention_ws, aweq_prefix_attention_ws_most) as there; a row without any key gets zeros and lse -inf, what a token does not
+ * see has no part in its out, whatever it holds, and rows past q_start[B] (a batch that is filled up) are left as they are; q_start[0] is 0.  q_start is required, and table if max_len > 0; lens[b] < m: AWEQ_ST_INDEX (results of that sequence unspecified). */
 int aweq_tree_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int64_t D, int64_t ldq,
                         const void* k_cache, const void* v_cache, const float* k_step, const float* v_step, aweq_dtype cache_dt,
                         int64_t pages, int64_t page_size, int64_t Hk, const int32_t* prefix_table, int64_t prefix_len,

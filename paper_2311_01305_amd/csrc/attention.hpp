@@ -87,6 +87,7 @@ struct Args {
     int prefix_len, max_len;
     int pages, page_size, page_shift;
     int Hq, Hk, G, max_q;
+    int B;
     int q_bf16;         // type of q and out (an 8-bit cache: either)
     int parts;          // of a row: 1: the result itself
     int fused;          // a sequence's rows take the prefix along
@@ -1011,6 +1012,9 @@ __device__ __forceinline__ bool wide_block(const Args& g, const Job& j, char* ld
 // tile by itself: 8-bit codes, row tiles of 64, 5 tokens of 16 sequences of up to 6000 keys 42.0 us -> 36.6; binary16, 711 tokens x 8 heads 21.5 -> 20.0)
 constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : MT == 1 ? 2 : 1; }
 
+// (trees) Rows of the sequences: those behind them are left as they are
+__device__ __forceinline__ int64_t rows_of_batch(const Args& g) { return min(max((int64_t)scalar_at(g.q_start, g.B), (int64_t)0), g.T); }
+
 // (trees) The n-th longest of up to 64 sequences: workgroups are dealt out in order, and the last ones to begin should be short (us, as they come -> longest
 // first: 40 tokens x 8 heads of 24 sequences of 2000 - 9000 keys behind 2000, codes, 520 -> 422; 8 x 4 of 40 of 500 - 4000 84 -> 65, binary16 97 -> 88; 211 x 4 of 5 of up to 3333
 // behind 4111 126 -> 118)
@@ -1052,7 +1056,8 @@ __device__ __forceinline__ bool attention_block(const Args& g, int block, char* 
     uint32_t est = 0;
     if (shared) {
         j.t0 = 0;
-        j.rows = (int)g.T * g.G;
+        j.rows = (int)(TREE ? rows_of_batch(g) : g.T) * g.G;
+        if (j.row0 >= j.rows) return false;
         j.pa = split * w.chunk;
         j.pb = min(j.pa + w.chunk, g.prefix_len);
     } else {
@@ -1112,14 +1117,14 @@ constexpr int kJoinParts = 256;
 
 // A row's parts joined by W wavefronts: a lane has the maximum and sum of the parts lane, lane + 64, .., wavefront v takes the values of the parts 64 c + W i
 // + v, D / 4 lanes to a part, kFlight of them in flight
-template <int D, int W>
+template <int D, int W, bool TREE>
 __global__ __launch_bounds__(256) void join_kernel(Args g)
 {
     constexpr int kRowsOf = 4 / W;   // rows of a workgroup
     __shared__ f32x4 s_part[W > 1 ? W : 1][W > 1 ? D / 4 : 1];
     const int wave = threadIdx.x / kWave, slice = wave % W, lane = threadIdx.x & (kWave - 1);
     const int64_t row = (int64_t)blockIdx.x * kRowsOf + wave / W, all_rows = g.T * g.Hq;
-    if (row >= all_rows) return;     // (W > 1: all of the workgroup or nobody)
+    if (row >= (TREE ? rows_of_batch(g) * g.Hq : all_rows)) return;     // (W > 1: all of the workgroup or nobody)
     constexpr int kLanes = D / 4, kAtOnce = kWave / kLanes, kOf = W > 1 ? kJoinParts / kWave : 1, kFlight = 8;
     const int sub = lane / kLanes, at = lane % kLanes * 4;
     float2 ml[kOf];
@@ -1298,8 +1303,8 @@ static int launch(Args& g, const Plan& p, hipStream_t st)
     if (rc == AWEQ_OK && g.parts > 1) {
         const int64_t rows = g.T * g.Hq;
         // (up to 64 parts a wavefront is as fast as four or faster: 2048 rows of 18 parts 35.1 us with the attention, four each 44.7)
-        if (g.parts > kWave) join_kernel<D, 4><<<(unsigned)rows, 256, 0, st>>>(g);
-        else join_kernel<D, 1><<<(unsigned)cdiv(rows, 4), 256, 0, st>>>(g);
+        if (g.parts > kWave) join_kernel<D, 4, TREE><<<(unsigned)rows, 256, 0, st>>>(g);
+        else join_kernel<D, 1, TREE><<<(unsigned)cdiv(rows, 4), 256, 0, st>>>(g);
     }
     return rc != AWEQ_OK ? rc : launch_status();
 }
@@ -1361,6 +1366,7 @@ static int attend_call(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int6
     g.out = out; g.lse = lse; g.status = status; g.mask = mask; g.mask_ld = mask_ld;
     g.T = T; g.ldq = ldq; g.ldo = ldo; g.table_ld = table_ld; g.prefix_len = (int)prefix_len; g.max_len = (int)max_len;
     g.pages = (int)pages; g.page_size = (int)page_size; g.page_shift = __builtin_ctz((unsigned)page_size);
+    g.B = (int)B;
     g.Hq = (int)Hq; g.Hk = (int)Hk; g.G = (int)(Hq / Hk); g.max_q = (int)max_q;
     g.q_bf16 = dt == AWEQ_BF16;
     g.parts = p.parts();

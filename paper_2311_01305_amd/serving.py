@@ -4,8 +4,13 @@ that all of them share.  Four calls of the library for a step of any tokens, one
 
     aweq_w8a8_gemm_tokens (q, k, v)  ->  aweq_kv_append  ->  aweq_prefix_attention  ->  aweq_w8a8_gemm_tokens (output)
 
+The projections may be 4-bit floating point instead (aweq_mx4_gemm_tokens), and the new tokens of a sequence a tree of drafts of which a path is kept
+(aweq_tree_attention); Sequences plans such steps on the device:
+
+    aweq_step_plan  ->  aweq_tree_mask  ->  the block's four calls  ->  aweq_kv_keep  ->  aweq_step_plan
+
 `python -m paper_2311_01305_amd.serving` calibrates a block's projections on synthetic activations, runs a shared prompt once and decodes a batch
-behind it.  No arithmetic of the operators happens here.
+behind it (--draft: in trees of that many tokens; --mx4: 4-bit projections).  No arithmetic of the operators happens here.
 """
 import argparse
 import time
@@ -60,6 +65,38 @@ class QuantLinear:
         return cls(sum(gb.Ns), gb.K, codes, join("step_w"), join("zero_w"), join("rowsum_w"), bias, gb.t["inv_s"] if fold else None, 0)
 
 
+@dataclass
+class Mx4Linear:
+    """A layer whose weight is in microscaled 4-bit floating point (aweq_quant_mx4), its tokens quantised the same way in the product.  factor: what the
+    input's channels are multiplied by first (an equalization's 1 / s), or None."""
+    N: int
+    K: int
+    codes: torch.Tensor
+    scales: torch.Tensor
+    bias: Optional[torch.Tensor] = None
+    factor: Optional[torch.Tensor] = None
+
+    @classmethod
+    def from_weight(cls, W: torch.Tensor, bias: Optional[torch.Tensor] = None, factor: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+        """W [N x K], float32, float16 or bfloat16, rows in one piece."""
+        if W.dim() != 2 or W.stride(1) != 1:
+            raise ValueError("a matrix whose rows are in one piece")
+        N, K = W.shape
+        if factor is not None:
+            _check("factor", factor, torch.float32, (K,), W.device)
+        if bias is not None:
+            _check("bias", bias, torch.float32, (N,), W.device)
+        codes, scales = (torch.empty(n(N, K), dtype=torch.uint8, device=W.device) for n in (B.aweq_mx4_code_bytes, B.aweq_mx4_scale_bytes))
+        B.aweq_quant_mx4(W, pipeline._dt(W) if W.dtype != torch.bfloat16 else B.AWEQ_BF16, N, K, W.stride(0), None, codes, scales, status)
+        return cls(N, K, codes, scales, bias, factor)
+
+    @classmethod
+    def from_layer(cls, buf: pipeline.LayerBuffers, fold: bool = True, bias: Optional[torch.Tensor] = None):
+        """The equalised weight of a layer that pipeline.calibrate_layer has been through; fold: with the equalization's 1 / s on its input."""
+        t = buf.t
+        return cls.from_weight(t["W_hat"], bias, t["inv_s"] if fold else None, t["status"])
+
+
 def _bias(t, layer, N, K, group, bias):
     """A bias less the mean output of what its layer's codes are off the folded weight by."""
     W = layer["W_hat"]
@@ -103,10 +140,79 @@ def _check(name, t, dtype, shape, device, longer=False):
         raise ValueError(f"{name}: {dtype} {list(shape)}{' or longer' if longer else ''}, in one piece, on {device}")
 
 
-class AttentionBlock:
-    """qkv [(Hq + 2 Hk) D x hidden] and out [hidden x Hq D]; buffers for max_tokens tokens of a step, allocated once."""
+class Sequences:
+    """What a batch of sequences has in a cache, kept on the device: lengths, page tables and a stack of the cache's free pages, which a step takes from and
+    gives back to without the host (all of them: the cache's own list is empty until give_back()).  Lengths and the stack's height are held twice, before and after a step: two steps, such as
+    one that appends drafts and one that drops the rejected ones, end where they began, so that both can be captured in one graph."""
 
-    def __init__(self, qkv: QuantLinear, out: QuantLinear, q_heads: int, cache: PagedCache, freq: Optional[torch.Tensor], rot: int, max_tokens: int,
+    def __init__(self, cache: PagedCache, batch: int, max_len: int, max_tokens: int, prefix_len: int = 0, max_drafts: int = 64):
+        """max_len: tokens of a sequence; max_tokens: rows of a step; max_drafts: new tokens of a sequence in a step with masks."""
+        self.cache, self.batch, self.prefix_len, self.max_tokens, self.max_drafts = cache, batch, prefix_len, max_tokens, max_drafts
+        where = cache.k.device
+        new = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device=where)
+        self.table = new(batch, max(1, -(-max_len // cache.page_size)))
+        free = cache.free
+        self.free = new(cache.pages)
+        self.free[:len(free)] = torch.tensor(free, dtype=torch.int32)
+        self.counts = [torch.tensor([len(free)], dtype=torch.int32, device=where), new(1)]
+        cache.free = []
+        self.lengths, self.at = [new(batch), new(batch)], 0
+        self.q_start, self.pos, self.slot = new(batch + 1), new(max_tokens), new(max_tokens, dtype=torch.int64)
+        self.change = new(batch)
+        self.mask = new(max_tokens, -(-max_drafts // 64), dtype=torch.int64)
+        self.status = new(1)
+
+    @property
+    def lens(self):
+        """Tokens of each sequence, after the last step."""
+        return self.lengths[self.at]
+
+    def step(self, change: torch.Tensor, tokens: int):
+        """change [batch] int32: new tokens of each sequence, or (below 0) tokens that go; tokens: rows of the step, at least the new tokens.  Returns q_start, and pos and
+        slot of the rows, buffers of this object's; nothing changes where the pages do not suffice (status ST_PAGES)."""
+        c = self.cache
+        _check("change", change, torch.int32, (self.batch,), c.k.device)
+        if not 0 < tokens <= self.max_tokens:
+            raise ValueError("one token at least, and no more than max_tokens")
+        i, o = self.at, 1 - self.at
+        pos, slot = self.pos[:tokens], self.slot[:tokens]
+        B.aweq_step_plan(self.lengths[i], change, self.batch, c.page_size, c.pages, self.table, self.table.stride(0), self.table.shape[1], self.free, self.counts[i],
+                         self.prefix_len, tokens, self.lengths[o], self.counts[o], self.q_start, pos, slot, self.status)
+        self.at = o
+        return self.q_start, pos, slot
+
+    def draft(self, parent: torch.Tensor, max_q: int):
+        """parent [tokens] int32: of each new token of the last step the place, among its sequence's, of the one that it goes on from, or -1.  Returns the masks
+        [tokens, words], and writes the step's positions: a token's is its depth in the tree behind what its sequence has."""
+        T = parent.shape[0]
+        _check("parent", parent, torch.int32, (T,), self.cache.k.device)
+        if not 0 < T <= self.max_tokens or not 0 < max_q <= self.max_drafts:
+            raise ValueError("one token at least, and no more than max_tokens and max_drafts")
+        B.aweq_tree_mask(parent, T, self.q_start, self.batch, max_q, self.lens, self.prefix_len, self.mask, self.mask.stride(0), self.pos, self.status)
+        return self.mask[:T]
+
+    def keep(self, kept: torch.Tensor, count: torch.Tensor, tokens: int) -> torch.Tensor:
+        """kept [batch, most] int32: of each sequence the first count[b] are the places of the drafts that are accepted, in order.  Moves them to the front and returns the change
+        that step() drops the others by."""
+        c = self.cache
+        if kept.dim() != 2 or kept.shape[1] < 1 or not 0 < tokens <= self.max_tokens:
+            raise ValueError("kept: a row of places for each sequence; tokens: the step's rows")
+        _check("kept", kept, torch.int32, (self.batch, kept.shape[1]), c.k.device)
+        _check("count", count, torch.int32, (self.batch,), c.k.device)
+        B.aweq_kv_keep(c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, c.heads, c.head_dim, self.table, self.table.stride(0), self.lens, self.q_start,
+                       self.batch, tokens, kept, kept.stride(0), count, self.change, self.status)
+        return self.change
+
+    def give_back(self):
+        """The stack's pages to the cache's own list (waits for the device); the sequences take no more."""
+        self.cache.free.extend(self.free[:int(self.counts[self.at].item())].tolist())
+        self.counts[self.at].zero_()
+
+
+class AttentionBlock:
+    """qkv [(Hq + 2 Hk) D x hidden] and out [hidden x Hq D], each a QuantLinear or a Mx4Linear; buffers for max_tokens tokens of a step, allocated once."""
+
+    def __init__(self, qkv, out, q_heads: int, cache: PagedCache, freq: Optional[torch.Tensor], rot: int, max_tokens: int,
                  interleaved: bool = False, gain: float = 1.0, q_norm=None, k_norm=None, eps: float = 1e-6, device="cuda:0"):
         D, Hk, where = cache.head_dim, cache.heads, cache.k.device
         if qkv.N != (q_heads + 2 * Hk) * D or out.K != q_heads * D:
@@ -122,11 +228,13 @@ class AttentionBlock:
         self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm, self.eps = freq, rot, interleaved, gain, q_norm, k_norm, eps
         self.max_tokens, self.device = max_tokens, device
         new = lambda *shape, dtype: torch.empty(shape, dtype=dtype, device=device)
-        self.xq = new(max(B.aweq_panel_bytes(max_tokens, qkv.K), B.aweq_panel_bytes(max_tokens, out.K)), dtype=torch.int8)
+        size = lambda layer: B.aweq_mx4_code_bytes(max_tokens, layer.K) if isinstance(layer, Mx4Linear) else B.aweq_panel_bytes(max_tokens, layer.K)
+        self.xq = new(max(size(qkv), size(out)), dtype=torch.int8)
+        self.x_scale = new(max([16] + [B.aweq_mx4_scale_bytes(max_tokens, layer.K) for layer in (qkv, out) if isinstance(layer, Mx4Linear)]), dtype=torch.uint8)
         self.step, self.zero, self.rowsum = new(max_tokens, dtype=torch.float32), new(max_tokens, dtype=torch.int32), new(max_tokens, dtype=torch.int32)
         self.qkv = new(max_tokens, qkv.N, dtype=cache.dtype)
         self.q = new(max_tokens, q_heads * D, dtype=cache.dtype)
-        self.attended = new(max_tokens, q_heads * D, dtype=cache.dtype)
+        self.attended = torch.zeros(max_tokens, q_heads * D, dtype=cache.dtype, device=device)   # (rows past a batch's tokens are left as they are, and quantised)
         self.y = new(max_tokens, out.N, dtype=cache.dtype)
         self.ws, self.kept = new(16, dtype=torch.uint8), []
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
@@ -143,12 +251,17 @@ class AttentionBlock:
 
     def _product(self, layer, x, out):
         T, dt = x.shape[0], DTYPES[x.dtype]
+        if isinstance(layer, Mx4Linear):
+            B.aweq_mx4_gemm_tokens(x, dt, T, layer.K, x.stride(0), layer.factor, self.xq, self.x_scale, layer.codes, layer.scales, layer.N, layer.bias, out, dt,
+                                   layer.N, self.status)
+            return
         B.aweq_w8a8_gemm_tokens(x, dt, T, layer.K, x.stride(0), layer.inv_s, self.xq, self.step, self.zero, self.rowsum, layer.codes, layer.N,
                                 layer.step_w, layer.zero_w, layer.w_group, layer.rowsum_w, layer.bias, out, dt, layer.N, self.status)
 
-    def __call__(self, x, pos, slot, lens, table, q_start, max_len, max_q, prefix_table=None, prefix_len=0):
+    def __call__(self, x, pos, slot, lens, table, q_start, max_len, max_q, prefix_table=None, prefix_len=0, mask=None):
         """x [T, hidden]: the step's tokens, sequence after sequence (q_start [B + 1], None: one each); pos [T] int32, slot [T] int64; lens [B]: the
-        sequences' own keys with these tokens; table [B, ..]: their pages.  Returns [T, hidden], a buffer of the block's."""
+        sequences' own keys with these tokens; table [B, ..]: their pages; mask [T, words] int64: which of its sequence's new tokens each one sees (None: those before
+        it and itself).  Returns [T, hidden], a buffer of the block's."""
         T, c = x.shape[0], self.cache
         if T > self.max_tokens or x.dtype != c.dtype:
             raise ValueError("more tokens than max_tokens, or another type than the cache's")
@@ -165,6 +278,9 @@ class AttentionBlock:
             raise ValueError(f"table: int32 [sequences, pages], each row in one piece, on {where}")
         if prefix_len:
             _check("prefix_table", prefix_table, torch.int32, (-(-prefix_len // c.page_size),), where, longer=True)
+        if mask is not None and (q_start is None or mask.device != where or mask.dtype != torch.int64 or mask.dim() != 2 or mask.shape[0] != T or
+                                 64 * mask.shape[1] < min(max_q, T) or (mask.shape[1] > 1 and mask.stride(1) != 1)):
+            raise ValueError(f"mask: int64 [{T}, a bit for each of max_q tokens], each row in one piece, on {where}, and q_start with it")
         max_len = min(max_len, table.shape[1] * c.page_size)   # (a view's pitch may be more than its pages)
         dt = DTYPES[x.dtype]
         Hq, Hk, D = self.q_heads, c.heads, c.head_dim
@@ -174,8 +290,13 @@ class AttentionBlock:
         B.aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, width, width, width, pos, self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm,
                          self.eps, self.q, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, slot, self.status)
         self._scratch(B.aweq_prefix_attention_ws(T, Hq, Hk, D, batch, max_q, prefix_len, max_len))
-        B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
-                                table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
+        if mask is None:
+            B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
+                                    table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
+        else:
+            B.aweq_tree_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
+                                  table, table.stride(0), lens, q_start, batch, max_len, max_q, mask, mask.stride(0), D ** -0.5, self.attended, Hq * D, None,
+                                  self.ws, self.status)
         self._product(self.out_layer, self.attended[:T], self.y)
         return self.y[:T]
 
@@ -189,8 +310,8 @@ def frequencies(rot: int, base: float = 10000.0, kind: int = B.ROPE_PLAIN, devic
     return host.to(device)
 
 
-def calibrated(N, K, seed, tokens=512, dtype=torch.float16, device="cuda:0") -> QuantLinear:
-    """A random layer without a bias, calibrated on random activations with loud channels."""
+def calibrated(N, K, seed, tokens=512, dtype=torch.float16, device="cuda:0", mx4=False):
+    """A random layer without a bias, calibrated on random activations with loud channels; mx4: its equalised weight in 4-bit floating point."""
     g = torch.Generator(device=device)
     g.manual_seed(seed)
     x = torch.randn(tokens, K, generator=g, device=device)
@@ -198,7 +319,26 @@ def calibrated(N, K, seed, tokens=512, dtype=torch.float16, device="cuda:0") -> 
     w = torch.randn(N, K, generator=g, device=device) * K ** -0.5
     buf = pipeline.LayerBuffers(tokens, K, N, torch.float16, want_out_i32=False, device=device)
     pipeline.calibrate_layer(x.half(), w.half(), None, buf, forward=False)
-    return QuantLinear.from_layer(buf, correct=False)
+    return Mx4Linear.from_layer(buf) if mx4 else QuantLinear.from_layer(buf, correct=False)
+
+
+def draft_steps(block, seqs, x, steps, tree, prefix_table, max_len):
+    """Steps of a batch whose sequences each draft the tokens of `tree` (parents) and keep the path to the last of them; x [batch * tokens, hidden]."""
+    m, dev = len(tree), x.device
+    path, at = [], m - 1
+    while at >= 0:
+        path.append(at)
+        at = tree[at]
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)
+    kept, count = ints([path[::-1]] * seqs.batch), ints([len(path)] * seqs.batch)
+    more, parent = ints([m] * seqs.batch), ints(tree * seqs.batch)
+    for _ in range(steps):
+        q_start, pos, slot = seqs.step(more, x.shape[0])
+        mask = seqs.draft(parent, m)
+        y = block(x, pos, slot, seqs.lens, seqs.table, q_start, max_len, m, prefix_table, seqs.prefix_len, mask)
+        seqs.step(seqs.keep(kept, count, x.shape[0]), x.shape[0])
+        x = y.clone()
+    return x, len(path)
 
 
 def main(argv=None):
@@ -210,13 +350,16 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=32)
     ap.add_argument("--steps", type=int, default=32)
     ap.add_argument("--codes", action="store_true", help="8-bit cache")
+    ap.add_argument("--mx4", action="store_true", help="projections in 4-bit floating point")
+    ap.add_argument("--draft", type=int, default=0, help="tokens of a tree that each sequence drafts in a step (0: one token a step)")
     a = ap.parse_args(argv)
     dev, D = "cuda:0", 128
     width = (a.heads + 2 * a.key_heads) * D
-    per = -(-a.steps // 64) + 1
+    most = a.steps * max(1, a.draft)        # tokens of a sequence, at most
+    per = -(-most // 64) + 1
     cache = PagedCache(-(-a.prefix // 64) + a.batch * per, 64, a.key_heads, D, codes=a.codes, device=dev)
-    block = AttentionBlock(calibrated(width, a.hidden, 1), calibrated(a.hidden, a.heads * D, 2), a.heads, cache, frequencies(D, device=dev), D,
-                           max(a.prefix, a.batch), device=dev)
+    block = AttentionBlock(calibrated(width, a.hidden, 1, mx4=a.mx4), calibrated(a.hidden, a.heads * D, 2, mx4=a.mx4), a.heads, cache, frequencies(D, device=dev), D,
+                           max(a.prefix, a.batch * max(1, a.draft)), device=dev)
     ints = lambda v, dtype=torch.int32: torch.tensor(v, dtype=dtype, device=dev)
     # the prompt once, as one sequence of its own
     pages = cache.take(a.prefix)
@@ -224,6 +367,20 @@ def main(argv=None):
     if a.prefix:
         block(x, torch.arange(a.prefix, dtype=torch.int32, device=dev), ints(cache.slots(pages, 0, a.prefix), torch.int64), ints([a.prefix]), ints([pages]),
               ints([0, a.prefix]), a.prefix, a.prefix)
+    if a.draft:
+        # then the batch behind it, a tree each: pairs of tokens that go on from the same one
+        seqs, shared = Sequences(cache, a.batch, most, a.batch * a.draft, a.prefix, a.draft), ints(pages)
+        tree = [-1] + [(i - 1) // 2 for i in range(1, a.draft)]
+        x = torch.randn(a.batch * a.draft, a.hidden, device=dev).half()
+        block.reserve(a.batch * a.draft, a.batch, a.draft, a.prefix, most)
+        torch.cuda.synchronize()
+        began = time.perf_counter()
+        x, path = draft_steps(block, seqs, x, a.steps, tree, shared, most)
+        torch.cuda.synchronize()
+        took = (time.perf_counter() - began) / a.steps
+        print(f"{a.batch} sequences behind {a.prefix} shared tokens, {a.draft} drafted and {path} kept: {took * 1e6:.1f} us a step of the block, "
+              f"status {int(block.status.item()) | int(seqs.status.item())}, output rms {x.float().pow(2).mean().sqrt().item():.3g}")
+        return
     # then the batch behind it, a token each
     own = [cache.take(a.steps) for _ in range(a.batch)]
     table, shared = ints(own), ints(pages)

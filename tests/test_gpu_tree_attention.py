@@ -255,3 +255,24 @@ def test_repeats_are_the_same_to_the_bit_and_streams(B):
     side.synchronize()
     for x in (b, d):
         assert torch.equal(a[0], x[0]) and torch.equal(a[1], x[1])
+
+
+@pytest.mark.parametrize("lens,new,prefix", [([40, 9], [5, 9], 0), ([1500, 300], [3, 40], 0), ([30, 200, 5], [1, 9, 2], 700), ([300, 200], [100, 90], 200)])
+def test_rows_behind_the_sequences_are_left_as_they_are(B, lens, new, prefix):
+    """A batch that is filled up with rows that belong to nobody, whose queries and masks are anything."""
+    for codes in (False, True):
+        c = Case("f16", codes, 64, 4, 2, 16, lens, new, prefix)
+        want = c.run(B)
+        T, ld = c.T + 7, -(-max(new) // 64)
+        q = torch.cat((c.q.to(DEV).view(c.T, -1), torch.full((7, 256), float("nan"), dtype=torch.float16, device=DEV)))
+        mask = torch.cat((c.mask(ld).to(DEV), torch.full((7, ld), -1, dtype=torch.int64, device=DEV)))
+        out, lse = torch.full((T, 256), 4.0, dtype=torch.float16, device=DEV), torch.full((T, 4), 7.0, device=DEV)
+        size = B.aweq_prefix_attention_ws(T, 4, 2, 64, len(lens), max(new), prefix, max(lens))
+        ws, status = torch.full((size // 4 + 4,), float("nan"), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        d = {k: None if getattr(c, k) is None else getattr(c, k).to(DEV) for k in ("k", "v", "ks", "vs", "table", "prefix_table")}
+        starts = ints([sum(new[:b]) for b in range(len(new) + 1)])
+        B.aweq_tree_attention(q, B.AWEQ_F16, T, 4, 64, 256, d["k"], d["v"], d["ks"], d["vs"], B.AWEQ_I8 if codes else B.AWEQ_F16, c.pages, 16, 2, d["prefix_table"], prefix,
+                              d["table"], c.width, ints(lens), starts, len(lens), max(lens), max(new), mask, ld, c.scale, out, 256, lse, ws, status, ws_bytes=size)
+        assert int(status.item()) == 0 and (out[c.T:] == 4.0).all() and (lse[c.T:] == 7.0).all()
+        c.check(out[:c.T].double().cpu(), lse[:c.T].double().cpu())
+        assert (out[:c.T].double().cpu() - want[0]).abs().max() <= 2.0 ** -9
