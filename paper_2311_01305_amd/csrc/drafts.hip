@@ -46,31 +46,43 @@ __device__ __forceinline__ int sequence_of(const int* sums, int B, int i)
     return lo;
 }
 
+// EACH: sequences of a thread, at most
+template <int EACH>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs g)
 {
-    extern __shared__ int sums[];    // [3][B + 1]: tokens, pages taken, pages given back ahead of each sequence
+    extern __shared__ int sums[];    // [3][B + 1]: tokens, pages taken, pages given back ahead of each sequence; [B]: what it had
     int* const s_new = sums;
     int* const s_take = sums + g.B + 1;
     int* const s_give = s_take + g.B + 1;
+    int* const s_len = s_give + g.B + 1;
     __shared__ long long s_part[3][kPlanWaves];
     __shared__ unsigned s_bad;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     if (tid == 0) s_bad = 0;
-    const int per = (g.B + kPlanThreads - 1) / kPlanThreads, from = min(tid * per, g.B), to = min(from + per, g.B);
+    // a thread has some sequences in a row, whose numbers it asks for at once
+    const int per = (g.B + kPlanThreads - 1) / kPlanThreads, from = min(tid * per, g.B), mine = min(per, g.B - from);
+    int len[EACH], change[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if (k < mine) { len[k] = g.lens[from + k]; change[k] = g.change[from + k]; }
     const int count = *g.free_count;
     const long long room = (long long)g.table_pages << g.page_shift;
     auto pages_of = [&](int tokens) { return (tokens + g.page_size - 1) >> g.page_shift; };
     long long add[3] = {0, 0, 0};
     bool bad = count < 0 || count > g.pages;
-    for (int b = from; b < to; ++b) {
-        const int len = g.lens[b], c = g.change[b];
-        const long long after = (long long)len + c;
-        if (len < 0 || len > room || after < 0 || after > room) { bad = true; continue; }
-        const int had = pages_of(len), has = pages_of((int)after);
-        add[0] += max(c, 0);
-        add[1] += max(has - had, 0);
-        add[2] += max(had - has, 0);
-    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if (k < mine) {
+            const long long after = (long long)len[k] + change[k];
+            if (len[k] < 0 || len[k] > room || after < 0 || after > room) {
+                bad = true;
+            } else {
+                const int had = pages_of(len[k]), has = pages_of((int)after);
+                add[0] += max(change[k], 0);
+                add[1] += max(has - had, 0);
+                add[2] += max(had - has, 0);
+            }
+        }
     __syncthreads();
     if (bad) atomicOr(&s_bad, (unsigned)AWEQ_ST_INDEX);
     long long sum[3];
@@ -106,28 +118,31 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs g)
         return;
     }
     // (the totals fit: tokens T, pages those of the tables' rows, which are at most 2^24 each; where they do not fit 32 bits the stack does not suffice)
-    for (int b = from; b < to; ++b) {
-        const int len = g.lens[b], c = g.change[b], had = pages_of(len), has = pages_of(len + c);
-        s_new[b] = (int)sum[0]; s_take[b] = (int)sum[1]; s_give[b] = (int)sum[2];
-        sum[0] += max(c, 0); sum[1] += max(has - had, 0); sum[2] += max(had - has, 0);
-    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if (k < mine) {
+            const int had = pages_of(len[k]), has = pages_of(len[k] + change[k]);
+            s_new[from + k] = (int)sum[0]; s_take[from + k] = (int)sum[1]; s_give[from + k] = (int)sum[2];
+            s_len[from + k] = len[k];
+            sum[0] += max(change[k], 0); sum[1] += max(has - had, 0); sum[2] += max(had - has, 0);
+        }
     const int tokens = (int)total[0], taken = (int)total[1], given = (int)total[2];
     if (tid == 0) { s_new[g.B] = tokens; s_take[g.B] = taken; s_give[g.B] = given; }
     __syncthreads();
     auto returned = [&](int i) {         // the i-th page that is given back
         const int b = sequence_of(s_give, g.B, i);
-        return g.table[b * g.table_ld + pages_of(g.lens[b] + g.change[b]) + (i - s_give[b])];
+        return g.table[b * g.table_ld + pages_of(s_len[b]) - s_give[b + 1] + i];   // (it keeps its pages less those that it gives)
     };
     auto page_at = [&](int i) { return i < given ? returned(i) : g.free_pages[count - 1 - (i - given)]; };
     for (int64_t b = first; b <= g.B; b += step) {
         g.q_start[b] = s_new[b];
-        if (b < g.B) g.lens_out[b] = g.lens[b] + g.change[b];
+        if (b < g.B) g.lens_out[b] = s_len[b] + g.change[b];
     }
     for (int64_t t = first; t < g.T; t += step) {
         int pos = 0;
         int64_t slot = -1;
         if (t < tokens) {
-            const int b = sequence_of(s_new, g.B, (int)t), len = g.lens[b], p = len + ((int)t - s_new[b]), j = p >> g.page_shift, had = pages_of(len);
+            const int b = sequence_of(s_new, g.B, (int)t), had_tokens = s_len[b], p = had_tokens + ((int)t - s_new[b]), j = p >> g.page_shift, had = pages_of(had_tokens);
             const int page = j < had ? g.table[b * g.table_ld + j] : page_at(s_take[b] + j - had);
             pos = g.prefix_len + p;
             slot = ((int64_t)page << g.page_shift) + (p & (g.page_size - 1));
@@ -137,7 +152,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs g)
     }
     for (int64_t i = first; i < taken; i += step) {
         const int b = sequence_of(s_take, g.B, (int)i);
-        g.table[b * g.table_ld + pages_of(g.lens[b]) + ((int)i - s_take[b])] = page_at((int)i);
+        g.table[b * g.table_ld + pages_of(s_len[b]) + ((int)i - s_take[b])] = page_at((int)i);
     }
     for (int64_t i = first; i < given - taken; i += step) g.free_pages[count + i] = returned(taken + (int)i);
     if (first == 0) *g.count_out = count + given - taken;
@@ -163,6 +178,7 @@ __global__ __launch_bounds__(kMaskThreads) void mask_kernel(MaskArgs g)
     const int b = blockIdx.x;
     uint32_t st = 0;
     int64_t t0 = g.q_start[b], t1 = g.q_start[b + 1];
+    const int len = g.pos ? g.lens[b] : 0;
     if (t0 < 0 || t1 < t0 || t1 > g.T || t1 - t0 > g.max_q) st |= AWEQ_ST_INDEX;
     t0 = min(max(t0, (int64_t)0), g.T);
     t1 = min(max(t1, t0), min(g.T, t0 + g.max_q));
@@ -173,7 +189,7 @@ __global__ __launch_bounds__(kMaskThreads) void mask_kernel(MaskArgs g)
         s_parent[i] = p;
     }
     __syncthreads();
-    const int base = g.pos ? g.prefix_len + g.lens[b] - m : 0;
+    const int base = g.prefix_len + len - m;
     for (int i = threadIdx.x; i < m; i += kMaskThreads) {
         uint64_t* const row = g.mask + (t0 + i) * g.mask_ld;
         int word = g.words - 1, depth = -1;
@@ -202,21 +218,26 @@ struct KeepArgs {
 };
 
 // A wavefront has a sequence's head in one of the caches.  Place j goes from kept[j] >= j to j, and the places rise: rows that have been written are none that is
-// still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.
+// still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.  A lane has the rows of one place of 64, found with as few
+// reads that wait for one another as there can be: the counts and places, then the pages, then the rows (one path of 5 of 12 tokens and 32 heads 8.7 us -> 6.6).
 template <class V>
 __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
 {
     const int b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x;
     const bool values = blockIdx.z != 0;
-    int64_t t0 = g.q_start[b], t1 = g.q_start[b + 1];
+    const int32_t* const kept = g.kept + b * g.kept_ld;
+    const int64_t last_kept = g.kept_ld - 1;
+    int place = kept[min((int64_t)lane, last_kept)];          // (of place `lane`; past the count anything)
+    const int64_t t0 = g.q_start[b], t1 = g.q_start[b + 1];
     const int len = g.lens[b], n = g.count[b];
     bool ok = t0 >= 0 && t1 >= t0 && t1 <= g.T && len >= t1 - t0 && len <= (g.table_ld << g.page_shift);
     const int m = ok ? (int)(t1 - t0) : 0, base = len - m;
     ok = ok && n >= 0 && n <= m && n <= g.kept_ld;
-    const int32_t* const kept = g.kept + b * g.kept_ld;
     if (ok) {
         bool order = true;
-        for (int j = lane; j < n; j += kWave) order = order && kept[j] > (j ? kept[j - 1] : -1) && kept[j] < m;
+        const int before = __shfl_up(place, 1);
+        if (lane < n) order = place > (lane ? before : -1) && place < m;
+        for (int j = lane + kWave; j < n; j += kWave) order = order && kept[j] > kept[j - 1] && kept[j] < m;
         ok = __builtin_amdgcn_ballot_w64(!order) == 0;
     }
     uint32_t st = ok ? 0u : (uint32_t)AWEQ_ST_INDEX;
@@ -227,35 +248,45 @@ __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
         const int32_t* const table = g.table + b * g.table_ld;
         const int rows = kWave / g.chunks, sub = lane / g.chunks, part = lane % g.chunks;
         const int64_t bytes = (int64_t)g.chunk * g.chunks;
-        auto row_of = [&](int key) -> int64_t {
-            const int page = table[key >> g.page_shift];
-            if ((unsigned)page >= (unsigned)g.pages) { st |= AWEQ_ST_INDEX; return -1; }
-            return (((int64_t)page * g.Hk + head) << g.page_shift) + (key & (g.page_size - 1));
-        };
         constexpr int kAtOnce = 4;
-        for (int j0 = 0; j0 < n; j0 += rows * kAtOnce) {
-            V v[kAtOnce];
-            float s[kAtOnce];
-            int64_t to[kAtOnce];
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const int j = j0 + u * rows + sub;
-                to[u] = -1;
-                if (sub < rows && j < n && kept[j] != j) {
-                    const int64_t source = row_of(base + kept[j]), dest = row_of(base + j);
-                    if (source >= 0 && dest >= 0) {
-                        to[u] = dest;
-                        v[u] = *reinterpret_cast<const V*>(cache + source * bytes + part * g.chunk);
-                        s[u] = step ? step[source] : 0.0f;
-                    }
+        for (int from = 0; from < n; from += kWave) {
+            // rows of place from + lane: where they are, and where they go; -1: they stay
+            const int j = from + lane;
+            if (from) place = kept[min((int64_t)j, last_kept)];
+            int64_t source = -1, dest = -1;
+            if (j < n && place != j) {
+                const int ks = base + place, kd = base + j;
+                const int ps = table[ks >> g.page_shift], pd = table[kd >> g.page_shift];
+                if ((unsigned)ps >= (unsigned)g.pages || (unsigned)pd >= (unsigned)g.pages) {
+                    st |= AWEQ_ST_INDEX;
+                } else {
+                    source = (((int64_t)ps * g.Hk + head) << g.page_shift) + (ks & (g.page_size - 1));
+                    dest = (((int64_t)pd * g.Hk + head) << g.page_shift) + (kd & (g.page_size - 1));
                 }
             }
+            const int here = min(n - from, kWave);
+            for (int j0 = 0; j0 < here; j0 += rows * kAtOnce) {
+                V v[kAtOnce];
+                float s[kAtOnce];
+                int64_t to[kAtOnce];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
-                if (to[u] >= 0) {
-                    *reinterpret_cast<V*>(cache + to[u] * bytes + part * g.chunk) = v[u];
-                    if (step && part == 0) step[to[u]] = s[u];
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int at = j0 + u * rows + sub;
+                    const int64_t row = __shfl(source, at & (kWave - 1));
+                    to[u] = __shfl(dest, at & (kWave - 1));
+                    if (sub >= rows || at >= here) to[u] = -1;
+                    if (to[u] >= 0) {
+                        v[u] = *reinterpret_cast<const V*>(cache + row * bytes + part * g.chunk);
+                        s[u] = step ? step[row] : 0.0f;
+                    }
                 }
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    if (to[u] >= 0) {
+                        *reinterpret_cast<V*>(cache + to[u] * bytes + part * g.chunk) = v[u];
+                        if (step && part == 0) step[to[u]] = s[u];
+                    }
+            }
         }
     }
     raise_status(g.status, st);
@@ -291,12 +322,15 @@ extern "C" int aweq_step_plan(const int32_t* lens, const int32_t* change, int64_
     g.lens_out = lens_out; g.count_out = count_out; g.q_start = q_start; g.pos = pos; g.slot = slot; g.status = status;
     g.table_ld = table_ld; g.T = T; g.B = (int)B; g.page_size = (int)page_size; g.page_shift = __builtin_ctz((unsigned)page_size);
     g.pages = (int)pages; g.table_pages = (int)table_pages; g.prefix_len = (int)prefix_len;
-    const int lds = 3 * ((int)B + 1) * 4;
-    const void* fn = reinterpret_cast<const void*>(drafts::plan_kernel);
+    const int lds = (3 * ((int)B + 1) + (int)B) * 4;
+    const int64_t each = cdiv(B, drafts::kPlanThreads), want = cdiv(T > B ? T : B, drafts::kPlanThreads);
+    const void* fn = each == 1   ? reinterpret_cast<const void*>(drafts::plan_kernel<1>)
+                     : each == 2 ? reinterpret_cast<const void*>(drafts::plan_kernel<2>)
+                                 : reinterpret_cast<const void*>(drafts::plan_kernel<drafts::kPlanMost / drafts::kPlanThreads>);
     int dev = 0, cus = 0;
-    if (lds > 32768 && (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, 3 * (drafts::kPlanMost + 1) * 4) != AWEQ_OK)) return AWEQ_ERR_LAUNCH;
-    const int64_t want = cdiv(T > B ? T : B, drafts::kPlanThreads);
-    drafts::plan_kernel<<<(unsigned)(want < 256 ? want : 256), drafts::kPlanThreads, lds, as_stream(stream)>>>(g);
+    if (lds > 32768 && (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, (4 * drafts::kPlanMost + 3) * 4) != AWEQ_OK)) return AWEQ_ERR_LAUNCH;
+    void* args[] = {&g};
+    if (hipLaunchKernel(fn, dim3((unsigned)(want < 256 ? want : 256)), dim3(drafts::kPlanThreads), args, lds, as_stream(stream)) != hipSuccess) return AWEQ_ERR_LAUNCH;
     return launch_status();
 }
 
