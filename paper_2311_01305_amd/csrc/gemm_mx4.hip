@@ -19,7 +19,7 @@ struct MxPlan {
 static MxPlan plan_mx4(int64_t T, int64_t N, int64_t K)
 {
     const double panels = (double)mx_panels(K), read = 2.2 + (double)N * (double)K * (17.0 / 32.0) / 5.2e6;
-    MxPlan best = {MxPlan::kFew, 1, 1, 1e300};
+    MxPlan best = {MxPlan::kFew, 4, 4, 1e300};
     auto offer = [&](int form, int a, int b, double us) {
         if (us < read) us = read;
         if (us < best.us) best = {static_cast<decltype(best.form)>(form), a, b, us};
@@ -28,9 +28,9 @@ static MxPlan plan_mx4(int64_t T, int64_t N, int64_t K)
     // few tokens: a round of workgroups in us a panel; two or more share a compute unit (one token's, two tokens' tiles)
     struct { int tt, nt; double us; } const few[] = {{1, 2, 0.085}, {1, 1, 0.045}, {2, 1, 0.066}, {2, 2, 0.1}, {4, 2, 0.14}, {4, 4, 0.22}};
     for (const auto& f : few)
-        if (T <= 16 * f.tt * 8) offer(MxPlan::kFew, f.tt, f.nt, 2.2 + panels * f.us * rounds(16 * f.tt, 16 * f.nt));
+        if (T <= 16 * f.tt * 8 && N < (1 << 26)) offer(MxPlan::kFew, f.tt, f.nt, 2.2 + panels * f.us * rounds(16 * f.tt, 16 * f.nt));
     // some hundred: rounds after the first take longer, since nothing of one overlaps with the next
-    if (T > 16 && T <= 2048) {
+    if (T > 16 && T <= 2048 && N < (1 << 23)) {
         offer(MxPlan::kMid, 0, 0, 5.0 + panels * (0.19 + 0.26 * (rounds(64, 128) - 1.0)));
         offer(MxPlan::kMid, 1, 0, 5.0 + panels * (0.33 + 0.42 * (rounds(128, 128) - 1.0)));
     }

@@ -19,7 +19,9 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 
 constexpr int BN = 256;
 
-struct Args : MxArgs, TileWalk {};
+struct Args : MxArgs, TileWalk {
+    int wide;      // rows of a 16-bit output begin at multiples of 16 bytes: eight channels a store (us, against four: 4096 x 4096 x 4096 40.3 -> 38.8)
+};
 
 constexpr int kThreads = 512, kWaves = 8, kWn = 4;   // wavefronts: 2 x 4
 constexpr int NJ = 2;                                // MI x 2 instruction tiles each (MI x 4, with half as many wavefronts, reads a third less of LDS and is slower:
@@ -137,10 +139,10 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
     start_tile(tile_m, tile_n);
     if (pre == kAhead) wait_vm<(kAhead - 1) * kLoads>(); else wait_vm<0>();
 
-    // Vector memory operations of a wave complete in the order issued.  A tile that lies inside the output issues kStores stores per wave after
+    // Vector memory operations of a wave complete in the order issued.  A tile that lies inside the output issues kStores stores per wave or more after
     // requesting the next tile's first panels, so "at most kStores operations pending" means those panels have landed while the stores may
     // still be on their way (relaxed: set for the tile that follows).
-    constexpr int kStores = 8 * MI;
+    constexpr int kStores = OUT == kMxF32 ? 8 * MI : 4 * MI;
     bool relaxed = false;
 
     for (;;) {
@@ -366,6 +368,19 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
                             e4{(E)a[4 * q], (E)a[4 * q + 1], (E)a[4 * q + 2], (E)a[4 * q + 3]};
                     }
                 wave_lds_fence();
+                if (g.wide && inside) {
+                    const int r0 = lane_ >> 3, c = (lane_ & 7) * 2;
+                    E* const row = reinterpret_cast<E*>(g.out) + (wave_t + 32 * i + r0) * g.ldo + wave_n + c * 4;
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        const int r = 8 * p + r0;
+                        union { e4 h[2]; v4i v; } u;
+                        u.h[0] = *reinterpret_cast<const e4*>(slab + r * 128 + (c ^ (r & 15)) * 8);
+                        u.h[1] = *reinterpret_cast<const e4*>(slab + r * 128 + ((c + 1) ^ (r & 15)) * 8);
+                        *reinterpret_cast<v4i*>(row + (int64_t)(8 * p) * g.ldo) = u.v;
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int p = 0; p < 8; ++p) {
                     const int r = 4 * p + rd_r;
@@ -412,6 +427,7 @@ int launch_mx4_tiled(const MxArgs& m, int mi, hipStream_t st)
 {
     mxtiled::Args g = {};
     static_cast<MxArgs&>(g) = m;
+    g.wide = g.ldo % 8 == 0;     // (out is 16-byte aligned)
     int64_t blocks = 0;
     const int rc = plan_walk(g, g.T, g.N, g.K / 2, 64 * mi, blocks);
     if (rc != AWEQ_OK) return rc;

@@ -157,7 +157,7 @@ def test_what_is_not_finite(B, dt, bad):
 
 
 # ---- the product
-def product(B, T, N, K, dt, fold, bias, out_dt, seed=1, given=False, ld_extra=0, change=None):
+def product(B, T, N, K, dt, fold, bias, out_dt, seed=1, given=False, ld_extra=0, change=None, ldo_extra=8):
     g = torch.Generator(device=DEV)
     g.manual_seed(seed)
     X = torch.randn(T, K + ld_extra, generator=g, device=DEV)
@@ -174,7 +174,7 @@ def product(B, T, N, K, dt, fold, bias, out_dt, seed=1, given=False, ld_extra=0,
     if not given:
         first = (xq, x_scale)
         xq, x_scale = torch.full_like(xq, 0xEE), torch.full_like(x_scale, 0xEE)
-    ldo = N + 8
+    ldo = N + ldo_extra
     out = torch.full((T, ldo), 5.0, dtype=TYPES[out_dt], device=DEV)
     B.aweq_mx4_gemm_tokens(None if given else X, dt_of(B, dt), T, K, K + ld_extra, factor, xq, x_scale, wq, w_scale, N, b, out, dt_of(B, out_dt), ldo, status)
     assert (out[:, N:] == 5.0).all()
@@ -216,6 +216,16 @@ def test_product(B, T, N, K, dt, out_dt):
     got = product(B, T, N, K, dt, fold, bias, out_dt, seed=T + K, ld_extra=8 * (T % 2))
     assert got[4] == 0
     check(*got[:4], out_dt)
+
+
+@pytest.mark.parametrize("T,N,K", [(2, 64, 96), (40, 260, 544), (300, 1024, 640), (1500, 1028, 1312)])
+@pytest.mark.parametrize("out_dt", ["f16", "f32"])
+def test_rows_of_the_output_that_begin_anywhere(B, T, N, K, out_dt):
+    """Pitches that are no multiple of 16 bytes' worth, and none at all."""
+    for extra in (0, 4, 12):
+        got = product(B, T, N, K, "bf16", False, True, out_dt, ldo_extra=extra)
+        assert got[4] == 0
+        check(*got[:4], out_dt)
 
 
 @pytest.mark.parametrize("T,N,K", [(1, 100, 544), (9, 260, 2048), (150, 516, 1056), (600, 2100, 640)])
