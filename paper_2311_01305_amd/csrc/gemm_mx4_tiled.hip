@@ -58,6 +58,13 @@ __device__ __forceinline__ void wait_vm()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// The same unless skip is not 0: a branch that the compiler does not see, since it would move products of the loop past one of its own
+template <int N>
+__device__ __forceinline__ void wait_vm_unless(uint32_t skip)
+{
+    asm volatile("s_cmp_lg_u32 %1, 0\n\ts_cbranch_scc1 1f\n\ts_waitcnt vmcnt(%0)\n1:" ::"n"(N), "s"(skip) : "memory", "scc");
+}
+
 #define SB() __builtin_amdgcn_sched_barrier(0)
 #define MF(A_, B_, S, i, j)                                                                                                                    \
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(B_[j]), mx_operand(A_[i]), acc[i][j], 4, 4, J, sb[j][S], J, sa[i][S])
@@ -288,11 +295,14 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
         // Four panels at a time while all of them have one to request.  In flight when panel h + 1 has to be complete: kAhead - 1 panels, and scales where
         // one of them begins a group.  relaxed: the panels requested before the stores landed together with panel 0: nothing to wait for, and a count would
         // wait for the stores.
+        uint32_t landed = relaxed ? 1u : 0u;      // (in the first four)
         auto steady = [&](auto j_c) {
             constexpr int J = decltype(j_c)::value;
             constexpr bool scales = (J + 2) % 4 == 0 || (J + 3) % 4 == 0 || (kAhead > 3 && (J + 4) % 4 == 0);
             half(j_c, integral_constant<int, J == 3 ? 1 : 0>{}, true_type{}, true_type{}, integral_constant<int, (J + kAhead) % 4 == 0 ? 1 : 0>{}, [&]() {
-                if (J >= kAhead - 1 || !relaxed || h >= 4) wait_vm<(kAhead - 1) * kLoads + (scales ? TL::kLoadsS : 0)>();
+                constexpr int left = (kAhead - 1) * kLoads + (scales ? TL::kLoadsS : 0);
+                if constexpr (J >= kAhead - 1) wait_vm<left>();
+                else wait_vm_unless<left>(landed);
             });
         };
         while (h + kAhead + 3 < nh) {
@@ -300,6 +310,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_tiled(Args g)
             steady(integral_constant<int, 1>{});
             steady(integral_constant<int, 2>{});
             steady(integral_constant<int, 3>{});
+            landed = 0;
         }
         // The rest, at most kAhead + 3: the scales of the panel in the lowest byte
         const integral_constant<int, 0> low;
