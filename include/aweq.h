@@ -475,8 +475,8 @@ int aweq_mx4_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, int64_t K, i
  *   lens_out[b] = lens + change, *count_out: pages on the stack;  q_start[B + 1]: the new tokens of each sequence, one sequence after the other;
  *   pos[t] = prefix_len + place in its sequence, slot[t] = where the token goes (aweq_kv_append), T of each; past q_start[B]: 0 and -1.
  * Where the pages do not suffice nothing is changed (lens_out = lens, *count_out = *free_count, q_start all 0, pos 0, slot -1) and AWEQ_ST_PAGES is raised; the same,
- * with AWEQ_ST_INDEX, for a length below 0, more taken away than there is, more tokens than T, a sequence longer than table_pages pages, or a count
- * outside [0, pages].  lens_out must not be lens, nor count_out free_count (AWEQ_ERR_ALIGN for an output that overlaps an input): a step has the next one's inputs
+ * with AWEQ_ST_INDEX, for a length below 0, more taken away than there is, more tokens than T, a sequence longer than table_pages pages, a count
+ * outside [0, pages], or more pages free and given back than there are.  lens_out must not be lens, nor count_out free_count (AWEQ_ERR_ALIGN for an output that overlaps an input): a step has the next one's inputs
  * beside its own.  B <= 8192, T <= 2^24,
  * pages < 2^31, table_pages <= 2^24, prefix_len <= 2^29, table_pages * page_size <= 2^29. */
 int aweq_step_plan(const int32_t* lens, const int32_t* change, int64_t B, int64_t page_size, int64_t pages, int32_t* table, int64_t table_ld,
@@ -488,7 +488,7 @@ int aweq_step_plan(const int32_t* lens, const int32_t* change, int64_t B, int64_
  * AWEQ_ST_INDEX).  mask[t] (words of 64 bits, pitch mask_ld words >= ceil(max_q / 64)): bit j says that t is new token j or goes on from it, however
  * far; bits of all ceil(max_q / 64) words are written.  pos[t] (nullable, with lens) = prefix_len + lens[b] - m + depth, m its sequence's new tokens, depth how
  * many of them come before t on its path.  max_q (HOST): no sequence has more; <= 4096.  Rows past q_start[B] are left as they are.  q_start out of
- * order, past T, or with more than max_q rows: AWEQ_ST_INDEX and clamped.  B <= 2^20, T <= 2^24. */
+ * order, past T, or with more than max_q rows: AWEQ_ST_INDEX and clamped.  mask or pos over an input: AWEQ_ERR_ALIGN.  B <= 2^20, T <= 2^24. */
 int aweq_tree_mask(const int32_t* parent, int64_t T, const int32_t* q_start, int64_t B, int64_t max_q, const int32_t* lens, int64_t prefix_len,
                    uint64_t* mask, int64_t mask_ld, int32_t* pos, uint32_t* status, void* stream);
 
@@ -508,7 +508,7 @@ int aweq_tree_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int
  * aweq_step_plan takes to drop the rest.  The tokens behind the kept ones are unspecified afterwards.  A count outside [0, min(m, kept_ld)], places out of
  * order or outside [0, m), lens[b] < m, or pages outside [0, pages): AWEQ_ST_INDEX, and nothing of that sequence is moved (change 0; a page outside: the
  * rows on it alone); so for a sequence longer than table_ld pages.  No two sequences may have a page of new tokens in common.  Caches as in aweq_kv_append;
- * T, q_start, lens, table: the step's.  B <= 2^20, Hk <= 2^16, T <= 2^24. */
+ * T, q_start, lens, table: the step's.  change over an input: AWEQ_ERR_ALIGN.  B <= 2^20, Hk < 2^16, B * Hk <= 2^24, T <= 2^24. */
 int aweq_kv_keep(void* k_cache, void* v_cache, float* k_step, float* v_step, aweq_dtype cache_dt, int64_t pages, int64_t page_size, int64_t Hk, int64_t D,
                  const int32_t* table, int64_t table_ld, const int32_t* lens, const int32_t* q_start, int64_t B, int64_t T,
                  const int32_t* kept, int64_t kept_ld, const int32_t* count, int32_t* change, uint32_t* status, void* stream);

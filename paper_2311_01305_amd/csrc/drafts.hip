@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs g)
         }
     }
     uint32_t st = s_bad;
-    if (total[0] > g.T || count - total[1] + total[2] > g.pages) st |= AWEQ_ST_INDEX;
+    if (total[0] > g.T || count + total[2] > g.pages) st |= AWEQ_ST_INDEX;
     if (total[1] > count + total[2]) st |= AWEQ_ST_PAGES;
     if (st & AWEQ_ST_INDEX) st = AWEQ_ST_INDEX;
     const int64_t first = (int64_t)blockIdx.x * kPlanThreads + tid, step = (int64_t)gridDim.x * kPlanThreads;
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs g)
         if (first == 0) *g.count_out = count;
         return;
     }
-    // (the totals fit: tokens T, pages those of the tables' rows, which are at most 2^24 each; where they do not fit 32 bits the stack does not suffice)
+    // (the totals fit 32 bits: tokens are no more than T, pages given back, and with the stack those taken, no more than there are)
 #pragma unroll
     for (int k = 0; k < EACH; ++k)
         if (k < mine) {
@@ -219,7 +219,7 @@ struct KeepArgs {
 
 // A wavefront has a sequence's head in one of the caches.  Place j goes from kept[j] >= j to j, and the places rise: rows that have been written are none that is
 // still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.  A lane has the rows of one place of 64, found with as few
-// reads that wait for one another as there can be: the counts and places, then the pages, then the rows (one path of 5 of 12 tokens and 32 heads 8.7 us -> 6.6).
+// reads that wait for one another as there can be: the counts and places, then the pages, then the rows (one path of 5 of 12 tokens and 32 heads 8.7 us -> 8.1).
 template <class V>
 __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
 {
@@ -280,6 +280,7 @@ __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
                         s[u] = step ? step[row] : 0.0f;
                     }
                 }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // (a row read by one lane may be another's to write)
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u)
                     if (to[u] >= 0) {
@@ -341,6 +342,8 @@ extern "C" int aweq_tree_mask(const int32_t* parent, int64_t T, const int32_t* q
     if (T <= 0 || T > (1 << 24) || B <= 0 || B > (1 << 20) || max_q <= 0 || max_q > drafts::kMaskMost || prefix_len < 0 || prefix_len > (1 << 29) || mask_ld < cdiv(max_q, 64))
         return AWEQ_ERR_SHAPE;
     if (!drafts::aligned(parent, 4) || !drafts::aligned(q_start, 4) || !drafts::aligned(lens, 4) || !drafts::aligned(mask, 8) || !drafts::aligned(pos, 4)) return AWEQ_ERR_ALIGN;
+    if (overlap({matrix_span(mask, T, cdiv(max_q, 64), mask_ld, 8), {pos, T * 4}}, {{parent, T * 4}, {q_start, (B + 1) * 4}, {pos ? lens : nullptr, B * 4}}))
+        return AWEQ_ERR_ALIGN;
     const drafts::MaskArgs g = {parent, q_start, lens, mask, pos, status, T, mask_ld, (int)max_q, (int)cdiv(max_q, 64), (int)prefix_len};
     drafts::mask_kernel<<<(unsigned)B, drafts::kMaskThreads, (size_t)max_q * 4, as_stream(stream)>>>(g);
     return launch_status();
@@ -360,6 +363,9 @@ extern "C" int aweq_kv_keep(void* k_cache, void* v_cache, float* k_step, float* 
     if (!aligned16(k_cache) || !aligned16(v_cache) || (codes && (!aligned16(k_step) || !aligned16(v_step)))) return AWEQ_ERR_ALIGN;
     for (const void* p : {(const void*)table, (const void*)lens, (const void*)q_start, (const void*)kept, (const void*)count, (const void*)change})
         if (!drafts::aligned(p, 4)) return AWEQ_ERR_ALIGN;
+    // (a workgroup would read what another one has written)
+    if (overlap({{change, B * 4}}, {{lens, B * 4}, {count, B * 4}, {q_start, (B + 1) * 4}, matrix_span(kept, B, kept_ld < T ? kept_ld : T, kept_ld, 4), matrix_span(table, B, 1, table_ld, 4)}))
+        return AWEQ_ERR_ALIGN;
     drafts::KeepArgs g = {};
     g.k_cache = reinterpret_cast<char*>(k_cache); g.v_cache = reinterpret_cast<char*>(v_cache);
     g.k_step = codes ? k_step : nullptr; g.v_step = codes ? v_step : nullptr;

@@ -81,6 +81,9 @@ def test_tree_mask(B):
         assert bad(**{name: None}) == "AWEQ_ERR_NULL"
     assert bad(T=0) == bad(T=2 ** 24 + 1) == bad(B=0) == bad(B=2 ** 20 + 1) == bad(max_q=0) == bad(max_q=4097, mask_ld=80) == bad(mask_ld=1) == bad(prefix_len=-1) == "AWEQ_ERR_SHAPE"
     assert bad(parent=P + 1) == bad(mask=P + 4) == bad(pos=P + 2) == bad(lens=P + 2) == "AWEQ_ERR_ALIGN"
+    apart = dict(parent=P + 0x1000, q_start=P + 0x2000, lens=P + 0x3000, mask=P + 0x4000, pos=P + 0x5000)
+    for name in ("parent", "q_start", "lens"):
+        assert bad(**{**apart, "pos": apart[name] + 4}) == bad(**{**apart, "mask": apart[name] - 8}) == "AWEQ_ERR_ALIGN"
 
 
 def test_tree_attention(B):
@@ -110,3 +113,6 @@ def test_kv_keep(B):
     assert bad(pages=0) == bad(page_size=8) == bad(Hk=0) == bad(Hk=65536) == bad(D=0) == bad(D=264) == bad(D=60) == bad(B=0) == bad(T=0) == bad(table_ld=0) == bad(kept_ld=0) == "AWEQ_ERR_SHAPE"
     assert bad(B=2 ** 20, Hk=64) == "AWEQ_ERR_SHAPE"
     assert bad(k_cache=P + 8) == bad(table=P + 2) == bad(change=P + 1) == bad(cache_dt=B.AWEQ_I8, k_step=P + 4, v_step=P) == "AWEQ_ERR_ALIGN"
+    apart = dict(table=P + 0x1000, lens=P + 0x2000, q_start=P + 0x3000, kept=P + 0x4000, count=P + 0x5000)
+    for at in apart.values():
+        assert bad(**apart, change=at + 4) == "AWEQ_ERR_ALIGN"

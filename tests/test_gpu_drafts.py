@@ -134,6 +134,10 @@ def test_plans_that_are_refused_change_nothing(B):
     assert s.unchanged(B) == B.ST_INDEX
     s.count = -1
     assert s.unchanged(B) == B.ST_INDEX
+    s = Step([128, 0], [-128, 128], width=8)
+    s.pages = 4                    # a sequence that says it has more pages than there are
+    s.count = 0
+    assert s.unchanged(B) == B.ST_INDEX
 
 
 # ---- masks
