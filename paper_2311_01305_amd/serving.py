@@ -96,6 +96,17 @@ class Mx4Linear:
         t = buf.t
         return cls.from_weight(t["W_hat"], bias, t["inv_s"] if fold else None, t["status"])
 
+    @classmethod
+    def from_group(cls, gb: pipeline.GroupBuffers, fold: bool = True, biases: Optional[Sequence] = None):
+        """The layers of pipeline.calibrate_group side by side as one; biases: of each, or None."""
+        biases = [None] * len(gb.Ns) if biases is None else list(biases)
+        if len(biases) != len(gb.Ns):
+            raise ValueError("a bias, or None, for each layer")
+        bias = None
+        if any(b is not None for b in biases):
+            bias = torch.cat([torch.zeros_like(p["step_w"]) if b is None else b for p, b in zip(gb.per, biases)])
+        return cls.from_weight(torch.cat([p["W_hat"] for p in gb.per]), bias, gb.t["inv_s"] if fold else None, gb.t["status"])
+
 
 def _bias(t, layer, N, K, group, bias):
     """A bias less the mean output of what its layer's codes are off the folded weight by."""

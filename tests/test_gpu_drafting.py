@@ -151,3 +151,36 @@ def test_command(S, capsys, prefix, more):
     S.main(["--hidden", "256", "--heads", "2", "--key-heads", "1", "--prefix", str(prefix), "--batch", "3", "--steps", "4"] + more)
     out = capsys.readouterr().out
     assert f"behind {prefix} shared tokens" in out and "status 0" in out
+
+
+@pytest.mark.parametrize("which", ["none", "some", "all"])
+def test_layers_of_a_group_as_one(S, which):
+    """Each layer's weight as by itself, its bias or zeros, and the whole in a block."""
+    from paper_2311_01305_amd import pipeline
+    B = S.B
+    torch.manual_seed(12)
+    T, K, Ns = 200, 288, (256, 128, 128)
+    x = torch.randn(T, K, device=DEV).half()
+    ws = [torch.randn(N, K, device=DEV).half() for N in Ns]
+    biases = [torch.randn(N, device=DEV) if which == "all" or (which == "some" and i == 1) else None for i, N in enumerate(Ns)]
+    gb = pipeline.GroupBuffers(T, K, Ns, torch.float16, device=DEV)
+    pipeline.calibrate_group(x, ws, biases, gb)
+    whole = S.Mx4Linear.from_group(gb, biases=biases)
+
+    def weight(layer):
+        out = torch.empty(layer.N, K, device=DEV)
+        B.aweq_mx4_values(layer.codes, layer.scales, layer.N, K, out, B.AWEQ_F32, K)
+        return out
+    assert torch.equal(weight(whole), torch.cat([weight(S.Mx4Linear.from_weight(p["W_hat"])) for p in gb.per]))
+    assert whole.factor is gb.t["inv_s"] and (whole.N, whole.K) == (512, K)
+    if which == "none":
+        assert whole.bias is None
+    else:
+        assert torch.equal(whole.bias, torch.cat([torch.zeros(N, device=DEV) if b is None else b for N, b in zip(Ns, biases)]))
+    with pytest.raises(ValueError):
+        S.Mx4Linear.from_group(gb, biases=biases[:2])
+    cache = S.PagedCache(4, 16, HK, D, device=DEV)
+    block = S.AttentionBlock(whole, S.calibrated(K, HQ * D, 2, mx4=True), HQ, cache, S.frequencies(D, device=DEV), D, 8, device=DEV)
+    pages = cache.take(3)
+    y = block(x[:3], ints([0, 1, 2]), ints(cache.slots(pages, 0, 3), torch.int64), ints([3]), ints([pages]), ints([0, 3]), 3, 3)
+    assert y.shape == (3, K) and bool(torch.isfinite(y).all()) and int(block.status.item()) == 0
