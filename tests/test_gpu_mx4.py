@@ -71,7 +71,7 @@ def quantised(B, X, dt, factor=None, ldx=None):
 
 
 def same_codes(got, want, scales):
-    """Equal, but for the sign of a zero of a block without a scale."""
+    """To the bit, the signs of zeros among them."""
     assert np.array_equal(got, want), np.argwhere(got != want)[:5]
 
 
@@ -205,7 +205,9 @@ def check(out, x, w, b, out_dt):
 
 SIZES = [(1, 4, 32), (1, 64, 4096), (2, 100, 544), (3, 20, 96), (4, 2052, 1056), (5, 36, 2080), (16, 64, 512), (17, 48, 1024), (31, 132, 640), (33, 260, 1536),
          (64, 128, 4608), (65, 516, 128), (100, 1028, 2016), (129, 260, 384), (200, 300, 5152), (257, 516, 1120), (300, 260, 160), (511, 8196, 256), (700, 2100, 1088),
-         (130, 1300, 9056), (260, 512, 4160), (1000, 1036, 1440), (2300, 260, 800), (4200, 4100, 1312), (6000, 2052, 928), (900, 9000, 992)]
+         (130, 1300, 9056), (260, 512, 4160), (1000, 1036, 1440), (2300, 260, 800), (4200, 4100, 1312), (6000, 2052, 928), (900, 9000, 992),
+         (1, 64, 32768), (4, 64, 8192), (2, 36, 33024), (70, 132, 33024), (3, 8, 64),
+         (3, 6000, 544), (520, 6004, 544), (777, 4100, 1056), (1500, 2052, 1440), (777, 16388, 544)]
 
 
 @pytest.mark.parametrize("T,N,K", SIZES)
@@ -246,6 +248,27 @@ def test_tokens_that_are_not_finite(B, T):
     rest = torch.arange(T) != T // 2
     if rest.any():
         check(out[rest], x[rest], w, b, "f32")
+
+
+@pytest.mark.parametrize("T", [1, 20, 200, 700])
+def test_weights_that_are_not_finite(B, T):
+    """Their channel's outputs are NaN, and no other's."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    N, K = 516, 1120
+    W = torch.randn(N, K, generator=g, device=DEV)
+    W[77, 1100], W[300, 3] = float("nan"), -float("inf")
+    wq, w_scale, status = quantised(B, W, "f32")
+    X = torch.randn(T, K, generator=g, device=DEV)
+    xq, x_scale, _ = quantised(B, X, "f32")
+    out = torch.empty(T, N, device=DEV)
+    B.aweq_mx4_gemm_tokens(None, B.AWEQ_F32, T, K, K, None, xq, x_scale, wq, w_scale, N, None, out, B.AWEQ_F32, N)
+    bad = torch.zeros(N, dtype=torch.bool)
+    bad[77] = bad[300] = True
+    assert status == B.ST_NONFINITE and torch.isnan(out[:, bad.to(DEV)]).all()
+    x = torch.from_numpy(values(*unpacked(xq.cpu().numpy(), x_scale.cpu().numpy(), T, K)))
+    w = torch.from_numpy(values(*unpacked(wq.cpu().numpy(), w_scale.cpu().numpy(), N, K)))
+    check(out.double().cpu()[:, ~bad], x, w[~bad], None, "f32")
 
 
 def test_large_and_small_scales(B):
