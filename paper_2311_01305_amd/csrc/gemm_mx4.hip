@@ -67,7 +67,7 @@ extern "C" int aweq_mx4_gemm_tokens(const void* X, aweq_dtype x_dt, int64_t T, i
     g.out_kind = out_dt == AWEQ_F16 ? kMxF16 : out_dt == AWEQ_BF16 ? kMxBf16 : kMxF32;
     hipStream_t st = as_stream(stream);
     const MxPlan p = plan_mx4(T, N, K);
-    if (X && p.form == MxPlan::kFew && p.a == 1 && T <= kMxQuantTokens && T * mx_panels(K) * 64 <= kMxQuantBytes)
+    if (X && p.form == MxPlan::kFew && p.a == 1 && mx4_few_quantises(T, N, K, p.b))
         return launch_mx4_few_quant(g, MxIn{X, ldx, factor, xq, x_scale}, x_dt, p.b, st);
     if (X) {
         const int rc = launch_quant_mx4(X, x_dt, T, K, ldx, factor, xq, x_scale, status, st);

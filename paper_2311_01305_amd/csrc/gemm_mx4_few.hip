@@ -4,6 +4,9 @@
 // order.  Both operands come straight from their panels (16 rows of one are 1 KiB contiguous) in the operand order of v_mfma_scale_f32_16x16x128_f8f6f4: lane l
 // holds row l % 16, the 32 values of block l / 16 of the panel.  The scales of that block in four panels are one register, of which each instruction names
 // the byte; so a wavefront takes the panels in groups of four.
+//
+// Bound by the launch and a round trip or two for small weights, by HBM for large ones (us, weights that are in no cache, tokens quantised by the launch: one
+// token 4096 x 4096 4.7, 11008 x 4096 7.8, 22016 x 8192 21.5; codes given 4.5, 7.3, 20.5: 96 MB at 4.7 TB/s).
 #include "gemm_mx4.hpp"
 
 #include <type_traits>
@@ -23,8 +26,8 @@ __device__ __forceinline__ f32x4 mul(const v4i& w, const v4i& x, const f32x4& c,
 }
 
 // E: void: the tokens' codes are in memory.  Otherwise every workgroup quantises the few tokens, of that type, for itself while its first weights are on their way, the
-// first one also for the caller.
-template <int TT, int NT, class E>
+// first one also for the caller; ROUNDS: units of eight values of a thread, at most.
+template <int TT, int NT, class E, int ROUNDS>
 __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int first_tile)
 {
     constexpr bool QX = !std::is_same<E, void>::value;
@@ -77,13 +80,12 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int 
     };
     // (QX) the tokens ahead of the weights: loads return in order
     using U = typename std::conditional<QX, E, float>::type;
-    constexpr int kRounds = QX ? 2 * (int)kMxQuantBytes / (8 * kThreads) : 1;   // units of 8 values a thread
-    Unit<U> raw[QX ? kRounds : 1];
-    float factor[QX ? kRounds : 1][8];
+    Unit<U> raw[QX ? ROUNDS : 1];
+    float factor[QX ? ROUNDS : 1][8];
     const int units = (int)(g.K / 8), padded = np * 16;                            // of a token
     if constexpr (QX) {
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
+        for (int i = 0; i < ROUNDS; ++i) {
             const int at = i * kThreads + (int)threadIdx.x;
             if (i * kThreads >= padded * (int)g.T) break;
             const int t = min(at / padded, (int)g.T - 1), u = min(at % padded, units - 1);   // (past the end: not kept)
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int 
     if constexpr (QX) {
         uint32_t st = 0;
 #pragma unroll
-        for (int i = 0; i < kRounds; ++i) {
+        for (int i = 0; i < ROUNDS; ++i) {
             const int at = i * kThreads + (int)threadIdx.x;
             if (i * kThreads >= padded * (int)g.T) break;
             const int t = at / padded, u = at % padded, p = u / 16, b = u / 4 % 4;
@@ -192,14 +194,14 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int 
 }
 
 // Token tiles ride on the grid's y dimension: at most 65535 of them to a launch, and fewer than 2^32 threads
-template <int TT, int NT, class E = void>
+template <int TT, int NT, class E = void, int ROUNDS = 0>
 static int launch_tile(MxArgs g, hipStream_t st, MxIn in = {})
 {
     constexpr bool QX = !std::is_same<E, void>::value;
     constexpr int kSums = kWaves * TT * NT * kWave * 16;
     static_assert(!QX || TT == 1, "one row of tokens");
     const int lds = kSums + (QX ? (int)(g.T * (mx_panels(g.K) * 64 + mx_groups(g.K) * 16)) : 0);
-    const void* fn = reinterpret_cast<const void*>(gemm_mx4_few<TT, NT, E>);
+    const void* fn = reinterpret_cast<const void*>(gemm_mx4_few<TT, NT, E, ROUNDS>);
     int dev = 0, cus = 0;
     if (lds > 32768 && (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, lds > 65536 ? 131072 : 65536) != AWEQ_OK)) return AWEQ_ERR_LAUNCH;
     const int64_t tiles = cdiv(g.T, 16 * TT), blocks = cdiv(g.N, 16 * NT), by_threads = ((1ll << 32) - 1) / (blocks * kThreads);
@@ -213,6 +215,27 @@ static int launch_tile(MxArgs g, hipStream_t st, MxIn in = {})
     }
     return launch_status();
 }
+
+// Units of eight values that a workgroup quantises, and how many of them a thread has at most: all are asked for ahead of the first weights, so that a thread keeps
+// them in registers (us, 8 of them for every call -> as many as there are: one token 11008 x 4096 10.9 -> 7.8, 22016 x 8192 24.6 -> 21.5)
+static int64_t units_of(int64_t T, int64_t K) { return T * mx_panels(K) * 16; }
+constexpr int kMostRounds = 4;
+
+template <int NT, class E>
+static int launch_rounds(const MxArgs& g, const MxIn& in, hipStream_t st)
+{
+    const int64_t units = units_of(g.T, g.K);
+    if (units <= kThreads) return launch_tile<1, NT, E, 1>(g, st, in);
+    if (units <= 2 * kThreads) return launch_tile<1, NT, E, 2>(g, st, in);
+    return launch_tile<1, NT, E, kMostRounds>(g, st, in);
+}
+
+template <class E>
+static int launch_quant(const MxArgs& g, const MxIn& in, int nt, hipStream_t st)
+{
+    return nt == 2 ? launch_rounds<2, E>(g, in, st) : launch_rounds<1, E>(g, in, st);
+}
+
 }  // namespace mxfew
 
 int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st)
@@ -222,11 +245,20 @@ int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st)
     return nt == 2 ? mxfew::launch_tile<4, 2>(g, st) : mxfew::launch_tile<4, 4>(g, st);
 }
 
+// Every workgroup repeats the work.  That is less than a launch of the quantizer's own (3 us) up to two units a thread, or up to four where each compute unit has a
+// workgroup (us, in the launch / before it: 4096 x 4096 one token 4.7 / 7.7, four tokens 6.5 / 7.9; 11008 x 4096 two 8.9 / 10.7, four 11.8 / 10.6;
+// 8192 x 8192 two 10.9 / 12.1)
+bool mx4_few_quantises(int64_t T, int64_t N, int64_t K, int nt)
+{
+    const int64_t units = mxfew::units_of(T, K);
+    return T <= 16 && (units <= 2 * mxfew::kThreads || (units <= mxfew::kMostRounds * mxfew::kThreads && cdiv(N, 16 * nt) <= 256));
+}
+
 int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, int nt, hipStream_t st)
 {
-    if (dt == AWEQ_F16) return nt == 2 ? mxfew::launch_tile<1, 2, _Float16>(g, st, in) : mxfew::launch_tile<1, 1, _Float16>(g, st, in);
-    if (dt == AWEQ_BF16) return nt == 2 ? mxfew::launch_tile<1, 2, __bf16>(g, st, in) : mxfew::launch_tile<1, 1, __bf16>(g, st, in);
-    return nt == 2 ? mxfew::launch_tile<1, 2, float>(g, st, in) : mxfew::launch_tile<1, 1, float>(g, st, in);
+    if (dt == AWEQ_F16) return mxfew::launch_quant<_Float16>(g, in, nt, st);
+    if (dt == AWEQ_BF16) return mxfew::launch_quant<__bf16>(g, in, nt, st);
+    return mxfew::launch_quant<float>(g, in, nt, st);
 }
 
 }  // namespace aweq

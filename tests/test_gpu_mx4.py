@@ -207,7 +207,8 @@ SIZES = [(1, 4, 32), (1, 64, 4096), (2, 100, 544), (3, 20, 96), (4, 2052, 1056),
          (64, 128, 4608), (65, 516, 128), (100, 1028, 2016), (129, 260, 384), (200, 300, 5152), (257, 516, 1120), (300, 260, 160), (511, 8196, 256), (700, 2100, 1088),
          (130, 1300, 9056), (260, 512, 4160), (1000, 1036, 1440), (2300, 260, 800), (4200, 4100, 1312), (6000, 2052, 928), (900, 9000, 992),
          (1, 64, 32768), (4, 64, 8192), (2, 36, 33024), (70, 132, 33024), (3, 8, 64),
-         (3, 6000, 544), (520, 6004, 544), (777, 4100, 1056), (1500, 2052, 1440), (777, 16388, 544)]
+         (3, 6000, 544), (520, 6004, 544), (777, 4100, 1056), (1500, 2052, 1440), (777, 16388, 544),
+         (16, 36, 1024), (13, 132, 544), (2, 68, 8192), (16, 5004, 512), (9, 12000, 288)]
 
 
 @pytest.mark.parametrize("T,N,K", SIZES)
