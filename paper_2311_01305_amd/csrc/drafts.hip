@@ -9,6 +9,7 @@ namespace drafts {
 // Every workgroup reads all lengths and adds them up for itself (three running sums: new tokens, pages taken, pages given back), so that one launch does it; then the
 // threads of all of them share tokens, pages and sequences.  Nothing that is read is written: pages taken go behind a sequence's own in its row, pages
 // given back are read from the end of theirs, the stack is read below its top and written above.
+// (us, a launch being 2.2: 7 sequences of a token each 4.3, 600 with 19544 new tokens, of which 112 give back, 7.7: lengths, running sums, pages)
 constexpr int kPlanThreads = 512, kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanMost = 8192;     // sequences
 
@@ -171,7 +172,8 @@ struct MaskArgs {
     int max_q, words, prefix_len;
 };
 
-// A workgroup has a sequence, a thread a token and its path: the places on it fall, so that a word of the mask is complete when the next one begins
+// A workgroup has a sequence, a thread a token and its path: the places on it fall, so that a word of the mask is complete when the next one begins (a tree of 12
+// tokens 2.5 us, five of up to 211 5.4: the longest path, a read of LDS after the other)
 __global__ __launch_bounds__(kMaskThreads) void mask_kernel(MaskArgs g)
 {
     extern __shared__ int s_parent[];

@@ -4,12 +4,12 @@
 namespace aweq {
 
 // What each form is modelled to take (us), from its time with a workgroup on few and on all of the 256 compute units; all are near a constant and a share of the
-// panels.  No form is below the read of the weight.  us, codes given, bfloat16 output, weights that change from call to call:
-//   tokens          1     16    32    64     128    256    512    1024   2048   4096
-//   4096 x 4096     3.1   3.5   4.1   5.1    6.7    9.5   11.5    15.2   23.5   38.9
-//   11008 x 4096    6.6   7.1   8.2   9.5   11.2   13.1   18.6    29.8   51.9    102
-//   8192 x 8192     7.7   7.9   8.7  10.2   15.4   18.6   25.1    38.3   64.0    126
-//   22016 x 8192   17.4  18.6  20    21.4   28.4   36.7   60       108    190    353      (90 MB of codes: 5.4 TB/s at one token)
+// panels.  No form is below the read of the weight.  us, codes given, bfloat16 output, weights that are in no cache:
+//   tokens          1     16    32    64     128    256    333    512    1024   2048   4096
+//   4096 x 4096     4.5   4.7   5.2   6.1    7.3   10.4   11.7   12.6    16.8   23.2   35.9
+//   11008 x 4096    7.2   7.9   9.7  11.3   13.2   16.9   19.1   19.8    28.8   53.1   94.9
+//   8192 x 8192     8.8   8.9  10.2  12.3   19.5   21.1   26.5   28.1    38.3   61.0   117
+//   22016 x 8192   20.7  21.4  21.5  23.6   32.2   36.1   44.1   49.1    107    177    337      (96 MB: 4.6 TB/s at one token; 4.4 PFLOP/s at 4096)
 struct MxPlan {
     enum { kFew, kMid, kTiled } form;
     int a, b;          // few: tt, nt; mid: square; tiled: mi

@@ -3,6 +3,8 @@
 // HBM-bound: 2 bytes in and 17/32 out a value (16-bit types), and about five vector operations.  A block's 32 values are four lanes' units of eight; 16 lanes
 // have a row's panel and a wavefront four rows of it, four panels one after the other, so that the four scales that a lane's block has in them are the four bytes
 // which belong together, and the codes of four rows are 256 bytes in one piece.
+// Measured, bfloat16: 22016 x 8192 84 - 100 us (4.6 - 5.4 TB/s; a copy of 1 GiB reaches 5.1), the values back 103 (4.4); 777 x 11008 7.6 and 8.6, one round of
+// workgroups of which the launch is 2.2.
 #include "mx4.hpp"
 
 namespace aweq {
