@@ -64,6 +64,8 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(QuantArgs g)
     raise_status(g.status, st);
 }
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 struct ValueArgs {
     const uint8_t *codes, *scales;
     int64_t rows, K, ldo;
@@ -71,14 +73,6 @@ struct ValueArgs {
     int groups;
     int64_t first;
 };
-
-// the value of a code: two bits of exponent and one of mantissa below the sign, under the block's power of two
-__device__ __forceinline__ float mx_value(uint32_t code, float step)
-{
-    const uint32_t m = code & 7u;
-    const float v = m < 2u ? 0.5f * (float)m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
-    return (code & 8u ? -v : v) * step;
-}
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void value_kernel(ValueArgs g)
@@ -89,16 +83,23 @@ __global__ __launch_bounds__(kThreads) void value_kernel(ValueArgs g)
     const int c = threadIdx.x & 15;
     if (r >= g.rows) return;
     const uint32_t scales = *reinterpret_cast<const uint32_t*>(g.scales + ((int64_t)group * g.rows + r) * 16 + mx_scale_place(c >> 2));
+    const int64_t first = (int64_t)group * kMxGroup, last = mx_panels(g.K) - 1;
+    uint32_t codes[kMxGroup];       // (all ahead of the first store)
+#pragma unroll
+    for (int p = 0; p < kMxGroup; ++p) codes[p] = *reinterpret_cast<const uint32_t*>(g.codes + (min(first + p, last) * g.rows + r) * 64 + c * 4);
 #pragma unroll
     for (int p = 0; p < kMxGroup; ++p) {
-        const int64_t panel = (int64_t)group * kMxGroup + p, k = panel * kMxPanel + c * 8;
+        const int64_t k = (first + p) * kMxPanel + c * 8;
         if (k >= g.K) continue;
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(g.codes + (panel * g.rows + r) * 64 + c * 4);
+        const uint32_t w = codes[p];
         const uint32_t s = scales >> (8 * p) & 255u;
         const float step = s == 255u ? NAN : s == 0u ? 0x1p-127f : __uint_as_float(s << 23);
+        // v_cvt_scalef32_pk_f32_fp4: a byte's two values, exact; the step is a factor of its own, since it may be subnormal or NaN
+        const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1),
+                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3)};
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = mx_value(w >> (4 * e) & 15u, step);
+        for (int e = 0; e < 8; ++e) x[e] = v[e / 2][e % 2] * step;
         store_unit(reinterpret_cast<E*>(g.out) + r * g.ldo + k, x);
     }
 }
