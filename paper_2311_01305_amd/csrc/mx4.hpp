@@ -26,13 +26,13 @@ __device__ __forceinline__ uint32_t mx_scale(uint32_t most)
 template <bool FACTOR, class E>
 __device__ __forceinline__ uint32_t mx_unit(const Unit<E>& u, const float factor[8], uint32_t& scale)
 {
-    float x[8];
-    uint32_t most = 0;
+    float x[8], top = 0.0f;       // (a NaN stays one)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         x[e] = FACTOR ? (float)u[e] * factor[e] : (float)u[e];
-        most = max(most, __float_as_uint(x[e]) & 0x7fffffffu);
+        top = __builtin_elementwise_maximum(top, __builtin_fabsf(x[e]));
     }
+    uint32_t most = __float_as_uint(top) & 0x7fffffffu;
     most = max(most, (uint32_t)partner<0>((int)most));
     most = max(most, (uint32_t)partner<1>((int)most));
     scale = mx_scale(most);

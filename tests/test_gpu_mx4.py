@@ -141,7 +141,7 @@ def test_ties_and_neighbours_at_every_exponent(B):
     assert np.array_equal(out.cpu().numpy().astype(np.float64), values(wc, wsc))
 
 
-@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("bad", [float("nan"), -float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 def test_what_is_not_finite(B, dt, bad):
     X = torch.randn(4, 160, device=DEV).to(TYPES[dt])
