@@ -3,8 +3,8 @@
 // HBM-bound: 2 bytes in and 17/32 out a value (16-bit types), and about five vector operations.  A block's 32 values are four lanes' units of eight; 16 lanes
 // have a row's panel and a wavefront four rows of it, four panels one after the other, so that the four scales that a lane's block has in them are the four bytes
 // which belong together, and the codes of four rows are 256 bytes in one piece.
-// Measured, bfloat16: 22016 x 8192 84 - 100 us (4.6 - 5.4 TB/s; a copy of 1 GiB reaches 5.1), the values back 103 (4.4); 777 x 11008 7.6 and 8.6, one round of
-// workgroups of which the launch is 2.2.
+// Measured, 16-bit types: 22016 x 8192 85 us (5.4 TB/s; a copy of 1 GiB reaches 5.1), the values back 95 (4.8); 777 x 11008 7.8 and 6.4, one round of workgroups
+// of which the launch is 2.2.
 #include "mx4.hpp"
 
 namespace aweq {
@@ -20,15 +20,14 @@ struct QuantArgs {
     uint8_t *codes, *scales;
     uint32_t* status;
     int groups;
-    int64_t first;
+    int64_t first;     // row of the launch
 };
 
 template <class E, bool FACTOR>
 __global__ __launch_bounds__(kThreads) void quant_kernel(QuantArgs g)
 {
-    const int64_t block = g.first + blockIdx.x;
-    const int group = (int)(block % g.groups);
-    const int64_t r = block / g.groups * kRows + threadIdx.x / 16;
+    const int group = (int)(blockIdx.x % (unsigned)g.groups);
+    const int64_t r = g.first + (int64_t)(blockIdx.x / (unsigned)g.groups) * kRows + threadIdx.x / 16;
     const int c = threadIdx.x & 15;
     const int64_t row = min(r, g.rows - 1);                                      // (rows past the last one: nothing is written)
     const int64_t k0 = (int64_t)group * (kMxPanel * kMxGroup) + c * 8;
@@ -71,15 +70,14 @@ struct ValueArgs {
     int64_t rows, K, ldo;
     void* out;
     int groups;
-    int64_t first;
+    int64_t first;     // row of the launch
 };
 
 template <class E>
 __global__ __launch_bounds__(kThreads) void value_kernel(ValueArgs g)
 {
-    const int64_t block = g.first + blockIdx.x;
-    const int group = (int)(block % g.groups);
-    const int64_t r = block / g.groups * kRows + threadIdx.x / 16;
+    const int group = (int)(blockIdx.x % (unsigned)g.groups);
+    const int64_t r = g.first + (int64_t)(blockIdx.x / (unsigned)g.groups) * kRows + threadIdx.x / 16;
     const int c = threadIdx.x & 15;
     if (r >= g.rows) return;
     const uint32_t scales = *reinterpret_cast<const uint32_t*>(g.scales + ((int64_t)group * g.rows + r) * 16 + mx_scale_place(c >> 2));
@@ -109,10 +107,11 @@ template <class A, class F>
 static int launch_blocks(A g, F kernel, hipStream_t st)
 {
     g.groups = (int)mx_groups(g.K);
-    const int64_t blocks = cdiv(g.rows, kRows) * g.groups, most = (1ll << 32) / kThreads - 1;
-    for (int64_t b = 0; b < blocks; b += most) {
-        g.first = b;
-        kernel<<<(unsigned)(blocks - b < most ? blocks - b : most), kThreads, 0, st>>>(g);
+    const int64_t most = ((1ll << 32) / kThreads - 1) / g.groups;     // blocks of rows of a launch
+    for (int64_t b = 0; b < cdiv(g.rows, kRows); b += most) {
+        g.first = b * kRows;
+        const int64_t left = cdiv(g.rows, kRows) - b;
+        kernel<<<(unsigned)((left < most ? left : most) * g.groups), kThreads, 0, st>>>(g);
     }
     return launch_status();
 }
