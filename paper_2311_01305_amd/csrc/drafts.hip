@@ -208,6 +208,9 @@ __global__ __launch_bounds__(kMaskThreads) void mask_kernel(MaskArgs g)
 }
 
 // ---------------------------------------------------------------- an accepted path to the front
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 struct KeepArgs {
     char *k_cache, *v_cache;
     float *k_step, *v_step;
@@ -222,6 +225,7 @@ struct KeepArgs {
 // A wavefront has a sequence's head in one of the caches.  Place j goes from kept[j] >= j to j, and the places rise: rows that have been written are none that is
 // still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.  A lane has the rows of one place of 64, found with as few
 // reads that wait for one another as there can be: the counts and places, then the pages, then the rows (one path of 5 of 12 tokens and 32 heads 8.7 us -> 8.1).
+// V: a vector type of the compiler's (of a structure the rows in flight would go to LDS)
 template <class V>
 __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
 {
@@ -377,7 +381,7 @@ extern "C" int aweq_kv_keep(void* k_cache, void* v_cache, float* k_step, float* 
     g.chunk = codes ? 8 : 16;
     g.chunks = (int)(D / 8);
     const dim3 grid((unsigned)B, (unsigned)Hk, 2);
-    if (codes) drafts::keep_kernel<uint2><<<grid, kWave, 0, as_stream(stream)>>>(g);
-    else drafts::keep_kernel<uint4><<<grid, kWave, 0, as_stream(stream)>>>(g);
+    if (codes) drafts::keep_kernel<drafts::u32x2><<<grid, kWave, 0, as_stream(stream)>>>(g);
+    else drafts::keep_kernel<drafts::u32x4><<<grid, kWave, 0, as_stream(stream)>>>(g);
     return launch_status();
 }

@@ -208,7 +208,7 @@ SIZES = [(1, 4, 32), (1, 64, 4096), (2, 100, 544), (3, 20, 96), (4, 2052, 1056),
          (130, 1300, 9056), (260, 512, 4160), (1000, 1036, 1440), (2300, 260, 800), (4200, 4100, 1312), (6000, 2052, 928), (900, 9000, 992),
          (1, 64, 32768), (4, 64, 8192), (2, 36, 33024), (70, 132, 33024), (3, 8, 64),
          (3, 6000, 544), (520, 6004, 544), (777, 4100, 1056), (1500, 2052, 1440), (777, 16388, 544),
-         (16, 36, 1024), (13, 132, 544), (2, 68, 8192), (16, 5004, 512), (9, 12000, 288)]
+         (16, 36, 1024), (13, 132, 544), (2, 68, 8192), (16, 5004, 512), (9, 12000, 288), (3, 8, 1 << 20), (40, 4, 1 << 20)]
 
 
 @pytest.mark.parametrize("T,N,K", SIZES)
