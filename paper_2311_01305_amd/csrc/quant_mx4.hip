@@ -3,8 +3,8 @@
 // HBM-bound: 2 bytes in and 17/32 out a value (16-bit types), and about five vector operations.  A block's 32 values are four lanes' units of eight; 16 lanes
 // have a row's panel and a wavefront four rows of it, four panels one after the other, so that the four scales that a lane's block has in them are the four bytes
 // which belong together, and the codes of four rows are 256 bytes in one piece.
-// Measured, 16-bit types: 22016 x 8192 85 us (5.4 TB/s; a copy of 1 GiB reaches 5.1), the values back 95 (4.8); 777 x 11008 7.8 and 6.4, one round of workgroups
-// of which the launch is 2.2.
+// Measured, 16-bit types: 22016 x 8192 76 - 81 us (5.6 - 6 TB/s; a copy of 1 GiB reaches 5.1), the values back 70 (6.5); 777 x 11008 7.8 and 6.4, one round of
+// workgroups of which the launch is 2.2.
 #include "mx4.hpp"
 
 namespace aweq {
@@ -23,7 +23,7 @@ struct QuantArgs {
     int64_t first;     // row of the launch
 };
 
-template <class E, bool FACTOR>
+template <class E, bool FACTOR, bool STREAM>
 __global__ __launch_bounds__(kThreads) void quant_kernel(QuantArgs g)
 {
     const int group = (int)(blockIdx.x % (unsigned)g.groups);
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kThreads) void quant_kernel(QuantArgs g)
 #pragma unroll
         for (int e = 0; e < 8; ++e) { raw[p][e] = (E)0.0f; factor[p][e] = 1.0f; }
         if (k < g.K) {
-            raw[p] = load_unit(from + k);
+            raw[p] = STREAM ? stream_unit(from + k) : load_unit(from + k);
             if constexpr (FACTOR) {
                 const f32x8 f = load_unit(g.factor + k);
 #pragma unroll
@@ -73,7 +73,8 @@ struct ValueArgs {
     int64_t first;     // row of the launch
 };
 
-template <class E>
+// STREAM: what is written goes past the caches
+template <class E, bool STREAM>
 __global__ __launch_bounds__(kThreads) void value_kernel(ValueArgs g)
 {
     const int group = (int)(blockIdx.x % (unsigned)g.groups);
@@ -98,7 +99,8 @@ __global__ __launch_bounds__(kThreads) void value_kernel(ValueArgs g)
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = v[e / 2][e % 2] * step;
-        store_unit(reinterpret_cast<E*>(g.out) + r * g.ldo + k, x);
+        if constexpr (STREAM) stream_unit(reinterpret_cast<E*>(g.out) + r * g.ldo + k, x);
+        else store_unit(reinterpret_cast<E*>(g.out) + r * g.ldo + k, x);
     }
 }
 
@@ -116,6 +118,26 @@ static int launch_blocks(A g, F kernel, hipStream_t st)
     return launch_status();
 }
 
+// past: what is read goes past the caches, where it does not fit them (us, bfloat16, through -> past them, the same tokens again / others: 16384 x 8192 60.8 -> 54.9 /
+// 64.9 -> 57.5, but 8192 x 8192 27.2 -> 30.8 / 35.2 -> 31.3, 777 x 11008 5.8 -> 6.1 / 7.6 -> 6.9; binary32 gains nothing)
+template <class E>
+static int launch_type(const QuantArgs& g, bool past, hipStream_t st)
+{
+    if constexpr (sizeof(E) == 2)
+        if (past) return g.factor ? launch_blocks(g, quant_kernel<E, true, true>, st) : launch_blocks(g, quant_kernel<E, false, true>, st);
+    return g.factor ? launch_blocks(g, quant_kernel<E, true, false>, st) : launch_blocks(g, quant_kernel<E, false, false>, st);
+}
+
+// Past the caches what they would not hold until somebody reads it (us, through -> past them, by itself / with a kernel that reads it: 22016 x 8192 98 -> 71 / 210 ->
+// 207, 8192 x 8192 40.5 -> 27.1 / 83.1 -> 82.8, but 777 x 11008 6.3 -> 5.1 / 12.9 -> 13.8)
+template <class E>
+static int launch_values(const ValueArgs& g, hipStream_t st)
+{
+    if constexpr (sizeof(E) == 2)
+        if (g.rows * g.K * 2 >= kCacheBytes / 2) return launch_blocks(g, value_kernel<E, true>, st);
+    return launch_blocks(g, value_kernel<E, false>, st);
+}
+
 }  // namespace mx
 
 int check_quant_mx4(const void* X, aweq_dtype dt, int64_t rows, int64_t K, int64_t ldx, const float* factor, const uint8_t* codes, const uint8_t* scales)
@@ -131,9 +153,10 @@ int launch_quant_mx4(const void* X, aweq_dtype dt, int64_t rows, int64_t K, int6
                      uint32_t* status, hipStream_t st)
 {
     const mx::QuantArgs g = {X, rows, K, ldx, factor, codes, scales, status, 0, 0};
-    if (dt == AWEQ_F16) return factor ? mx::launch_blocks(g, mx::quant_kernel<_Float16, true>, st) : mx::launch_blocks(g, mx::quant_kernel<_Float16, false>, st);
-    if (dt == AWEQ_BF16) return factor ? mx::launch_blocks(g, mx::quant_kernel<__bf16, true>, st) : mx::launch_blocks(g, mx::quant_kernel<__bf16, false>, st);
-    return factor ? mx::launch_blocks(g, mx::quant_kernel<float, true>, st) : mx::launch_blocks(g, mx::quant_kernel<float, false>, st);
+    const bool past = rows * K * (int64_t)dtype_size(dt) > kCacheBytes / 4 * 3;
+    if (dt == AWEQ_F16) return mx::launch_type<_Float16>(g, past, st);
+    if (dt == AWEQ_BF16) return mx::launch_type<__bf16>(g, past, st);
+    return mx::launch_type<float>(g, past, st);
 }
 
 }  // namespace aweq
@@ -158,7 +181,7 @@ extern "C" int aweq_mx4_values(const uint8_t* codes, const uint8_t* scales, int6
     if (!mx_shape_ok(rows, K) || ldo < K) return AWEQ_ERR_SHAPE;
     if (!aligned16(codes) || !aligned16(scales) || !aligned16(out) || (ldo * (int64_t)dtype_size(out_dt)) % 16 != 0) return AWEQ_ERR_ALIGN;
     const mx::ValueArgs g = {codes, scales, rows, K, ldo, out, 0, 0};
-    if (out_dt == AWEQ_F16) return mx::launch_blocks(g, mx::value_kernel<_Float16>, as_stream(stream));
-    if (out_dt == AWEQ_BF16) return mx::launch_blocks(g, mx::value_kernel<__bf16>, as_stream(stream));
-    return mx::launch_blocks(g, mx::value_kernel<float>, as_stream(stream));
+    if (out_dt == AWEQ_F16) return mx::launch_values<_Float16>(g, as_stream(stream));
+    if (out_dt == AWEQ_BF16) return mx::launch_values<__bf16>(g, as_stream(stream));
+    return mx::launch_values<float>(g, as_stream(stream));
 }
