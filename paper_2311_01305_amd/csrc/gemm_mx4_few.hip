@@ -27,7 +27,10 @@ __device__ __forceinline__ f32x4 mul(const v4i& w, const v4i& x, const f32x4& c,
 
 // E: void: the tokens' codes are in memory.  Otherwise every workgroup quantises the few tokens, of that type, for itself while its first weights are on their way, the
 // first one also for the caller; ROUNDS: units of eight values of a thread, at most.
-template <int TT, int NT, class E, int ROUNDS>
+// ONCE: the tokens are one tile, so that nobody else reads these weights: past the caches, which the other layers' weights have gone through since (us, through ->
+// past them: one token 22016 x 8192 20.0 -> 18.9, 16 tokens 21.8 -> 19.6, 8192 x 8192 8.5 -> 8.1; of the caches, a layer again and again, 7.2 -> 7.8; but 200
+// tokens 5120 x 1536, 13 tiles, 8.9 -> 9.5).
+template <int TT, int NT, bool ONCE, class E, int ROUNDS>
 __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int first_tile)
 {
     constexpr bool QX = !std::is_same<E, void>::value;
@@ -64,7 +67,10 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int 
     auto load = [&](int j, int group) {
         const int64_t p = min(group * kMxGroup + j, np - 1);   // (panels past the last one re-read it: they are not multiplied)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) w[j][n] = *reinterpret_cast<const v4i*>(wbase + p * wp + wo[n] * 64);
+        for (int n = 0; n < NT; ++n) {
+            const v4i* const at = reinterpret_cast<const v4i*>(wbase + p * wp + wo[n] * 64);
+            w[j][n] = ONCE ? __builtin_nontemporal_load(at) : *at;
+        }
         if constexpr (!QX) {
 #pragma unroll
             for (int t = 0; t < TT; ++t) x[j][t] = *reinterpret_cast<const v4i*>(xbase + p * xp + xo[t] * 64);
@@ -194,14 +200,14 @@ __global__ __launch_bounds__(kThreads) void gemm_mx4_few(MxArgs g, MxIn in, int 
 }
 
 // Token tiles ride on the grid's y dimension: at most 65535 of them to a launch, and fewer than 2^32 threads
-template <int TT, int NT, class E = void, int ROUNDS = 0>
+template <int TT, int NT, bool ONCE, class E = void, int ROUNDS = 0>
 static int launch_tile(MxArgs g, hipStream_t st, MxIn in = {})
 {
     constexpr bool QX = !std::is_same<E, void>::value;
     constexpr int kSums = kWaves * TT * NT * kWave * 16;
     static_assert(!QX || TT == 1, "one row of tokens");
     const int lds = kSums + (QX ? (int)(g.T * (mx_panels(g.K) * 64 + mx_groups(g.K) * 16)) : 0);
-    const void* fn = reinterpret_cast<const void*>(gemm_mx4_few<TT, NT, E, ROUNDS>);
+    const void* fn = reinterpret_cast<const void*>(gemm_mx4_few<TT, NT, ONCE, E, ROUNDS>);
     int dev = 0, cus = 0;
     if (lds > 32768 && (device_cus(dev, cus) != AWEQ_OK || raise_lds_limit(fn, dev, lds > 65536 ? 131072 : 65536) != AWEQ_OK)) return AWEQ_ERR_LAUNCH;
     const int64_t tiles = cdiv(g.T, 16 * TT), blocks = cdiv(g.N, 16 * NT), by_threads = ((1ll << 32) - 1) / (blocks * kThreads);
@@ -216,6 +222,12 @@ static int launch_tile(MxArgs g, hipStream_t st, MxIn in = {})
     return launch_status();
 }
 
+template <int TT, int NT>
+static int launch_given(const MxArgs& g, hipStream_t st)
+{
+    return g.T <= 16 * TT ? launch_tile<TT, NT, true>(g, st) : launch_tile<TT, NT, false>(g, st);
+}
+
 // Units of eight values that a workgroup quantises, and how many of them a thread has at most: all are asked for ahead of the first weights, so that a thread keeps
 // them in registers (us, 8 of them for every call -> as many as there are: one token 11008 x 4096 10.9 -> 7.8, 22016 x 8192 24.6 -> 21.5)
 static int64_t units_of(int64_t T, int64_t K) { return T * mx_panels(K) * 16; }
@@ -225,9 +237,9 @@ template <int NT, class E>
 static int launch_rounds(const MxArgs& g, const MxIn& in, hipStream_t st)
 {
     const int64_t units = units_of(g.T, g.K);
-    if (units <= kThreads) return launch_tile<1, NT, E, 1>(g, st, in);
-    if (units <= 2 * kThreads) return launch_tile<1, NT, E, 2>(g, st, in);
-    return launch_tile<1, NT, E, kMostRounds>(g, st, in);
+    if (units <= kThreads) return launch_tile<1, NT, true, E, 1>(g, st, in);
+    if (units <= 2 * kThreads) return launch_tile<1, NT, true, E, 2>(g, st, in);
+    return launch_tile<1, NT, true, E, kMostRounds>(g, st, in);
 }
 
 template <class E>
@@ -240,9 +252,9 @@ static int launch_quant(const MxArgs& g, const MxIn& in, int nt, hipStream_t st)
 
 int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st)
 {
-    if (tt == 1) return nt == 1 ? mxfew::launch_tile<1, 1>(g, st) : mxfew::launch_tile<1, 2>(g, st);
-    if (tt == 2) return nt == 1 ? mxfew::launch_tile<2, 1>(g, st) : mxfew::launch_tile<2, 2>(g, st);
-    return nt == 2 ? mxfew::launch_tile<4, 2>(g, st) : mxfew::launch_tile<4, 4>(g, st);
+    if (tt == 1) return nt == 1 ? mxfew::launch_given<1, 1>(g, st) : mxfew::launch_given<1, 2>(g, st);
+    if (tt == 2) return nt == 1 ? mxfew::launch_given<2, 1>(g, st) : mxfew::launch_given<2, 2>(g, st);
+    return nt == 2 ? mxfew::launch_given<4, 2>(g, st) : mxfew::launch_given<4, 4>(g, st);
 }
 
 // Every workgroup repeats the work.  That is less than a launch of the quantizer's own (3 us) up to two units a thread, or up to four where each compute unit has a
