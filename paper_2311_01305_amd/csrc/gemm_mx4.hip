@@ -6,10 +6,10 @@ namespace aweq {
 // What each form is modelled to take (us), from its time with a workgroup on few and on all of the 256 compute units; all are near a constant and a share of the
 // panels.  No form is below the read of the weight.  us, codes given, bfloat16 output, weights that are in no cache:
 //   tokens          1     16    32    64     128    256    333    512    1024   2048   4096
-//   4096 x 4096     4.5   4.7   5.2   6.1    7.3   10.4   11.7   12.6    16.8   23.2   35.9
-//   11008 x 4096    7.2   7.9   9.7  11.3   13.2   16.9   19.1   19.8    28.8   53.1   94.9
-//   8192 x 8192     8.8   8.9  10.2  12.3   19.5   21.1   26.5   28.1    38.3   61.0   117
-//   22016 x 8192   20.7  21.4  21.5  23.6   32.2   36.1   44.1   49.1    107    177    337      (96 MB: 4.6 TB/s at one token; 4.4 PFLOP/s at 4096)
+//   4096 x 4096     4.3   4.5   5.0   6.1    7.3   10.4   11.6   12.6    16.5   21.6   34.1
+//   11008 x 4096    6.9   7.5   9.4  10.7   13.2   17.1   19.1   19.7    27.4   51.4   93.0
+//   8192 x 8192     8.3   8.5   9.9  11.9   19.7   20.9   26.3   27.4    36.6   59.7   114
+//   22016 x 8192   19.0  19.6  21.4  23.5   32.3   36.1   43.2   48.0    102    176    331      (96 MB: 5 TB/s at one token; 4.5 PFLOP/s at 4096)
 struct MxPlan {
     enum { kFew, kMid, kTiled } form;
     int a, b;          // few: tt, nt; mid: square; tiled: mi

@@ -6,7 +6,7 @@
 // the byte; so a wavefront takes the panels in groups of four.
 //
 // Bound by the launch and a round trip or two for small weights, by HBM for large ones (us, weights that are in no cache, tokens quantised by the launch: one
-// token 4096 x 4096 4.7, 11008 x 4096 7.8, 22016 x 8192 21.5; codes given 4.5, 7.3, 20.5: 96 MB at 4.7 TB/s).
+// token 4096 x 4096 4.5, 11008 x 4096 7.4, 22016 x 8192 20.3; codes given 4.2, 6.9, 18.9: 96 MB at 5.1 TB/s).
 #include "gemm_mx4.hpp"
 
 #include <type_traits>
@@ -257,9 +257,9 @@ int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st)
     return nt == 2 ? mxfew::launch_given<4, 2>(g, st) : mxfew::launch_given<4, 4>(g, st);
 }
 
-// Every workgroup repeats the work.  That is less than a launch of the quantizer's own (3 us) up to two units a thread, or up to four where each compute unit has a
-// workgroup (us, in the launch / before it: 4096 x 4096 one token 4.7 / 7.7, four tokens 6.5 / 7.9; 11008 x 4096 two 8.9 / 10.7, four 11.8 / 10.6;
-// 8192 x 8192 two 10.9 / 12.1)
+// Every workgroup repeats the work.  That is less than a launch of the quantizer's own (2.7 us) up to two units a thread, or up to four where each compute unit has a
+// workgroup (us, in the launch / before it: 4096 x 4096 one token 4.5 / 7.0, four tokens 6.3 / 7.0; 11008 x 4096 two 8.6 / 9.9, four 11.8 / 10.6;
+// 8192 x 8192 two 10.4 / 11.0)
 bool mx4_few_quantises(int64_t T, int64_t N, int64_t K, int nt)
 {
     const int64_t units = mxfew::units_of(T, K);

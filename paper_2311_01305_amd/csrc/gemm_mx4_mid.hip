@@ -5,8 +5,8 @@
 // ring of LDS slots filled by LDS-DMA loads, one barrier a stage; a stage brings the scales of its group of four panels along, and a wavefront shifts its panel's
 // to the lowest byte.
 //
-// Bound by the loads of the one workgroup that a compute unit has room for, 40 - 60 GB/s with a barrier a stage: 64 tokens 22016 x 8192 23.6 us (4.1 TB/s of
-// weights), 512 tokens 4096 x 4096 12.6 (1.4 PFLOP/s), 8192 x 8192 28.1 (2.4).
+// Bound by the loads of the one workgroup that a compute unit has room for, 40 - 60 GB/s with a barrier a stage: 64 tokens 22016 x 8192 23.5 us (4.1 TB/s of
+// weights), 512 tokens 4096 x 4096 12.6 (1.4 PFLOP/s), 8192 x 8192 27.4 (2.5).
 #include "gemm_mx4.hpp"
 
 namespace aweq {
