@@ -1016,7 +1016,7 @@ __device__ __forceinline__ bool wide_block(const Args& g, const Job& j, char* ld
 // tile by itself: 8-bit codes, row tiles of 64, 5 tokens of 16 sequences of up to 6000 keys 42.0 us -> 36.6; binary16, 711 tokens x 8 heads 21.5 -> 20.0)
 constexpr int waves_wanted(int D, int MT) { return D == 64 ? (MT == 2 ? 2 : 4) : D == 128 ? (MT == 0 ? 3 : 2) : MT == 1 ? 2 : 1; }
 
-// (trees) Rows of the sequences: those behind them are left as they are
+// Rows of the sequences (q_start given): those behind them are left as they are by trees and by the join
 __device__ __forceinline__ int64_t rows_of_batch(const Args& g) { return min(max((int64_t)scalar_at(g.q_start, g.B), (int64_t)0), g.T); }
 
 // (trees) The n-th longest of up to 64 sequences: workgroups are dealt out in order, and the last ones to begin should be short (us, as they come -> longest
@@ -1128,7 +1128,8 @@ __global__ __launch_bounds__(256) void join_kernel(Args g)
     __shared__ f32x4 s_part[W > 1 ? W : 1][W > 1 ? D / 4 : 1];
     const int wave = threadIdx.x / kWave, slice = wave % W, lane = threadIdx.x & (kWave - 1);
     const int64_t row = (int64_t)blockIdx.x * kRowsOf + wave / W, all_rows = g.T * g.Hq;
-    if (row >= (TREE ? rows_of_batch(g) * g.Hq : all_rows)) return;     // (W > 1: all of the workgroup or nobody)
+    // (rows past q_start[B]: no sequence's workgroup has written a part of them.  W > 1: all of the workgroup or nobody)
+    if (row >= (TREE || g.q_start ? rows_of_batch(g) * g.Hq : all_rows)) return;
     constexpr int kLanes = D / 4, kAtOnce = kWave / kLanes, kOf = W > 1 ? kJoinParts / kWave : 1, kFlight = 8;
     const int sub = lane / kLanes, at = lane % kLanes * 4;
     float2 ml[kOf];

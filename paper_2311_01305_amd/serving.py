@@ -245,7 +245,7 @@ class AttentionBlock:
         self.step, self.zero, self.rowsum = new(max_tokens, dtype=torch.float32), new(max_tokens, dtype=torch.int32), new(max_tokens, dtype=torch.int32)
         self.qkv = new(max_tokens, qkv.N, dtype=cache.dtype)
         self.q = new(max_tokens, q_heads * D, dtype=cache.dtype)
-        self.attended = torch.zeros(max_tokens, q_heads * D, dtype=cache.dtype, device=device)   # (rows past a batch's tokens are left as they are, and quantised)
+        self.attended = new(max_tokens, q_heads * D, dtype=cache.dtype)
         self.y = new(max_tokens, out.N, dtype=cache.dtype)
         self.ws, self.kept = new(16, dtype=torch.uint8), []
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
@@ -272,7 +272,7 @@ class AttentionBlock:
     def __call__(self, x, pos, slot, lens, table, q_start, max_len, max_q, prefix_table=None, prefix_len=0, mask=None):
         """x [T, hidden]: the step's tokens, sequence after sequence (q_start [B + 1], None: one each); pos [T] int32, slot [T] int64; lens [B]: the
         sequences' own keys with these tokens; table [B, ..]: their pages; mask [T, words] int64: which of its sequence's new tokens each one sees (None: those before
-        it and itself).  Returns [T, hidden], a buffer of the block's."""
+        it and itself).  Rows past q_start[B], of a step that is filled up, have no part in the others' results.  Returns [T, hidden], a buffer of the block's."""
         T, c = x.shape[0], self.cache
         if T > self.max_tokens or x.dtype != c.dtype:
             raise ValueError("more tokens than max_tokens, or another type than the cache's")
@@ -301,6 +301,8 @@ class AttentionBlock:
         B.aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, width, width, width, pos, self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm,
                          self.eps, self.q, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, slot, self.status)
         self._scratch(B.aweq_prefix_attention_ws(T, Hq, Hk, D, batch, max_q, prefix_len, max_len))
+        if q_start is not None:
+            self.attended[:T].zero_()      # (rows behind the sequences' are nobody's, and are quantised like the others: not what an earlier step left there)
         if mask is None:
             B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
                                     table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
