@@ -503,12 +503,12 @@ int aweq_tree_attention(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int
                         int64_t max_len, int64_t max_q, const uint64_t* mask, int64_t mask_ld, float scale, void* out, int64_t ldo, float* lse,
                         void* ws, size_t ws_bytes, uint32_t* status, void* stream);
 
-/* ---- After a step some of whose new tokens are kept: kept[b][j], j < count[b] (int32, pitch kept_ld >= every count), are their places among sequence
+/* ---- After a step some of whose new tokens are kept: kept[b][j], j < count[b] (int32, pitch kept_ld >= every count; what lies behind them is not read), are their places among sequence
  * b's m new tokens, in strictly increasing order.  Their keys and values (and steps) move to the places 0 .. count - 1 of those, and change[b] = count - m is what
  * aweq_step_plan takes to drop the rest.  The tokens behind the kept ones are unspecified afterwards.  A count outside [0, min(m, kept_ld)], places out of
  * order or outside [0, m), lens[b] < m, or pages outside [0, pages): AWEQ_ST_INDEX, and nothing of that sequence is moved (change 0; a page outside: the
  * rows on it alone); so for a sequence longer than table_ld pages.  No two sequences may have a page of new tokens in common.  Caches as in aweq_kv_append;
- * T, q_start, lens, table: the step's.  change over an input: AWEQ_ERR_ALIGN.  B <= 2^20, Hk < 2^16, B * Hk <= 2^24, T <= 2^24. */
+ * T, q_start, lens, table: the step's.  change over an input, or among the min(kept_ld, T) entries from a row of kept on: AWEQ_ERR_ALIGN.  B <= 2^20, Hk < 2^16, B * Hk <= 2^24, T <= 2^24. */
 int aweq_kv_keep(void* k_cache, void* v_cache, float* k_step, float* v_step, aweq_dtype cache_dt, int64_t pages, int64_t page_size, int64_t Hk, int64_t D,
                  const int32_t* table, int64_t table_ld, const int32_t* lens, const int32_t* q_start, int64_t B, int64_t T,
                  const int32_t* kept, int64_t kept_ld, const int32_t* count, int32_t* change, uint32_t* status, void* stream);

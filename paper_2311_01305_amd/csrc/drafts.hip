@@ -223,8 +223,8 @@ struct KeepArgs {
 };
 
 // A wavefront has a sequence's head in one of the caches.  Place j goes from kept[j] >= j to j, and the places rise: rows that have been written are none that is
-// still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.  A lane has the rows of one place of 64, found with as few
-// reads that wait for one another as there can be: the counts and places, then the pages, then the rows (us: one path of 5 of 12 tokens and 32 heads 3.5, 32 of 4 of 8 4.0, 256 of 9 of 64 with 8 heads of codes 4.9, a launch being 2.2).
+// still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.  A lane has the rows of one place of 64, found with few
+// reads that wait for one another: the counts, then the places (no more of a row than its count need be there), the pages, the rows (us: one path of 5 of 12 tokens and 32 heads 3.5, 32 of 4 of 8 4.0, 256 of 9 of 64 with 8 heads of codes 4.9, a launch being 2.2).
 // V: a vector type of the compiler's (of a structure the rows in flight went to LDS: one path 8.0 us, 32 of them 17)
 template <class V>
 __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
@@ -232,14 +232,14 @@ __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
     const int b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x;
     const bool values = blockIdx.z != 0;
     const int32_t* const kept = g.kept + b * g.kept_ld;
-    const int64_t last_kept = g.kept_ld - 1;
-    int place = kept[min((int64_t)lane, last_kept)];          // (of place `lane`; past the count anything)
     const int64_t t0 = g.q_start[b], t1 = g.q_start[b + 1];
     const int len = g.lens[b], n = g.count[b];
     bool ok = t0 >= 0 && t1 >= t0 && t1 <= g.T && len >= t1 - t0 && len <= (g.table_ld << g.page_shift);
     const int m = ok ? (int)(t1 - t0) : 0, base = len - m;
     ok = ok && n >= 0 && n <= m && n <= g.kept_ld;
+    int place = 0;          // kept[b][lane]
     if (ok) {
+        if (lane < n) place = kept[lane];
         bool order = true;
         const int before = __shfl_up(place, 1);
         if (lane < n) order = place > (lane ? before : -1) && place < m;
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)
         for (int from = 0; from < n; from += kWave) {
             // rows of place from + lane: where they are, and where they go; -1: they stay
             const int j = from + lane;
-            if (from) place = kept[min((int64_t)j, last_kept)];
+            if (from && j < n) place = kept[j];
             int64_t source = -1, dest = -1;
             if (j < n && place != j) {
                 const int ks = base + place, kd = base + j;
