@@ -1034,6 +1034,40 @@ __device__ __forceinline__ int longest_first(const int32_t* lens, int B, int n)
     return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < B && ahead == n));
 }
 
+// A sequence's rows and how many keys it has, clamped to what the call was given; status: what lay outside.  read: an element of the tables
+struct Sequence {
+    int64_t t0;
+    int tokens, len;
+    uint32_t status;
+};
+template <bool TREE, class Read>
+__device__ __forceinline__ Sequence sequence(const Args& g, int b, Read read)
+{
+    Sequence s = {b, 1, 0, 0};
+    if (g.q_start) {
+        int64_t t0 = read(g.q_start, b), t1 = read(g.q_start, b + 1);
+        if (t0 < 0 || t1 < t0 || t1 > g.T || t1 - t0 > g.max_q) s.status |= AWEQ_ST_INDEX;
+        t0 = min(max(t0, (int64_t)0), g.T);
+        t1 = min(max(t1, t0), min(g.T, t0 + g.max_q));
+        s.t0 = t0;
+        s.tokens = (int)(t1 - t0);
+    }
+    s.len = read(g.lens, b);
+    const int most = (int)min((int64_t)g.max_len, g.table_ld << g.page_shift);
+    if (s.len < (TREE ? s.tokens : 0) || s.len > most) s.status |= AWEQ_ST_INDEX;
+    s.len = min(max(s.len, 0), most);
+    return s;
+}
+
+// Where the launch has no workgroups for the sequences (no keys of their own), one looks at what they are told to be
+template <bool TREE>
+__device__ __forceinline__ void look_at_sequences(const Args& g)
+{
+    uint32_t st = 0;
+    for (int b = (int)threadIdx.x; b < g.B; b += kThreads) st |= sequence<TREE>(g, b, [](const int32_t* p, int64_t i) { return p[i]; }).status;
+    raise_status(g.status, st);
+}
+
 // MT: 16 MT rows for each wavefront of the tall form; 0: a launch without it.  STREAM (MT 0): keys and values past the caches (rule and figures at the launch)
 template <class E, int D, int MT, bool STREAM, bool SEEN, bool TREE>
 __device__ __forceinline__ bool attention_block(const Args& g, int block, char* lds)
@@ -1057,7 +1091,6 @@ __device__ __forceinline__ bool attention_block(const Args& g, int block, char* 
     j.pa = j.pb = j.oa = j.ob = 0;
     j.sees0 = 0;
     j.table = g.table;
-    uint32_t est = 0;
     if (shared) {
         j.t0 = 0;
         j.rows = (int)(TREE ? rows_of_batch(g) : g.T) * g.G;
@@ -1065,21 +1098,10 @@ __device__ __forceinline__ bool attention_block(const Args& g, int block, char* 
         j.pa = split * w.chunk;
         j.pb = min(j.pa + w.chunk, g.prefix_len);
     } else {
-        int64_t t0 = b, t1 = b + 1;
-        if (g.q_start) {
-            t0 = scalar_at(g.q_start, b);
-            t1 = scalar_at(g.q_start, b + 1);
-            if (t0 < 0 || t1 < t0 || t1 > g.T || t1 - t0 > g.max_q) est |= AWEQ_ST_INDEX;
-            t0 = min(max(t0, (int64_t)0), g.T);
-            t1 = min(max(t1, t0), min(g.T, t0 + g.max_q));
-        }
-        const int tokens = (int)(t1 - t0);
-        int len = scalar_at(g.lens, b);
-        const int most = (int)min((int64_t)g.max_len, g.table_ld << g.page_shift);
-        if (len < (TREE ? tokens : 0) || len > most) est |= AWEQ_ST_INDEX;
-        len = min(max(len, 0), most);
-        if (est && threadIdx.x == 0) raise_status(g.status, est);
-        j.t0 = t0;
+        const Sequence s = sequence<TREE>(g, b, [](const int32_t* p, int64_t i) { return scalar_at(p, i); });
+        if (s.status && threadIdx.x == 0) raise_status(g.status, s.status);
+        const int tokens = s.tokens, len = s.len;
+        j.t0 = s.t0;
         j.rows = tokens * g.G;
         if (j.row0 >= j.rows) return false;
         j.sees0 = TREE ? len - tokens : len - tokens + 1;
@@ -1107,6 +1129,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(waves_
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     int block = (int)blockIdx.x;
+    if (g.own.splits == 0 && block == 0) look_at_sequences<TREE>(g);
     if (!attention_block<E, D, MT, STREAM, false, TREE>(g, block, lds) || Shape<E, D>::kCodes) return;
     // Once more, from the arguments on: nothing is kept in registers for it
     typedef const __attribute__((address_space(4))) Args* ConstArgs;
@@ -1369,7 +1392,7 @@ static int attend_call(const void* q, aweq_dtype dt, int64_t T, int64_t Hq, int6
     g.q = q; g.k_cache = k_cache; g.v_cache = v_cache; g.k_step = k_step; g.v_step = v_step;
     g.prefix_table = prefix_table; g.table = table; g.lens = lens; g.q_start = q_start;
     g.out = out; g.lse = lse; g.status = status; g.mask = mask; g.mask_ld = mask_ld;
-    g.T = T; g.ldq = ldq; g.ldo = ldo; g.table_ld = table_ld; g.prefix_len = (int)prefix_len; g.max_len = (int)max_len;
+    g.T = T; g.ldq = ldq; g.ldo = ldo; g.table_ld = max_len > 0 ? table_ld : 0; g.prefix_len = (int)prefix_len; g.max_len = (int)max_len;
     g.pages = (int)pages; g.page_size = (int)page_size; g.page_shift = __builtin_ctz((unsigned)page_size);
     g.B = (int)B;
     g.Hq = (int)Hq; g.Hk = (int)Hk; g.G = (int)(Hq / Hk); g.max_q = (int)max_q;
