@@ -300,14 +300,15 @@ class AttentionBlock:
         q, k, v = self.qkv[:T].split([Hq * D, Hk * D, Hk * D], 1)
         B.aweq_kv_append(q, k, v, dt, T, Hq, Hk, D, width, width, width, pos, self.freq, self.rot, self.interleaved, self.gain, self.q_norm, self.k_norm,
                          self.eps, self.q, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, slot, self.status)
-        self._scratch(B.aweq_prefix_attention_ws(T, Hq, Hk, D, batch, max_q, prefix_len, max_len))
+        rows = T if q_start is None else min(T, batch * max_q)      # (the others of a step that is filled up are nobody's, and what was reserved is for no more)
+        self._scratch(B.aweq_prefix_attention_ws(rows, Hq, Hk, D, batch, max_q, prefix_len, max_len))
         if q_start is not None:
             self.attended[:T].zero_()      # (rows behind the sequences' are nobody's, and are quantised like the others: not what an earlier step left there)
         if mask is None:
-            B.aweq_prefix_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
+            B.aweq_prefix_attention(self.q, dt, rows, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
                                     table, table.stride(0), lens, q_start, batch, max_len, max_q, D ** -0.5, self.attended, Hq * D, None, self.ws, self.status)
         else:
-            B.aweq_tree_attention(self.q, dt, T, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
+            B.aweq_tree_attention(self.q, dt, rows, Hq, D, Hq * D, c.k, c.v, c.k_step, c.v_step, c.kind, c.pages, c.page_size, Hk, prefix_table, prefix_len,
                                   table, table.stride(0), lens, q_start, batch, max_len, max_q, mask, mask.stride(0), D ** -0.5, self.attended, Hq * D, None,
                                   self.ws, self.status)
         self._product(self.out_layer, self.attended[:T], self.y)
