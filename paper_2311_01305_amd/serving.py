@@ -78,10 +78,12 @@ class Mx4Linear:
 
     @classmethod
     def from_weight(cls, W: torch.Tensor, bias: Optional[torch.Tensor] = None, factor: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
-        """W [N x K], float32, float16 or bfloat16, rows in one piece."""
+        """W [N x K], float32, float16 or bfloat16, rows in one piece; N a multiple of 4, K of 32."""
         if W.dim() != 2 or W.stride(1) != 1:
             raise ValueError("a matrix whose rows are in one piece")
         N, K = W.shape
+        if N % 4 or not B.aweq_mx4_code_bytes(N, K):
+            raise ValueError("output channels in fours and input channels in blocks of 32, up to 2^20: the product reads no others")
         if factor is not None:
             _check("factor", factor, torch.float32, (K,), W.device)
         if bias is not None:
