@@ -104,6 +104,9 @@ class Mx4Linear:
         biases = [None] * len(gb.Ns) if biases is None else list(biases)
         if len(biases) != len(gb.Ns):
             raise ValueError("a bias, or None, for each layer")
+        for i, (b, N) in enumerate(zip(biases, gb.Ns)):
+            if b is not None:
+                _check(f"bias {i}", b, torch.float32, (N,), gb.per[i]["W_hat"].device)
         bias = None
         if any(b is not None for b in biases):
             bias = torch.cat([torch.zeros_like(p["step_w"]) if b is None else b for p, b in zip(gb.per, biases)])
