@@ -44,6 +44,13 @@ static MxPlan plan_mx4(int64_t T, int64_t N, int64_t K)
     return best;
 }
 
+// 100 form + 10 a + b of the form that a shape is given to (the tests name the one that each of their shapes is meant for)
+int mx4_form(int64_t T, int64_t N, int64_t K)
+{
+    const MxPlan p = plan_mx4(T, N, K);
+    return 100 * p.form + 10 * p.a + p.b;
+}
+
 }  // namespace aweq
 
 using namespace aweq;

@@ -31,4 +31,6 @@ int launch_mx4_few(const MxArgs& g, int tt, int nt, hipStream_t st);
 bool mx4_few_quantises(int64_t T, int64_t N, int64_t K, int nt);
 int launch_mx4_few_quant(const MxArgs& g, const MxIn& in, aweq_dtype dt, int nt, hipStream_t st);
 
+int mx4_form(int64_t T, int64_t N, int64_t K);
+
 }  // namespace aweq
