@@ -560,7 +560,8 @@ def mfma_probe(torch, dev, iters=20000, reps=12):
     res = {}
     for mode, name, ops in ((0, "constant_bytes", 65536), (1, "random_bytes", 65536), (2, "small_signed_codes", 65536),
                             (3, "f16_32x32x16_random_values", 32768), (4, "small_codes_first_operand_random_second", 65536),
-                            (5, "random_first_operand_small_codes_second", 65536)):
+                            (5, "random_first_operand_small_codes_second", 65536), (6, "f4_32x32x64_random_codes", 131072),
+                            (7, "f4_32x32x64_zeros", 131072)):
         for _ in range(reps):  # the clock settles over a few tens of milliseconds
             assert lib.bench_probe_mfma_clock(iters, mode, out.data_ptr(), st) == 0
         cyc, ticks = int(out[0].item()), int(out[1].item())

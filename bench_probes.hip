@@ -110,6 +110,44 @@ __global__ __launch_bounds__(256) void mfma_clock_probe(int iters, int operand_m
     }
 }
 
+// operand_mode 6, 7: the same loop with v_mfma_scale_f32_32x32x64_f8f6f4 on 4-bit codes, any of them or zeros alone, all scales 1
+__global__ __launch_bounds__(256) void mfma_clock_probe_f4(int iters, int zeros, unsigned long long* out)
+{
+    typedef int pv8i __attribute__((ext_vector_type(8)));
+    pv4i a[4], b[4];
+    unsigned x = threadIdx.x * 2654435761u + blockIdx.x * 40503u + 12345u;
+    for (int i = 0; i < 4; ++i)
+        for (int c = 0; c < 4; ++c) {
+            x ^= x << 13; x ^= x >> 17; x ^= x << 5;
+            a[i][c] = zeros ? 0 : (int)x;
+            x ^= x << 13; x ^= x >> 17; x ^= x << 5;
+            b[i][c] = zeros ? 0 : (int)x;
+        }
+    pv16f acc[4][4];
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j)
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    auto operand = [](pv4i v) -> pv8i { return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1); };   // (a 4-bit one is in the first four registers)
+    const unsigned long long c0 = __builtin_amdgcn_s_memtime(), r0 = __builtin_amdgcn_s_memrealtime();
+    for (int it = 0; it < iters; ++it) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a[i]), operand(b[j]), acc[i][j], 4, 4, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+    }
+    float s = 0.0f;
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j)
+            for (int v = 0; v < 16; ++v) s += acc[i][j][v];
+    const unsigned long long c1 = __builtin_amdgcn_s_memtime(), r1 = __builtin_amdgcn_s_memrealtime();
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        out[0] = c1 - c0;
+        out[1] = r1 - r0;
+        out[2] = (unsigned long long)__float_as_uint(s);  // keeps the accumulators alive
+    }
+}
+
 typedef int sv4i __attribute__((ext_vector_type(4)));
 typedef int sv2i __attribute__((ext_vector_type(2)));
 constexpr int kStreamInFlight = 8;
@@ -146,17 +184,20 @@ __global__ __launch_bounds__(256) void stream_probe(const sv4i* __restrict__ in,
 // out[3] (device, uint64): shader-clock cycles of one wavefront's loop, 100 MHz reference ticks of the
 // same interval, a checksum.  operand_mode 0: constant bytes, 1: uniformly random bytes, 2: small signed
 // codes (int8 32x32x32 MFMA, 65536 ops each); 3: the binary16 32x32x16 MFMA (32768 flop each) on
-// activation- and weight-like values; 4 / 5: small codes in the first / second int8 operand only, any byte in the other.  One workgroup of four wavefronts per compute unit, iters x 16
+// activation- and weight-like values; 4 / 5: small codes in the first / second int8 operand only, any byte in the other; 6 / 7: the scaled 4-bit
+// 32x32x64 MFMA (131072 flop each) on any codes / on zeros.  One workgroup of four wavefronts per compute unit, iters x 16
 // instructions per wavefront.  Returns 0 or a negative number (bad argument / launch refused).
 extern "C" int bench_probe_mfma_clock(int iters, int operand_mode, uint64_t* out, void* stream)
 {
-    if (!out || iters <= 0 || iters > (1 << 22) || operand_mode < 0 || operand_mode > 5) return -1;
+    if (!out || iters <= 0 || iters > (1 << 22) || operand_mode < 0 || operand_mode > 7) return -1;
     int dev = 0, cus = 0;
     if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
         return -2;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (operand_mode == 3)
         probes::mfma_clock_probe_f16<<<(unsigned)cus, 256, 0, st>>>(iters, reinterpret_cast<unsigned long long*>(out));
+    else if (operand_mode >= 6)
+        probes::mfma_clock_probe_f4<<<(unsigned)cus, 256, 0, st>>>(iters, operand_mode == 7, reinterpret_cast<unsigned long long*>(out));
     else
         probes::mfma_clock_probe<<<(unsigned)cus, 256, 0, st>>>(iters, operand_mode, reinterpret_cast<unsigned long long*>(out));
     return hipGetLastError() == hipSuccess ? 0 : -2;
