@@ -27,8 +27,8 @@
 // such calls alone (the others: a look at the outputs, us, before -> now: 6 prompts behind 4111 keys 373.3 -> 376.2, 3 of 700 tokens 24.0 -> 25.1).
 //
 // Trees: of its sequence's last keys, the new tokens, a row sees those whose bits its token's mask has.  Tiles that hold such keys ask the mask where the others compare
-// places; all else is the same (us, masks included: 12 tokens x 32 heads behind 1900 keys 15.6; 5 sequences of 1 - 211 tokens x 32 heads, up to 3333 keys behind 4111, 122;
-// 24 of 40 x 64, 2000 - 9000 behind 2000, codes, 427: 551 TFLOP/s).
+// places; all else is the same (us, masks included: 12 tokens x 32 heads behind 1900 keys 15.4; 5 sequences of 1 - 211 tokens x 32 heads, up to 3333 keys behind 4111, 123;
+// 24 of 40 x 64, 2000 - 9000 behind 2000, codes, 426: 552 TFLOP/s).
 //
 // An 8-bit cache is multiplied as binary16 codes.  The step of a key goes to its score.  The step of a value goes to the probability that multiplies
 // its codes, p' = p step 2^e, with a power of two for each row that keeps p' in binary16's range and follows the largest step which the row has seen, as the
@@ -404,7 +404,10 @@ struct Rows {
         }
     }
 
-    // Scores to probabilities for the second product
+    // Scores to probabilities for the second product, which takes them in the type of what they multiply: 16 bits (the sum l and the maximum are of the unrounded ones, in
+    // binary32).  Each is off by half a last place at most, 2^-11 of itself (bfloat16: 2^-8), the output by no more than that of sum p |v| / sum p, which is what its own
+    // rounding may be off by; a product that takes them as a sum of two of 16 bits would be two.  (Against softmax in 64 bits, 2-norm, an output that is rounded alone -> this:
+    // 12 drafted tokens behind 1900 keys, binary16, 2.1e-4 -> 2.5e-4; 24 of 40 behind up to 11000, codes, 2.1e-4 -> 2.9e-4; 5 of up to 211, bfloat16, 1.7e-3 -> 2.3e-3)
     template <int N, class VSteps>
     __device__ __forceinline__ void weights(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], VSteps v_steps, bool odd)
     {
@@ -1021,7 +1024,7 @@ __device__ __forceinline__ int64_t rows_of_batch(const Args& g) { return min(max
 
 // (trees) The n-th longest of up to 64 sequences: workgroups are dealt out in order, and the last ones to begin should be short (us, as they come -> longest
 // first: 40 tokens x 8 heads of 24 sequences of 2000 - 9000 keys behind 2000, codes, 520 -> 422; 8 x 4 of 40 of 500 - 4000 84 -> 65, binary16 97 -> 88; 211 x 4 of 5 of up to 3333
-// behind 4111 126 -> 118)
+// behind 4111 126 -> 118; 64 sequences of 8 x 4, 500 - 4000 behind 2000, codes, 173, but 65 of them, as they come, 206)
 __device__ __forceinline__ int longest_first(const int32_t* lens, int B, int n)
 {
     if (B < 2 || B > kWave) return n;

@@ -224,7 +224,8 @@ struct KeepArgs {
 
 // A wavefront has a sequence's head in one of the caches.  Place j goes from kept[j] >= j to j, and the places rise: rows that have been written are none that is
 // still to be read, so that as many as lanes and registers hold go at a time, reads ahead of writes.  A lane has the rows of one place of 64, found with few
-// reads that wait for one another: the counts, then the places (no more of a row than its count need be there), the pages, the rows (us: one path of 5 of 12 tokens and 32 heads 3.5, 32 of 4 of 8 4.0, 256 of 9 of 64 with 8 heads of codes 4.9, a launch being 2.2).
+// reads that wait for one another: the counts, then the places (no more of a row than its count need be there), the pages, the rows (us: one path of 5 of 12 tokens and 32 heads
+// 3.6, 256 of 9 of 64 with 8 heads of codes 5.2, a launch being 2.2).
 // V: a vector type of the compiler's (of a structure the rows in flight went to LDS: one path 8.0 us, 32 of them 17)
 template <class V>
 __global__ __launch_bounds__(kWave) void keep_kernel(KeepArgs g)

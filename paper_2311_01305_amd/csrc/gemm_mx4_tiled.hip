@@ -8,8 +8,8 @@
 // The weight is the instruction's first operand: a lane ends up with four consecutive channels of one token.  The bias is what the sums begin with.
 // Persistent: the first panels of a workgroup's next tile are requested before it stores the current one.
 //
-// Several rounds are bound by the clock under load: 8192 x 8192 x 22016 585 - 610 us, 4.9 - 5.05 PFLOP/s, where the matrix unit alone sustains 6.4 on random codes
-// (9.4 on zeros).  A single round of 172 workgroups, 333 tokens 22016 x 8192, takes 44 us: products and LDS reads with nothing loaded 37 (on zeros 30), loads with
+// Several rounds are bound by the clock under load: 8192 x 8192 x 22016 585 - 610 us, 4.9 - 5.05 PFLOP/s, where the matrix unit alone sustains 6.7 on random codes
+// (9.8 on zeros).  A single round of 172 workgroups, 333 tokens 22016 x 8192, takes 44 us: products and LDS reads with nothing loaded 37 (on zeros 30), loads with
 // nothing multiplied 41 (33 where the weights are in the caches), and a barrier a panel lets them overlap in part.  A fifth slot for tiles of 192 tokens
 // changed nothing.
 #include "gemm_mx4.hpp"

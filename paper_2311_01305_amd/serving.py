@@ -68,7 +68,8 @@ class QuantLinear:
 @dataclass
 class Mx4Linear:
     """A layer whose weight is in microscaled 4-bit floating point (aweq_quant_mx4), its tokens quantised the same way in the product.  factor: what the
-    input's channels are multiplied by first (an equalization's 1 / s), or None."""
+    input's channels are multiplied by first (an equalization's 1 / s), or None.  bias: the layer's own, as it is: unlike a QuantLinear's it has no mean error of the
+    codes taken off (Eq. 12-15 is of a quantizer whose errors the calibration has measured, which it does for integers alone)."""
     N: int
     K: int
     codes: torch.Tensor
