@@ -405,8 +405,8 @@ struct Rows {
     }
 
     // Scores to probabilities for the second product, which takes them in the type of what they multiply: 16 bits (the sum l and the maximum are of the unrounded ones, in
-    // binary32).  Each is off by half a last place at most, 2^-11 of itself (bfloat16: 2^-8), the output by no more than that of sum p |v| / sum p, which is what its own
-    // rounding may be off by; a product that takes them as a sum of two of 16 bits would be two.  (Against softmax in 64 bits, 2-norm, an output that is rounded alone -> this:
+    // binary32).  Each is off by half a last place at most, 2^-11 of itself (bfloat16: 2^-8), the output by no more than that share of sum p |v| / sum p, and by that
+    // share of itself where it is rounded; a product that takes them as a sum of two of 16 bits would be two.  (Against softmax in 64 bits, 2-norm, an output that is rounded alone -> this:
     // 12 drafted tokens behind 1900 keys, binary16, 2.1e-4 -> 2.5e-4; 24 of 40 behind up to 11000, codes, 2.1e-4 -> 2.9e-4; 5 of up to 211, bfloat16, 1.7e-3 -> 2.3e-3)
     template <int N, class VSteps>
     __device__ __forceinline__ void weights(f32x4 (&s)[MT][N], V (&p)[MT][N / 2], VSteps v_steps, bool odd)
